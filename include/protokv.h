@@ -441,7 +441,167 @@ protokv_status protokv_profile(protokv_t h, uint32_t kernel_mask);
 /* Sums the recorded event pairs into `out` (waits for each end event). */
 protokv_status protokv_profile_read(protokv_t h, protokv_kernel_times* out);
 
-/* Message for the last failure on h (or of protokv_init when h is NULL).
+/* ---------------------------------------------------------------------------
+ * The exact part of the attention around the readout: tokens among themselves
+ * (the text of a question or an answer, a clip before it is compressed) and
+ * over a dialogue kept in pages.  protokv_attend leaves this part to its
+ * caller; each call below can join its result with a readout's (o, lse).
+ *
+ * These calls take no handle and keep nothing between calls; they may run on
+ * several streams and threads at once as long as what they write (outputs,
+ * pages, workspace) is not shared.  They enqueue kernels only (no copies, no
+ * memsets, no allocation), so they can be captured into HIP graphs: sizes and
+ * addresses are frozen, what the device arrays hold is read at every replay.
+ * Their messages are protokv_last_error(NULL)'s, per calling thread.
+ *
+ * Rows of q, k and v are tokens: row t of x starts at x + t * x_stride
+ * elements, head h at h * head_dim in it, so the three may be parts of one
+ * projection's output.  Strides are multiples of 16 bytes, at least the heads'
+ * size; pointers to rows and pages are aligned to 16 bytes, other arrays to 4.
+ * Outputs without a stride are contiguous.  kv_dtype is the type of q, k, v,
+ * pages and o; head_dim is 128; num_q_heads is a multiple of num_kv_heads, at
+ * most 256 times; query head h reads kv head h / (Hq / Hkv).
+ *
+ * cu (device int32 [n + 1], non-decreasing from 0) gives the rows of packed
+ * sequences: those of sequence i are cu[i] .. cu[i+1] - 1.  Entries are taken
+ * within [0, total]; output rows behind cu[n] are left as they were.
+ * --------------------------------------------------------------------------- */
+
+/* A cache of exact keys and values in pages of page_size tokens.  Slot s is
+ * row s % page_size of page s / page_size. */
+typedef struct {
+  void* k;              /* device, kv_dtype [num_pages][num_kv_heads][page_size][D] */
+  void* v;              /* likewise */
+  int32_t num_pages;    /* num_pages * page_size < 2^31 */
+  int32_t page_size;    /* a power of two, 1..1024 */
+} protokv_pages;
+
+typedef struct {
+  int32_t num_requests;   /* n, 1..8192 */
+  int32_t num_pages, page_size;  /* as in protokv_pages, num_pages at most 2^29 */
+  int32_t table_stride;   /* entries of a row of the block table */
+  int32_t max_tokens;     /* entries of slots and positions, 1..2^29 */
+  const int32_t* ctx;     /* device [n]: tokens held (taken within [0, table_stride * page_size]) */
+  const int32_t* add;     /* device [n]: new tokens, or < 0: the request is over */
+  const int32_t* base;    /* device [n] or NULL: position of the request's token 0 (NULL: 0) */
+  int32_t* table;         /* device [n][table_stride], in and out: page of tokens j * page_size .. */
+  int32_t* free_pages;    /* device [num_pages], in and out: a stack of free pages */
+  const int32_t* free_count;  /* device [1]: pages on the stack (taken within [0, num_pages]) */
+  int32_t* free_count_out;    /* device [1]: after the call; not free_count itself */
+  int32_t* cu;            /* device [n + 1] out: first row of each request's new tokens */
+  int32_t* kv_len;        /* device [n] out: ctx + add, 0 if refused or over */
+  int32_t* slots;         /* device [max_tokens] out: slot of each new token, -1: none */
+  int32_t* positions;     /* device [max_tokens] out or NULL: base + ctx + index */
+  int32_t* refused;       /* device [1] out or NULL: requests with new tokens that were refused */
+} protokv_page_plan_args;
+
+/* Block tables and slot maps of one step, from the requests' lengths.
+ * First the pages of requests that are over (add < 0; ceil(ctx / page_size) of
+ * them) go onto the stack in request order; then every request with new
+ * tokens takes the ceil((ctx + add) / page_size) - ceil(ctx / page_size) pages
+ * that it lacks from its top, in request order, and they are entered in its
+ * table row behind those it holds.  Rows of requests that are over, and
+ * entries behind a request's last page, are left as they were.
+ * A request is refused if its tokens do not fit its table row, if they end
+ * behind max_tokens, or if it needs pages and those of the requests up to and
+ * including it (refused for want of pages or not) are more than the stack
+ * holds: then it takes no page, its slots are -1 and its kv_len is 0, so that
+ * protokv_rotate stores nothing for it and protokv_page_attend lets its rows
+ * see no key.  Its rows still count in cu.
+ * cu is the running sum of max(add, 0), at most max_tokens.  slots and
+ * positions are written whole: entries behind cu[n] are -1 and 0.
+ * A slot whose page is outside [0, num_pages) is -1 as well. */
+protokv_status protokv_page_plan(const protokv_page_plan_args* a, void* stream);
+
+typedef struct {
+  int32_t num_tokens;     /* N, >= 0 */
+  int32_t num_q_heads, num_kv_heads, head_dim, kv_dtype;
+  int32_t num_axes;       /* 1..8 */
+  const int32_t* positions;  /* device: axis a of token t at positions[a * position_stride + t] */
+  int64_t position_stride;   /* 0: every axis reads the same N positions */
+  const uint8_t* axes;    /* host [D / 2]: axis of each pair */
+  double theta;           /* rotary base, > 1 */
+  const void* q;          /* device rows of num_q_heads heads, or NULL */
+  const void* k;          /* device rows of num_kv_heads heads, or NULL */
+  const void* v;          /* device rows of num_kv_heads heads: stored with k, NULL without pages */
+  int64_t q_stride, k_stride, v_stride;
+  void* q_out;            /* rows at q_out_stride; may be q itself with the same stride */
+  void* k_out;            /* rows at k_out_stride, may be k likewise; NULL if only stored */
+  int64_t q_out_stride, k_out_stride;
+  const protokv_pages* pages;  /* NULL: nothing is stored */
+  const int32_t* slots;   /* device [N]: slot of each token; outside the pages: not stored */
+} protokv_rotate_args;
+
+/* Rotary positions of several axes (time, height and width of a video's
+ * tokens; one axis for text): pair i of every head of q and k, dims i and
+ * i + D / 2, turns by positions[axes[i]] * theta^(-2 i / D), the angle in
+ * float64, the rotation in float32, rounded once.  (With one axis this is the
+ * rotation of rope_theta.)  With pages, k's rotated rows and v's rows as they
+ * are also go to their slots.  The slots of one call that name a place in the
+ * pages are distinct (of two rows with one slot, parts of either may stay). */
+protokv_status protokv_rotate(const protokv_rotate_args* a, void* stream);
+
+typedef struct {
+  int32_t num_q_heads, num_kv_heads, head_dim, kv_dtype;
+  int32_t num_seqs;       /* n, 0..2^24 - 1 */
+  int32_t total;          /* rows of q, k, v and o; total * Hq < 2^31 */
+  const int32_t* cu;      /* device [n + 1] */
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  void* o;                /* [total][num_q_heads][D] */
+  float* lse;             /* [total][num_q_heads] (natural log) or NULL */
+  const void* prior_o;    /* [total][num_q_heads][D] or NULL */
+  const float* prior_lse; /* [total][num_q_heads]; NULL exactly if prior_o is */
+} protokv_prompt_args;
+
+/* Causal attention of packed sequences over themselves: row t of a sequence
+ * sees rows 0..t of it,
+ *   o = softmax(q K^T / sqrt(D)) V,  lse = log sum exp(q K^T / sqrt(D)).
+ * With a prior (another attention's result for the same rows over other keys,
+ * such as a layer of protokv_attend's) o and lse are those over both:
+ * lse = log(e^own + e^prior), o weighted by e^(own - lse) and e^(prior - lse);
+ * a prior_lse of -inf leaves prior_o unread.  o and lse may be the prior's
+ * own arrays. */
+protokv_status protokv_prompt_attend(const protokv_prompt_args* a, void* stream);
+
+typedef struct {
+  int32_t num_q_heads, num_kv_heads, head_dim, kv_dtype;
+  int32_t num_requests;   /* n, 0..2^24 - 1 */
+  int32_t total;          /* rows of q and o; total * Hq < 2^31 */
+  int32_t max_add;        /* no request has more rows (rows beyond are left as they were), >= 1 */
+  int32_t table_stride;
+  const int32_t* cu;      /* device [n + 1] */
+  const int32_t* kv_len;  /* device [n]: tokens in the pages, the new ones among them */
+  const int32_t* table;   /* device [n][table_stride] */
+  const void* q;
+  int64_t q_stride;
+  protokv_pages pages;
+  void* o;                /* [total][num_q_heads][D] */
+  float* lse;             /* [total][num_q_heads] or NULL */
+  const void* prior_o;
+  const float* prior_lse;
+  void* workspace;        /* device, protokv_page_attend_workspace bytes, 256-byte aligned */
+  size_t workspace_bytes;
+} protokv_page_attend_args;
+
+/* Attention of new tokens over a paged cache: row j of request i, of add_i
+ * rows, sits at position p = kv_len_i - add_i + j and sees tokens 0..p of its
+ * request (their rows are in the pages already).  A row with p < 0 sees
+ * nothing: o = 0 and lse = -inf, or the prior alone.  kv_len is taken within
+ * [0, table_stride * page_size]; a page outside [0, num_pages) holds no
+ * tokens.  What masked places, and places behind kv_len, hold does not matter.
+ * o, lse and the prior as in protokv_prompt_attend.
+ * The workspace holds partial results between the call's kernels; nothing in
+ * it outlives the call, so calls in order on one stream may share it, calls
+ * that can overlap may not (two graphs that replay at once among them). */
+protokv_status protokv_page_attend(const protokv_page_attend_args* a, void* stream);
+
+/* Bytes of workspace for these sizes (device arrays, workspace and row
+ * pointers of `a` are not looked at; 0: none is needed).  Host only. */
+protokv_status protokv_page_attend_workspace(const protokv_page_attend_args* a, size_t* bytes);
+
+/* Message for the last failure on h (or, when h is NULL, of protokv_init and
+ * of the calls that take no handle, on this thread).
  * Valid until the next call on h. */
 const char* protokv_last_error(protokv_t h);
 

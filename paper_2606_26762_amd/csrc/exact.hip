@@ -1,0 +1,684 @@
+// Exact attention of libprotokv for gfx950: packed prompts over themselves and
+// new tokens over a paged cache, causal, grouped heads, joined with a prior.
+//
+//   o_r = sum_{key <= p_r} e^(s_rk) v_k / sum e^(s_rk),  s_rk = q_r . k_k / sqrt(D)
+//
+// in one pass over the keys with a running reference m and sum l per row:
+// O <- O 2^(m - m') + sum 2^(s log2 e - m') v.  Query rows of a kv head are
+// packed: row r of a sequence is token r / grp, query head kvh * grp + r % grp,
+// so every key tile serves all heads of the group.
+#include <algorithm>
+
+#include "exact.h"
+#include "pkv_internal.h"
+
+namespace pkv {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef short v8i16 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+typedef __attribute__((address_space(1))) const f32x4 gbl_f32x4;
+
+namespace {
+
+constexpr float EX_LOG2E = 1.4426950408889634f;
+constexpr float EX_LN2 = 0.6931471805599453f;
+constexpr float EX_SCALE = EX_LOG2E * 0.08838834764831845f;  // log2 e / sqrt(D)
+// Reference of a row that has seen no key: below every finite score, and
+// 2^(-inf - EX_NONE) is 0, not NaN.
+constexpr float EX_NONE = -3.402823466e38f;
+
+// A row block: `rows` rows of sequence `seq`, this block's first one `row0`.
+struct Item {
+  int seq, s0;   // first token row of the sequence in q
+  int add, rows; // its tokens; its query rows of one kv head
+  int row0;
+  int off;       // position of its first token
+  int kend;      // keys that the block's last row sees
+};
+
+// Row-block index b of R rows: sequence i has the indices from
+// f(i) = floor(cu[i] grp / R) + i, non-decreasing, so it is found by comparing 64
+// entries at a time; indices behind a sequence's rows are left empty.  Every
+// lane of the wave takes part; false (uniform) if the block is empty.
+template <int R>
+__device__ __forceinline__ bool find_item(const ExactArgs& a, int b, Item& it) {
+  const int lane = threadIdx.x & 63;
+  auto entry = [&](int i) { return min(max(a.cu[i], 0), a.total); };
+  auto first = [&](int c, int i) { return (int)((unsigned)(c * a.grp) / R) + i; };
+  int lo = 0, hi = a.n;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const bool in = i < hi && first(entry(min(i, a.n)), i) <= b;
+    lo += (max(__popcll(__ballot(in)), 1) - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  const int c0 = __builtin_amdgcn_readfirstlane(entry(lo)), c1 = __builtin_amdgcn_readfirstlane(entry(lo + 1));
+  const int blk = b - first(c0, lo);
+  it.seq = lo;
+  it.s0 = c0;
+  it.add = c1 - c0;
+  if (it.add <= 0 || blk < 0) return false;
+  it.rows = min(it.add, a.max_add) * a.grp;
+  if (blk >= (it.rows + R - 1) / R) return false;
+  it.row0 = blk * R;
+  int kv = it.add;
+  it.off = 0;
+  if (a.kv_len) {
+    kv = min(max(__builtin_amdgcn_readfirstlane(a.kv_len[lo]), 0), a.stride << a.shift);
+    it.off = kv - it.add;
+  }
+  const int last = (min(it.rows, it.row0 + R) - 1) / a.grp;
+  it.kend = min(max(it.off + last + 1, 0), kv);
+  return true;
+}
+
+// Context splits of a block with `tiles` key tiles, and tiles of each.
+__device__ __forceinline__ int splits_of(const ExactArgs& a, int tiles, int& per) {
+  const int want = min(a.splits, max(1, tiles / EX_MIN_TILES));
+  per = max(1, (tiles + want - 1) / want);
+  return max(1, (tiles + per - 1) / per);
+}
+
+// Weights of a row's own result (log2 of its sum: own2) and of the prior's, and
+// the log-sum-exp of both.
+struct Join {
+  float own, prior, lse;
+};
+__device__ __forceinline__ Join join_of(float own2, const float* pl, size_t row) {
+  const float own = own2 * EX_LN2;
+  if (!pl) return {1.f, 0.f, own};
+  const float p = pl[row];
+  if (p == -INFINITY) return {1.f, 0.f, own};
+  if (own == -INFINITY) return {0.f, 1.f, p};
+  const float m = fmaxf(own, p);
+  const float e1 = expf(own - m), e2 = expf(p - m), s = e1 + e2;
+  return {e1 / s, e2 / s, m + logf(s)};
+}
+
+// Four dims from dim d on of output row `row`: own value x (normalised) joined.
+template <int FP32>
+__device__ __forceinline__ void store4(const ExactArgs& a, size_t row, int d, f32x4 x, const Join& j) {
+  const size_t e = row * D + d;
+  if (a.pl && j.prior != 0.f) {  // an unread prior may hold anything
+    f32x4 p;
+    if constexpr (FP32) {
+      p = *reinterpret_cast<const f32x4*>((const float*)a.po + e);
+    } else {
+      const bf16x4 b = *reinterpret_cast<const bf16x4*>((const __bf16*)a.po + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = (float)b[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = j.own == 0.f ? p[i] * j.prior : fmaf(p[i], j.prior, x[i] * j.own);
+  }
+  if constexpr (FP32) {
+    *reinterpret_cast<f32x4*>((float*)a.o + e) = x;
+  } else {
+    bf16x4 b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = (__bf16)x[i];
+    *reinterpret_cast<bf16x4*>((__bf16*)a.o + e) = b;
+  }
+}
+
+// Barrier for LDS traffic only: outstanding global loads are not waited for.
+__device__ __forceinline__ void ex_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  asm volatile("s_barrier" ::: "memory");
+}
+
+constexpr int EX_KEYS = 64;             // keys per tile
+constexpr int EX_TILE = EX_KEYS * D * 2;  // one K or V tile, 16 KB
+constexpr int EX_NBUF = 4;              // tile t computes while t + 1 .. t + 3 load
+constexpr int EX_IDS = 2048;            // page ids staged at a time
+
+// Workgroup = eight waves of 32 query rows each.  A tile of 64 keys sits in LDS
+// in two layouts under which every operand read is a per-lane base plus
+// compile-time offsets on distinct banks:
+//   K chunk-major: 16-byte chunk c (dims 8 c .. + 7) of row r at c * 1024 + r * 16;
+//   V by 32-dim block: dims 32 b .. + 31 of row r at b * 4096 + r * 64.
+// Tiles go straight from global memory into them (global_load_lds_dwordx4),
+// three tiles ahead.  S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x16_bf16,
+// V^T through ds_read_b64_tr_b16: each lane holds one query column, so the
+// softmax is lane-local plus one exchange with the partner lane.
+template <int PAGED>
+__global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t s_kv[EX_NBUF][2][EX_TILE];
+  __shared__ int32_t s_ids[PAGED ? EX_IDS : 1];
+  __shared__ unsigned long long s_bad[8];  // keys of a tile on pages that are none
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // kv heads innermost: workgroups are dealt round robin to the 8 XCDs, so a
+  // head's keys meet in few L2s; the last row blocks, which see the most keys, first
+  const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
+  const int split = rest % a.splits, blk = a.blocks - 1 - rest / a.splits;
+  Item it;
+  if (!find_item<EX_ROWS>(a, blk, it)) return;  // uniform in the workgroup
+  int per;
+  const int tiles = (it.kend + EX_KEYS - 1) / EX_KEYS;
+  const int nsp = splits_of(a, tiles, per);
+  if (split >= nsp) return;
+  const int t0 = split * per, t1 = min(tiles, t0 + per);
+
+  const int m = lane & 31, half = lane >> 5;
+  const int rw = it.row0 + wave * 32, r = rw + m;
+  const bool wvalid = rw < it.rows, rvalid = r < it.rows;  // wvalid is uniform
+  const int tok = rvalid ? r / a.grp : 0;
+  const int head = kvh * a.grp + (rvalid ? r - tok * a.grp : 0);
+  const size_t orow = (size_t)(it.s0 + tok) * a.Hq + head;
+  const int klim = rvalid ? it.off + tok : -1;  // last key that this lane's row sees
+  const int wtok0 = wvalid ? rw / a.grp : 0, wtok1 = wvalid ? (min(it.rows, rw + 32) - 1) / a.grp : 0;
+  const int wfull = it.off + wtok0 + 1;  // keys that every row of the wave sees
+  const int wend = it.off + wtok1 + 1;   // keys that some row of it sees
+
+  bf16x8 bq[8];
+  {
+    const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(it.s0 + tok) * a.qs + head * (D * 2));
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[2 * kk + half]);
+  }
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  f32x16 oacc[4] = {zero, zero, zero, zero};
+  // l1: sum of the weights as rounded for the PV product (normalises o: a row with
+  // one key returns its value exactly); l2: of the unrounded ones (for lse)
+  float mref = EX_NONE, l1 = 0.f, l2 = 0.f;
+
+  const uint8_t* kb = (const uint8_t*)a.k + (PAGED ? 0 : (size_t)it.s0 * a.ks + kvh * (D * 2));
+  const uint8_t* vb = (const uint8_t*)a.v + (PAGED ? 0 : (size_t)it.s0 * a.vs + kvh * (D * 2));
+  const int tpc = PAGED ? (EX_IDS << a.shift) / EX_KEYS : 1;  // tiles per staged run of page ids
+  auto load_ids = [&](int t) {  // the run that tile t is in
+    const int e0 = (t / tpc) * EX_IDS, n = min(EX_IDS, ((it.kend - 1) >> a.shift) + 1 - e0);
+    const int32_t* row = a.table + (size_t)it.seq * a.stride + e0;
+    for (int i = tid; i < n; i += 512) s_ids[i] = row[i];
+  };
+  // byte offset of key's row; bad: its page is none (page 0 is read instead)
+  auto paged_row = [&](int key, bool& bad) {
+    const int id = s_ids[(key >> a.shift) & (EX_IDS - 1)];
+    bad = (unsigned)id >= (unsigned)a.num_pages;
+    const size_t page = bad ? 0 : id;
+    return ((((page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1)))) * (size_t)(D * 2);
+  };
+  auto issue = [&](int t) {
+    const int buf = t % EX_NBUF;
+    // keys past the last one repeat it (they are masked)
+    const int key_k = min(t * EX_KEYS + lane, it.kend - 1);
+    const int key_v = min(t * EX_KEYS + (wave & 3) * 16 + (lane >> 2), it.kend - 1);
+    const uint8_t *rk, *rv;
+    if constexpr (PAGED) {
+      bool bad, bad2;
+      rk = kb + paged_row(key_k, bad);
+      rv = vb + paged_row(key_v, bad2);
+      const unsigned long long bm = __ballot(bad);
+      if (wave == 0 && lane == 0) s_bad[t & 7] = bm;
+    } else {
+      rk = kb + (size_t)key_k * a.ks;
+      rv = vb + (size_t)key_v * a.vs;
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int i = wave + 8 * q;  // chunk of K; 32-dim block i / 4 of V, rows 16 (i % 4) .. + 15
+      lds_dma16(rk + i * 16, s_kv[buf][0] + i * 1024);
+      lds_dma16(rv + (i >> 2) * 64 + (lane & 3) * 16, s_kv[buf][1] + i * 1024);
+    }
+  };
+  const int grp16 = lane >> 4, s16 = lane & 15;
+  const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
+  auto compute_tile = [&](int t, auto masked) {
+    constexpr bool MASK = decltype(masked)::value;
+    const uint8_t* kl = s_kv[t % EX_NBUF][0] + m * 16 + half * 1024;
+    const uint8_t* vl = s_kv[t % EX_NBUF][1] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
+    f32x16 s[2] = {zero, zero};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {
+        const bf16x8 ak = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u16x8*>(kl + kk * 2048 + h * 512));
+        s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak, bq[kk], s[h], 0, 0, 0);
+      }
+    unsigned long long bad = 0;
+    const int rel = klim - t * EX_KEYS - 4 * half;
+    if constexpr (MASK) {
+      if constexpr (PAGED) bad = s_bad[t & 7] >> (4 * half);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int c = 32 * h + 8 * (i >> 2) + (i & 3);  // key c + 4 half of the tile
+          const bool hidden = c > rel || (PAGED && ((bad >> c) & 1));
+          s[h][i] = hidden ? -INFINITY : s[h][i];
+        }
+    }
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, s[h][i]);
+    tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
+    // the reference moves up only when a row's maximum exceeds it by more than 8
+    // (weights up to 2^8 keep bf16's relative precision)
+    const bool grow = tmax > mref + 8.0f;
+    if (__ballot(grow)) {  // uniform
+      const float mnew = grow ? tmax : mref;
+      const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
+      l1 *= alpha;
+      l2 *= alpha;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
+      mref = mnew;
+    }
+    bf16x8 pb[4];
+    float part[2] = {0.f, 0.f}, sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[h][i], EX_SCALE, -mref));
+        part[i & 1] += p;
+        pb[2 * h + (i >> 3)][i & 7] = (__bf16)p;
+      }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sum0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 0, 1), ones2, sum0, false);
+      sum1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 2, 3), ones2, sum1, false);
+      sum0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 4, 5), ones2, sum0, false);
+      sum1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 6, 7), ones2, sum1, false);
+    }
+    l1 += sum0 + sum1;   // this half's keys; the halves meet at the end
+    l2 += part[0] + part[1];
+    // V^T operand of 32-dim block b, 16-key step st: positions half * 8 + i are
+    // keys 16 st + 4 half + {0..3} (i < 4) and + 8 (i >= 4), as P's registers are
+    auto read_v = [&](int b, int st) {
+      const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + b * 4096 + st * 1024));
+      const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + b * 4096 + st * 1024 + 512));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    if constexpr (MASK) {
+      // A masked key has weight 0, but 0 x inf and 0 x NaN are not 0.  If the tile
+      // holds such a value, the products are formed for one token's rows at a time,
+      // with the keys that it does not see set to 0.
+      bool odd = false;
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+          const v8i16 v = read_v(b, st);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) odd |= (v[i] & 0x7F80) == 0x7F80;
+        }
+      if (__ballot(odd)) {  // uniform
+        for (int tk = wtok0; tk <= wtok1; ++tk) {  // uniform
+          const int lim = it.off + tk - t * EX_KEYS - 4 * half;
+          const bool mine = rvalid && tok == tk;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            f32x16 acc = zero;
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+              v8i16 v = read_v(b, st);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int c = 16 * st + 8 * (i >> 2) + (i & 3);
+                if (c > lim || (PAGED && ((bad >> c) & 1))) v[i] = 0;
+              }
+              acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pb[st], acc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[b][i] = mine ? oacc[b][i] + acc[i] : oacc[b][i];
+          }
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+        oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, read_v(b, st)), pb[st], oacc[b], 0, 0, 0);
+  };
+
+  if constexpr (PAGED) {
+    if (t0 < t1) load_ids(t0);
+  }
+  wait_vm<0>();  // the query operands are in registers before any tile is in flight
+  ex_barrier();
+  for (int t = t0; t < t0 + 3 && t < t1; ++t) {
+    if constexpr (PAGED) {
+      if (t > t0 && t % tpc == 0) {  // uniform
+        ex_barrier();
+        load_ids(t);
+        ex_barrier();
+      }
+    }
+    issue(t);
+  }
+  for (int t = t0; t < t1; ++t) {
+    // this wave's loads of tile t have landed; those of t + 1, t + 2 may be in flight
+    if (t + 2 < t1) wait_vm<8>();
+    else if (t + 1 < t1) wait_vm<4>();
+    else wait_vm<0>();
+    ex_barrier();
+    // buffer (t + 3) % 4 held tile t - 1, finished by every wave before this barrier
+    if (t + 3 < t1) {
+      if constexpr (PAGED) {
+        if ((t + 3) % tpc == 0) {  // uniform
+          load_ids(t + 3);
+          ex_barrier();
+        }
+      }
+      issue(t + 3);
+    }
+    if (!wvalid || t * EX_KEYS >= wend) continue;  // uniform: nothing of the tile is seen
+    bool mask = (t + 1) * EX_KEYS > wfull;
+    if constexpr (PAGED) mask |= __builtin_amdgcn_readfirstlane((int)(s_bad[t & 7] != 0));
+    if (mask) compute_tile(t, std::true_type{});
+    else compute_tile(t, std::false_type{});
+  }
+  if (!wvalid) return;
+  l1 += xor32(l1);
+  l2 += xor32(l2);
+  if (nsp > 1) {
+    const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * EX_ROWS + wave * 32 + m;
+    if (rvalid) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4*>(a.part_o + pr * D + b * 32 + i * 8 + half * 4) =
+              (f32x4){oacc[b][4 * i], oacc[b][4 * i + 1], oacc[b][4 * i + 2], oacc[b][4 * i + 3]};
+      if (half == 0) {
+        a.part_ml[pr * 3] = mref;
+        a.part_ml[pr * 3 + 1] = l1;
+        a.part_ml[pr * 3 + 2] = l2;
+      }
+    }
+    return;
+  }
+  if (!rvalid) return;
+  const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;  // no key: 0; a NaN stays one
+  const Join j = join_of(l2 == 0.f ? -INFINITY : mref + log2f(l2), a.pl, orow);
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      store4<0>(a, orow, b * 32 + i * 8 + half * 4,
+                (f32x4){oacc[b][4 * i] * inv, oacc[b][4 * i + 1] * inv, oacc[b][4 * i + 2] * inv, oacc[b][4 * i + 3] * inv}, j);
+  if (half == 0 && a.lse) a.lse[orow] = j.lse;
+}
+
+// float32: S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x2_f32.  One wave =
+// one work item (kv head, 32 query rows, context split), 32 keys per tile, four
+// independent waves per workgroup.  K and V go from global memory into the
+// operand registers; the query sits in LDS (each lane reads back what it wrote).
+//   K: lane (m = lane % 32, h = lane / 32) loads dims 8 j + 4 h .. + 3 of key m.
+//   P: register i of S^T holds key 8 (i / 4) + 4 h + i % 4 of query lane % 32.
+//   V: lane (m, h) loads dims 4 m .. 4 m + 3 of register i's key of its half; row
+//      m of accumulator b is dim 4 m + b.
+// A dot product is the sum of eight 16-dim chains: its rounding error is that of
+// a pairwise sum.
+constexpr int EX_KEYS32 = 32;
+
+template <int PAGED>
+__global__ __launch_bounds__(256, 2) void k_exact_f32(ExactArgs a) {
+  __shared__ f32x4 s_q[4][16][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const long long item = (long long)blockIdx.x * 4 + wave;
+  if (item >= (long long)a.Hkv * a.blocks * a.splits) return;  // uniform, and nothing below synchronises waves
+  const int kvh = (int)(item % a.Hkv), rest = (int)(item / a.Hkv);
+  const int split = rest % a.splits, blk = a.blocks - 1 - rest / a.splits;
+  Item it;
+  if (!find_item<EX_ROWS_F32>(a, blk, it)) return;
+  int per;
+  const int tiles = (it.kend + EX_KEYS32 - 1) / EX_KEYS32;
+  const int nsp = splits_of(a, tiles, per);
+  if (split >= nsp) return;
+  const int t0 = split * per, t1 = min(tiles, t0 + per);
+  const int m = lane & 31, half = lane >> 5;
+  const int r = it.row0 + m;
+  const bool rvalid = r < it.rows;
+  const int tok = rvalid ? r / a.grp : 0;
+  const int head = kvh * a.grp + (rvalid ? r - tok * a.grp : 0);
+  const size_t orow = (size_t)(it.s0 + tok) * a.Hq + head;
+  const int klim = rvalid ? it.off + tok : -1;
+  const int wtok0 = it.row0 / a.grp, wtok1 = (min(it.rows, it.row0 + 32) - 1) / a.grp;
+  const int wfull = it.off + wtok0 + 1;
+  {
+    const f32x4* qr = reinterpret_cast<const f32x4*>((const uint8_t*)a.q + (size_t)(it.s0 + tok) * a.qs) + head * (D / 4);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s_q[wave][j][lane] = qr[2 * j + half];
+  }
+  const uint8_t* kb = (const uint8_t*)a.k + (PAGED ? 0 : (size_t)it.s0 * a.ks + kvh * (D * 4));
+  const uint8_t* vb = (const uint8_t*)a.v + (PAGED ? 0 : (size_t)it.s0 * a.vs + kvh * (D * 4));
+  // K and V rows of this lane's key of tile t (keys past the last repeat it)
+  auto resolve = [&](int t, const float*& kp, const float*& vp, bool& bad) {
+    const int key = min(t * EX_KEYS32 + m, it.kend - 1);
+    bad = false;
+    if constexpr (PAGED) {
+      const int id = a.table[(size_t)it.seq * a.stride + (key >> a.shift)];
+      bad = (unsigned)id >= (unsigned)a.num_pages;
+      const size_t page = bad ? 0 : id;
+      const size_t e = ((((page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1)))) * (size_t)D;
+      kp = (const float*)kb + e;
+      vp = (const float*)vb + e;
+    } else {
+      kp = reinterpret_cast<const float*>(kb + (size_t)key * a.ks);
+      vp = reinterpret_cast<const float*>(vb + (size_t)key * a.vs);
+    }
+  };
+  // half h of a tile: dims 64 h .. 64 h + 63 of K; registers 8 h .. 8 h + 7 of V
+  auto load_k = [&](const float* kp, int h, f32x4 (&kr)[8]) {
+    gbl_f32x4* p = (gbl_f32x4*)(uintptr_t)kp + half + 16 * h;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) kr[j] = p[2 * j];
+  };
+  auto of_key = [&](int x, int i) {  // register i's key's value of x
+    return __builtin_amdgcn_ds_bpermute(16 * half + 4 * (8 * (i >> 2) + (i & 3)), x);
+  };
+  auto load_v = [&](const float* vp, int h, f32x4 (&vr)[8]) {
+    const uint64_t p = reinterpret_cast<uint64_t>(vp);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t lo = of_key((int)(uint32_t)p, 8 * h + i), hi = of_key((int)(uint32_t)(p >> 32), 8 * h + i);
+      vr[i] = ((gbl_f32x4*)(uintptr_t)((uint64_t)hi << 32 | lo))[m];
+    }
+  };
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  f32x16 oacc[4] = {zero, zero, zero, zero};
+  float mrun = EX_NONE, lrun = 0.f;
+  // four chains over the dims of half h
+  auto dots = [&](const f32x4 (&kr)[8], int h) {
+    f32x16 s = zero;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      f32x16 c = zero;
+#pragma unroll
+      for (int j = 2 * g; j < 2 * g + 2; ++j) {
+        const f32x4 qv = s_q[wave][8 * h + j][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(kr[j][e], qv[e], c, 0, 0, 0);
+      }
+      s = g ? s + c : c;
+      asm("" : "+v"(s));  // summed here, not after every chain is done
+    }
+    return s;
+  };
+  auto weigh = [&](const f32x4 (&vr)[8], const f32x16& p, int h, f32x16 (&o)[4]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[i][b], p[8 * h + i], o[b], 0, 0, 0);
+  };
+  f32x4 k0[8], k1[8], v0[8], v1[8];
+  const float *kp = nullptr, *vp = nullptr;
+  bool bad = false;
+  if (t0 < t1) {
+    resolve(t0, kp, vp, bad);
+    load_k(kp, 0, k0);
+    load_k(kp, 1, k1);
+  }
+  for (int t = t0; t < t1; ++t) {
+    load_v(vp, 0, v0);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16 s = dots(k0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(vp, 1, v1);
+    __builtin_amdgcn_sched_barrier(0);
+    s = s + dots(k1, 1);
+    const unsigned badm = PAGED ? (unsigned)__ballot(bad) >> (4 * half) : 0u;  // lanes 0 .. 31: the tile's keys
+    const bool masked = (t + 1) * EX_KEYS32 > wfull || (PAGED && __ballot(bad) != 0);  // uniform
+    const int rel = klim - t * EX_KEYS32 - 4 * half;
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int c = 8 * (i >> 2) + (i & 3);
+        s[i] = c > rel || ((badm >> c) & 1) ? -INFINITY : s[i];
+      }
+    }
+    // the next tile's keys load while this tile's values are used (past the
+    // last tile the loads repeat it)
+    resolve(min(t + 1, t1 - 1), kp, vp, bad);
+    load_k(kp, 0, k0);
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, s[i]);
+    tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
+    const float mnew = fmaxf(mrun, tmax);
+    if (__ballot(!(mnew <= mrun))) {  // uniform
+      const float alpha = __builtin_amdgcn_exp2f(mrun - mnew);
+      lrun *= alpha;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
+      mrun = mnew;
+    }
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], EX_SCALE, -mrun));
+      part[i & 3] += s[i];
+    }
+    lrun += (part[0] + part[1]) + (part[2] + part[3]);
+    bool odd = false;
+    if (masked) {  // 0 x inf is not 0: as in the bf16 kernel
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          odd |= (__float_as_uint(v0[i][b]) & 0x7F800000u) == 0x7F800000u ||
+                 (__float_as_uint(v1[i][b]) & 0x7F800000u) == 0x7F800000u;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (__ballot(odd)) {  // uniform
+      for (int tk = wtok0; tk <= wtok1; ++tk) {  // uniform
+        const int lim = it.off + tk - t * EX_KEYS32 - 4 * half;
+        const bool mine = rvalid && tok == tk;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          f32x16 acc = zero;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int c = 8 * (i >> 2) + (i & 3);
+            const bool hide = c > lim || ((badm >> c) & 1);
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(hide ? 0.f : (i < 8 ? v0 : v1)[i & 7][b], s[i], acc, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[b][i] = mine ? oacc[b][i] + acc[i] : oacc[b][i];
+        }
+      }
+      load_k(kp, 1, k1);
+      continue;
+    }
+    weigh(v0, s, 0, oacc);
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(kp, 1, k1);
+    __builtin_amdgcn_sched_barrier(0);
+    weigh(v1, s, 1, oacc);
+  }
+  lrun += xor32(lrun);
+  if (!rvalid) return;
+  // register i of oacc[0..3]: dims 4 mm .. 4 mm + 3 with mm = 8 (i / 4) + 4 half + i % 4
+  if (nsp > 1) {
+    const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * EX_ROWS_F32 + m;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      reinterpret_cast<f32x4*>(a.part_o + pr * D)[8 * (i >> 2) + 4 * half + (i & 3)] =
+          (f32x4){oacc[0][i], oacc[1][i], oacc[2][i], oacc[3][i]};
+    if (half == 0) {
+      a.part_ml[pr * 3] = mrun;
+      a.part_ml[pr * 3 + 1] = lrun;
+      a.part_ml[pr * 3 + 2] = lrun;
+    }
+    return;
+  }
+  const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;
+  const Join j = join_of(lrun == 0.f ? -INFINITY : mrun + log2f(lrun), a.pl, orow);
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    store4<1>(a, orow, 4 * (8 * (i >> 2) + 4 * half + (i & 3)),
+              (f32x4){oacc[0][i] * inv, oacc[1][i] * inv, oacc[2][i] * inv, oacc[3][i] * inv}, j);
+  if (half == 0 && a.lse) a.lse[orow] = j.lse;
+}
+
+// Joins the splits of a row block: O = sum_s w_s O_s / sum_s w_s l_s with
+// w_s = 2^(m_s - max m).  Workgroup = 32 rows of one (kv head, row block), 32
+// threads per row, four dims each.
+template <int FP32, int R>
+__global__ __launch_bounds__(256) void k_exact_join(ExactArgs a) {
+  const int part = blockIdx.x % (R / 32), rest = blockIdx.x / (R / 32);
+  const int kvh = rest % a.Hkv, blk = rest / a.Hkv;
+  Item it;
+  if (!find_item<R>(a, blk, it)) return;
+  int per;
+  const int tiles = (it.kend + (FP32 ? EX_KEYS32 : EX_KEYS) - 1) / (FP32 ? EX_KEYS32 : EX_KEYS);
+  const int nsp = splits_of(a, tiles, per);
+  if (nsp == 1) return;  // written by the attention itself
+  const size_t base = ((size_t)kvh * a.blocks + blk) * a.splits;
+  const int d = (threadIdx.x & 31) * 4;
+  for (int i = threadIdx.x >> 5; i < 32; i += 8) {
+    const int lr = part * 32 + i, r = it.row0 + lr;
+    if (r >= it.rows) return;
+    float M = EX_NONE, l1 = 0.f, l2 = 0.f;
+    for (int s = 0; s < nsp; ++s) M = fmaxf(M, a.part_ml[((base + s) * R + lr) * 3]);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < nsp; ++s) {
+      const size_t pr = (base + s) * R + lr;
+      const float w = __builtin_amdgcn_exp2f(a.part_ml[pr * 3] - M);
+      l1 += w * a.part_ml[pr * 3 + 1];
+      l2 += w * a.part_ml[pr * 3 + 2];
+      o += w * *reinterpret_cast<const f32x4*>(a.part_o + pr * D + d);
+    }
+    const int tok = r / a.grp;
+    const size_t orow = (size_t)(it.s0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp);
+    const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
+    const Join j = join_of(l2 == 0.f ? -INFINITY : M + log2f(l2), a.pl, orow);
+    store4<FP32>(a, orow, d, o * inv, j);
+    if (d == 0 && a.lse) a.lse[orow] = j.lse;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t st) {
+  const unsigned items = (unsigned)a.Hkv * a.blocks * a.splits;
+  if (fp32) {
+    if (paged) hipLaunchKernelGGL((k_exact_f32<1>), dim3((items + 3) / 4), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_f32<0>), dim3((items + 3) / 4), dim3(256), 0, st, a);
+  } else {
+    if (paged) hipLaunchKernelGGL((k_exact_bf16<1>), dim3(items), dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_bf16<0>), dim3(items), dim3(512), 0, st, a);
+  }
+  if (a.splits > 1) {
+    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), dim3(a.Hkv * a.blocks), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), dim3(a.Hkv * a.blocks * (EX_ROWS / 32)), dim3(256), 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace pkv

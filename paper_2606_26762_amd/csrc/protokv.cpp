@@ -9,9 +9,14 @@
 #include <string>
 #include <vector>
 
+#include "exact.h"
 #include "pkv_internal.h"
 
 using namespace pkv;
+
+// Message of the last failure without a handle, per thread.
+static thread_local std::string g_init_err;
+std::string& pkv::call_error() { return g_init_err; }
 
 namespace {
 
@@ -32,8 +37,6 @@ struct Layout {
   size_t pk, pv, pbias, pcodes, part_o, part_ml, counters, touched, ring_kr, qrot, rope_inv, reservoir, ema_res;
   size_t ps_count, ps_off, prow_bias, ps_var, total;
 };
-
-thread_local std::string g_init_err;
 
 size_t kv_bytes(const protokv_config& c) { return c.kv_dtype == PROTOKV_KV_FP32 ? 4 : 2; }
 

@@ -29,6 +29,8 @@ EXPORTED = [
     "protokv_read_pseudo", "protokv_read_codebooks", "protokv_profile", "protokv_profile_read",
     "protokv_state_size", "protokv_get_state", "protokv_set_state", "protokv_attend_static",
     "protokv_read_pseudo_counts",
+    "protokv_page_plan", "protokv_rotate", "protokv_prompt_attend", "protokv_page_attend",
+    "protokv_page_attend_workspace",
     "protokv_last_error",
 ]
 
@@ -94,6 +96,49 @@ class KernelTimes(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * 16), ("launches", ctypes.c_uint64 * 16)]
 
 
+class Pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class PagePlanArgs(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("table_stride", ctypes.c_int32), ("max_tokens", ctypes.c_int32)] + [
+        (f, ctypes.c_void_p) for f in ("ctx", "add", "base", "table", "free_pages", "free_count", "free_count_out",
+                                       "cu", "kv_len", "slots", "positions", "refused")]
+
+
+class RotateArgs(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("kv_dtype", ctypes.c_int32), ("num_axes", ctypes.c_int32),
+                ("positions", ctypes.c_void_p), ("position_stride", ctypes.c_int64), ("axes", ctypes.c_char_p),
+                ("theta", ctypes.c_double), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64),
+                ("pages", ctypes.POINTER(Pages)), ("slots", ctypes.c_void_p)]
+
+
+class PromptArgs(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("kv_dtype", ctypes.c_int32), ("num_seqs", ctypes.c_int32), ("total", ctypes.c_int32),
+                ("cu", ctypes.c_void_p), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("o", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("prior_o", ctypes.c_void_p), ("prior_lse", ctypes.c_void_p)]
+
+
+class PageAttendArgs(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("kv_dtype", ctypes.c_int32), ("num_requests", ctypes.c_int32), ("total", ctypes.c_int32),
+                ("max_add", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+                ("cu", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("pages", Pages),
+                ("o", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("prior_o", ctypes.c_void_p), ("prior_lse", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -127,6 +172,11 @@ def lib() -> ctypes.CDLL:
         L.protokv_state_size.argtypes = [vp, P(sz)]
         L.protokv_get_state.argtypes = [vp, i32, vp, sz, vp]
         L.protokv_set_state.argtypes = [vp, i32, vp, sz, vp]
+        L.protokv_page_plan.argtypes = [P(PagePlanArgs), vp]
+        L.protokv_rotate.argtypes = [P(RotateArgs), vp]
+        L.protokv_prompt_attend.argtypes = [P(PromptArgs), vp]
+        L.protokv_page_attend.argtypes = [P(PageAttendArgs), vp]
+        L.protokv_page_attend_workspace.argtypes = [P(PageAttendArgs), P(sz)]
         L.protokv_last_error.argtypes = [vp]
         L.protokv_last_error.restype = ctypes.c_char_p
         for name in EXPORTED:
@@ -414,3 +464,236 @@ class ProtoKV:
             raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
         if t.dtype != self.kv_dtype or not t.is_cuda or not t.is_contiguous():
             raise ValueError(f"expected a contiguous {self.kv_dtype} CUDA tensor")
+
+
+# -- exact attention around the readout (no handle) ---------------------------
+
+
+def _rows(t, name, dtype=None):
+    """-> (pointer, row stride in elements) of token rows [N][heads][D]."""
+    import torch
+    if t.dim() != 3 or t.shape[2] != 128 or not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or (
+            dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name}: expected CUDA rows [N, heads, 128] in {dtype or 'bfloat16 or float32'}")
+    n, heads, _ = t.shape
+    if n > 0 and ((t.stride(2) != 1) or (heads > 1 and t.stride(1) != 128)):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return t.data_ptr(), t.stride(0) if n > 1 else heads * 128
+
+
+def _ints(t, name, *shape):
+    """Pointer of a contiguous int32 CUDA tensor (None stays None)."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected a contiguous int32 CUDA tensor {shape}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, where the call will run."""
+    import torch
+    d = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t is not False and t.device.index != d:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{d}")
+
+
+def _pages(pages, dtype, kv_heads):
+    """Pages of (k, v) [num_pages][kv heads][page size][D]."""
+    k, v = pages
+    if k.dim() != 4 or k.shape != v.shape or k.shape[1] != kv_heads or k.shape[3] != 128:
+        raise ValueError(f"pages: expected k and v [num_pages, {kv_heads}, page_size, 128]")
+    for t in (k, v):
+        if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"pages: expected contiguous {dtype} CUDA tensors")
+    return Pages(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2])
+
+
+def _new(shape, dtype, like, stream):
+    """A tensor for a call on `stream`: allocated there, so that its memory is not
+    reused before that stream's work is done."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if stream.device.index != torch.cuda.current_device():
+        raise ValueError(f"the stream is on {stream.device}, not on the current device")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _result(q, out, lse, prior, stream):
+    """Outputs [N][Hq][D] and [N][Hq] (made where not given; lse=False: none) and the prior's pointers."""
+    import torch
+    n, hq, _ = q.shape
+    if out is None:
+        out = _new((n, hq, 128), q.dtype, q, stream)
+    if lse is None:
+        lse = _new((n, hq), torch.float32, q, stream)
+    po, pl = prior if prior is not None else (None, None)
+    for t, name in ((out, "out"), (po, "prior")):
+        if t is not None and (tuple(t.shape) != (n, hq, 128) or t.dtype != q.dtype or not t.is_contiguous()):
+            raise ValueError(f"{name}: expected a contiguous {q.dtype} tensor {(n, hq, 128)}")
+    for t, name in ((lse, "lse"), (pl, "prior lse")):
+        if t is not None and t is not False and (
+                tuple(t.shape) != (n, hq) or t.dtype != torch.float32 or not t.is_contiguous()):
+            raise ValueError(f"{name}: expected a contiguous float32 tensor {(n, hq)}")
+    _here(q, out, lse, po, pl)
+    return out, lse, po.data_ptr() if po is not None else None, pl.data_ptr() if pl is not None else None
+
+
+def _kv(t):
+    import torch
+    return KV_FP32 if t.dtype == torch.float32 else KV_BF16
+
+
+def pair_axes(sections: Sequence[int], interleaved: bool = False) -> bytes:
+    """Axis of each of the 64 rotary pairs, for ``rotate``: sections[a] pairs turn
+    by axis a, in one run after the other, or (interleaved) dealt out in turn,
+    an axis leaving the round once it has all of its pairs."""
+    left = [int(n) for n in sections]
+    if not 1 <= len(left) <= 8 or min(left) < 0 or sum(left) != 64:
+        raise ValueError("pair_axes: 1 to 8 sections of 64 pairs in all")
+    if not interleaved:
+        return bytes(a for a, n in enumerate(left) for _ in range(n))
+    out = []
+    while len(out) < 64:
+        for a, n in enumerate(left):
+            if n:
+                left[a] = n - 1
+                out.append(a)
+    return bytes(out)
+
+
+def rotate(q, k, positions, axes: bytes, theta: float, *, q_out=None, k_out=None, v=None, pages=None, slots=None,
+           stream=None):
+    """protokv_rotate on token rows q [N][Hq][D] and k [N][Hkv][D] (either may be
+    None; rows may be strided): positions int32 [num_axes][N] (or [N]: every axis
+    the same), axes from ``pair_axes``.  With pages=(k, v) tensors [num_pages][Hkv]
+    [page_size][D] and slots int32 [N] the turned keys and v's rows are stored, and
+    k_out is written only if given.  -> (q_out, k_out)"""
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("rotate: neither q nor k")
+    n, dtype = some.shape[0], some.dtype
+    a = RotateArgs()
+    a.num_tokens, a.head_dim, a.kv_dtype = n, 128, _kv(some)
+    a.num_kv_heads = k.shape[1] if k is not None else 1
+    a.num_q_heads = q.shape[1] if q is not None else a.num_kv_heads
+    if not isinstance(axes, bytes) or len(axes) != 64:
+        raise ValueError("rotate: axes are 64 bytes (pair_axes)")
+    a.num_axes, a.axes, a.theta = max(axes) + 1, axes, theta
+    if positions.dim() == 1:
+        a.positions, a.position_stride = _ints(positions, "positions", n), 0
+    else:
+        if positions.shape[0] < a.num_axes:
+            raise ValueError("rotate: positions has fewer axes than axes names")
+        a.positions, a.position_stride = _ints(positions, "positions", positions.shape[0], n), n
+    if q is not None:
+        a.q, a.q_stride = _rows(q, "q", dtype)
+        if q_out is None:
+            q_out = _new(tuple(q.shape), dtype, q, stream)
+        elif q_out.shape != q.shape:
+            raise ValueError("rotate: q_out must have q's shape")
+        a.q_out, a.q_out_stride = _rows(q_out, "q_out", dtype)
+    if k is not None:
+        if k.shape[0] != n:
+            raise ValueError("rotate: q and k must have the same rows")
+        a.k, a.k_stride = _rows(k, "k", dtype)
+        if k_out is None and pages is None:
+            k_out = _new(tuple(k.shape), dtype, k, stream)
+        if k_out is not None:
+            if k_out.shape != k.shape:
+                raise ValueError("rotate: k_out must have k's shape")
+            a.k_out, a.k_out_stride = _rows(k_out, "k_out", dtype)
+    if pages is not None:
+        if k is None or v is None or slots is None or v.shape != k.shape:
+            raise ValueError("rotate: pages take k, v of its shape, and slots")
+        a.v, a.v_stride = _rows(v, "v", dtype)
+        p = _pages(pages, dtype, k.shape[1])
+        a.pages = ctypes.pointer(p)
+        a.slots = _ints(slots, "slots", n)
+        _here(v, slots, *pages)
+    _here(q, k, positions, q_out, k_out)
+    _check(lib().protokv_rotate(ctypes.byref(a), _stream_ptr(stream)))
+    return q_out, k_out
+
+
+class PagePlan:
+    """What protokv_page_plan returned: cu [n+1], kv_len [n], slots and positions
+    [max_tokens], count [1] (pages left on the stack), refused [1]."""
+    __slots__ = ("cu", "kv_len", "slots", "positions", "count", "refused")
+
+
+def page_plan(ctx, add, table, free_pages, count, page_size: int, max_tokens: int, *, base=None, count_out=None,
+              stream=None) -> PagePlan:
+    """protokv_page_plan: one step's slots, positions and lengths from the requests'
+    held (ctx) and new (add, < 0: over) tokens, int32 [n]; table int32 [n][width] and
+    the stack free_pages [num_pages] are updated in place, count [1] is not
+    (count_out or a new tensor holds the pages left)."""
+    import torch
+    n = ctx.shape[0]
+    out = PagePlan()
+    new = lambda m: _new(m, torch.int32, ctx, stream)  # noqa: E731
+    out.cu, out.kv_len, out.slots, out.positions, out.refused = new(n + 1), new(n), new(max_tokens), new(max_tokens), new(1)
+    out.count = new(1) if count_out is None else count_out
+    _here(ctx, add, table, free_pages, count, base, out.count)
+    a = PagePlanArgs(n, free_pages.shape[0], page_size, table.shape[1], max_tokens, _ints(ctx, "ctx", n),
+                     _ints(add, "add", n), _ints(base, "base", n), _ints(table, "table", n, table.shape[1]),
+                     _ints(free_pages, "free_pages", free_pages.shape[0]), _ints(count, "count", 1),
+                     _ints(out.count, "count_out", 1), out.cu.data_ptr(), out.kv_len.data_ptr(), out.slots.data_ptr(),
+                     out.positions.data_ptr(), out.refused.data_ptr())
+    _check(lib().protokv_page_plan(ctypes.byref(a), _stream_ptr(stream)))
+    return out
+
+
+def prompt_attend(q, k, v, cu, *, out=None, lse=None, prior=None, stream=None):
+    """protokv_prompt_attend on token rows q [N][Hq][D], k, v [N][Hkv][D] (rows may be
+    strided) of the packed sequences cu int32 [n+1]; prior: (o, lse) of the same rows
+    over other keys, joined with the result.  -> (o, lse); lse=False: none."""
+    a = PromptArgs()
+    a.q, a.q_stride = _rows(q, "q")
+    a.k, a.k_stride = _rows(k, "k", q.dtype)
+    a.v, a.v_stride = _rows(v, "v", q.dtype)
+    if k.shape != v.shape or k.shape[0] != q.shape[0]:
+        raise ValueError("prompt_attend: q, k and v must have the same rows, k and v the same heads")
+    a.total, a.num_q_heads, _ = q.shape
+    a.num_kv_heads, a.head_dim, a.kv_dtype = k.shape[1], 128, _kv(q)
+    a.num_seqs = cu.shape[0] - 1
+    a.cu = _ints(cu, "cu", cu.shape[0])
+    out, lse, a.prior_o, a.prior_lse = _result(q, out, lse, prior, stream)
+    a.o, a.lse = out.data_ptr(), lse.data_ptr() if lse is not False else None
+    _here(k, v, cu)
+    _check(lib().protokv_prompt_attend(ctypes.byref(a), _stream_ptr(stream)))
+    return out, lse
+
+
+def page_attend(q, pages, table, cu, kv_len, max_add: int, *, out=None, lse=None, prior=None, workspace=None,
+                stream=None):
+    """protokv_page_attend: rows q [N][Hq][D] of the requests cu int32 [n+1], at most
+    max_add each, over their kv_len [n] tokens in pages=(k, v) [num_pages][Hkv]
+    [page_size][D] by the block table [n][width].  workspace: a uint8 tensor (None: one
+    of this call's own).  -> (o, lse); lse=False: none."""
+    import torch
+    a = PageAttendArgs()
+    a.q, a.q_stride = _rows(q, "q")
+    a.total, a.num_q_heads, _ = q.shape
+    a.num_kv_heads, a.head_dim, a.kv_dtype = pages[0].shape[1], 128, _kv(q)
+    a.pages = _pages(pages, q.dtype, a.num_kv_heads)
+    n = a.num_requests = cu.shape[0] - 1
+    a.max_add, a.table_stride = max_add, table.shape[1]
+    a.cu, a.kv_len = _ints(cu, "cu", n + 1), _ints(kv_len, "kv_len", n)
+    a.table = _ints(table, "table", n, table.shape[1])
+    out, lse, a.prior_o, a.prior_lse = _result(q, out, lse, prior, stream)
+    a.o, a.lse = out.data_ptr(), lse.data_ptr() if lse is not False else None
+    _here(cu, kv_len, table, workspace, *pages)
+    if workspace is None:
+        need = ctypes.c_size_t()
+        _check(lib().protokv_page_attend_workspace(ctypes.byref(a), ctypes.byref(need)))
+        if need.value:
+            workspace = _new(need.value, torch.uint8, q, stream)
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib().protokv_page_attend(ctypes.byref(a), _stream_ptr(stream)))
+    return out, lse

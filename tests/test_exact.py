@@ -1,0 +1,162 @@
+"""CPU: the handle-free calls (rotary positions, block tables, exact attention)
+refuse what they cannot do before anything is launched, and say why.  No GPU is
+touched: every call below is refused on the host."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2606_26762_amd import protokv as pk
+
+GOOD = 1 << 20   # an aligned address; refused calls never read it
+
+
+def _status(name, args):
+    return getattr(pk.lib(), "protokv_" + name)(ctypes.byref(args), None)
+
+
+def _set(a, **kw):
+    for f, v in kw.items():
+        head, _, rest = f.partition("__")
+        setattr(getattr(a, head) if rest else a, rest or head, v)
+    return a
+
+
+def plan(**kw):
+    a = pk.PagePlanArgs(4, 100, 16, 8, 64, *([GOOD] * 12))
+    a.free_count_out = GOOD + 64
+    return _set(a, **kw)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(num_requests=0), 1), (dict(num_requests=8193), 2), (dict(num_pages=0), 1), (dict(page_size=0), 2),
+    (dict(page_size=24), 2), (dict(page_size=2048), 2), (dict(num_pages=1 << 27), 2), (dict(table_stride=0), 1),
+    (dict(table_stride=1 << 27), 1), (dict(max_tokens=0), 1), (dict(max_tokens=(1 << 29) + 1), 1),
+    (dict(page_size=1, num_pages=(1 << 29) + 1), 2),
+    (dict(ctx=None), 1), (dict(add=None), 1), (dict(table=None), 1), (dict(free_pages=None), 1),
+    (dict(free_count=None), 1), (dict(free_count_out=None), 1), (dict(cu=None), 1), (dict(kv_len=None), 1),
+    (dict(slots=None), 1), (dict(slots=GOOD + 2), 1), (dict(base=GOOD + 1), 1), (dict(refused=GOOD + 3), 1),
+    (dict(free_count_out=GOOD), 1)])
+def test_page_plan_refuses(kw, status):
+    assert _status("page_plan", plan(**kw)) == status
+    assert b"page_plan: " in pk.lib().protokv_last_error(None)
+
+
+def rotate(**kw):
+    a = pk.RotateArgs(num_tokens=3, num_q_heads=8, num_kv_heads=2, head_dim=128, kv_dtype=pk.KV_BF16, num_axes=3,
+                      positions=GOOD, position_stride=3, axes=pk.pair_axes((16, 24, 24)), theta=1e6, q=GOOD, k=GOOD,
+                      v=GOOD, q_stride=1024, k_stride=256, v_stride=256, q_out=GOOD, k_out=None, q_out_stride=1024,
+                      k_out_stride=256, slots=GOOD)
+    pages = pk.Pages(GOOD, GOOD, 10, 16)
+    for f in [f for f in kw if f.startswith("pages__")]:
+        setattr(pages, f[7:], kw.pop(f))
+    a.pages = ctypes.pointer(pages)
+    if kw.pop("no_pages", False):
+        a.pages = None
+    return _set(a, **kw)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(num_tokens=-1), 1), (dict(num_q_heads=7), 1), (dict(num_kv_heads=0), 1), (dict(head_dim=64), 2),
+    (dict(kv_dtype=2), 1), (dict(num_axes=0), 1), (dict(num_axes=9), 1), (dict(num_axes=2), 1), (dict(axes=None), 1),
+    (dict(theta=1.0), 1), (dict(theta=float("nan")), 1), (dict(theta=float("inf")), 1), (dict(position_stride=-1), 1),
+    (dict(positions=None), 1), (dict(positions=GOOD + 2), 1), (dict(q=None), 1), (dict(q_out=None), 1),
+    (dict(k=None), 1), (dict(v=None), 1), (dict(no_pages=True), 1), (dict(no_pages=True, v=None), 1),
+    (dict(slots=None), 1), (dict(q=GOOD + 8), 1), (dict(q_stride=1020), 1), (dict(q_stride=1025), 1),
+    (dict(k_stride=255), 1), (dict(v_stride=260), 1), (dict(q_out_stride=2048), 1),
+    (dict(k_out=GOOD + 16, k_out_stride=128), 1), (dict(pages__page_size=12), 2), (dict(pages__num_pages=0), 1),
+    (dict(pages__num_pages=1 << 27), 2), (dict(pages__k=None), 1), (dict(pages__v=GOOD + 4), 1)])
+def test_rotate_refuses(kw, status):
+    assert _status("rotate", rotate(**dict(kw))) == status
+    assert b"rotate: " in pk.lib().protokv_last_error(None)
+
+
+def prompt(**kw):
+    return _set(pk.PromptArgs(8, 2, 128, pk.KV_BF16, 2, 40, GOOD, GOOD, GOOD, GOOD, 1024, 256, 256, GOOD, GOOD, None,
+                              None), **kw)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(num_q_heads=9), 1), (dict(num_q_heads=0), 1), (dict(num_q_heads=1024, num_kv_heads=2, q_stride=1 << 17), 2),
+    (dict(head_dim=96), 2), (dict(kv_dtype=7), 1), (dict(num_seqs=-1), 1), (dict(num_seqs=1 << 24), 2),
+    (dict(total=-1), 1), (dict(total=1 << 28), 2), (dict(cu=None), 1), (dict(cu=GOOD + 2), 1), (dict(q=None), 1),
+    (dict(k=GOOD + 4), 1), (dict(v=None), 1), (dict(q_stride=1016), 1), (dict(k_stride=257), 1),
+    (dict(v_stride=(1 << 32) + 8), 1), (dict(o=None), 1), (dict(o=GOOD + 8), 1), (dict(lse=GOOD + 1), 1),
+    (dict(prior_o=GOOD), 1), (dict(prior_lse=GOOD), 1), (dict(prior_o=GOOD + 8, prior_lse=GOOD), 1)])
+def test_prompt_attend_refuses(kw, status):
+    assert _status("prompt_attend", prompt(**kw)) == status
+    assert b"prompt_attend: " in pk.lib().protokv_last_error(None)
+
+
+def page(**kw):
+    a = pk.PageAttendArgs(8, 2, 128, pk.KV_BF16, 2, 40, 30, 64, GOOD, GOOD, GOOD, GOOD, 1024,
+                          pk.Pages(GOOD, GOOD, 100, 16), GOOD, GOOD, None, None, GOOD, 1 << 40)
+    return _set(a, **kw)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(num_q_heads=9), 1), (dict(head_dim=64), 2), (dict(kv_dtype=-1), 1), (dict(num_requests=-1), 1),
+    (dict(total=-5), 1), (dict(total=1 << 28), 2), (dict(max_add=0), 1), (dict(table_stride=0), 1),
+    (dict(table_stride=1 << 27), 1), (dict(cu=None), 1), (dict(kv_len=None), 1), (dict(kv_len=GOOD + 1), 1),
+    (dict(table=None), 1), (dict(q=None), 1), (dict(q_stride=1000), 1), (dict(pages__page_size=0), 2),
+    (dict(pages__page_size=48), 2), (dict(pages__num_pages=0), 1), (dict(pages__num_pages=1 << 27), 2),
+    (dict(pages__k=None), 1), (dict(pages__v=GOOD + 2), 1), (dict(o=None), 1), (dict(prior_o=GOOD), 1),
+    (dict(workspace=None), 3), (dict(workspace=GOOD + 16), 3), (dict(workspace_bytes=1000), 3)])
+def test_page_attend_refuses(kw, status):
+    assert _status("page_attend", page(**kw)) == status
+    assert b"page_attend: " in pk.lib().protokv_last_error(None)
+
+
+def test_null_arguments_are_refused():
+    L = pk.lib()
+    for name in ("page_plan", "rotate", "prompt_attend", "page_attend"):
+        assert getattr(L, "protokv_" + name)(None, None) == 1
+    n = ctypes.c_size_t()
+    assert L.protokv_page_attend_workspace(None, ctypes.byref(n)) == 1
+    assert L.protokv_page_attend_workspace(ctypes.byref(page()), None) == 1
+
+
+def test_empty_calls_are_done_at_once():
+    """Nothing to do is no error, and nothing is launched."""
+    assert _status("rotate", rotate(num_tokens=0, positions=None, slots=None)) == 0
+    for kw in (dict(num_seqs=0), dict(total=0)):
+        assert _status("prompt_attend", prompt(**kw)) == 0
+    for kw in (dict(num_requests=0), dict(total=0)):
+        assert _status("page_attend", page(**kw)) == 0
+
+
+def _workspace(**kw):
+    n = ctypes.c_size_t(1 << 62)
+    assert pk.lib().protokv_page_attend_workspace(ctypes.byref(page(**kw)), ctypes.byref(n)) == 0
+    return n.value
+
+
+def test_page_attend_workspace_goes_by_sizes_alone():
+    base = _workspace()
+    assert base == _workspace(cu=None, kv_len=None, table=None, q=None, o=None, workspace=None, pages__k=None)
+    assert 0 < base < 1 << 28
+    n = ctypes.c_size_t()
+    assert pk.lib().protokv_page_attend_workspace(ctypes.byref(page(head_dim=64)), ctypes.byref(n)) == 2
+
+
+def test_pair_axes():
+    assert pk.pair_axes((16, 24, 24)) == bytes([0] * 16 + [1] * 24 + [2] * 24)
+    inter = pk.pair_axes((16, 24, 24), interleaved=True)
+    assert inter[:48] == bytes([0, 1, 2] * 16) and inter[48:] == bytes([1, 2] * 8)
+    assert pk.pair_axes((64,)) == bytes(64) == pk.pair_axes([64], interleaved=True)
+    for bad in ((16, 24), (65, -1), (), (8,) * 9, (0, 63)):
+        with pytest.raises(ValueError):
+            pk.pair_axes(bad)
+
+
+def test_binding_refuses_host_tensors_and_wrong_shapes():
+    q, k = torch.zeros(4, 8, 128, dtype=torch.bfloat16), torch.zeros(4, 2, 128, dtype=torch.bfloat16)
+    cu = torch.tensor([0, 4], dtype=torch.int32)
+    with pytest.raises(ValueError):
+        pk.prompt_attend(q, k, k, cu)
+    with pytest.raises(ValueError):
+        pk.rotate(q, k, torch.zeros(4, dtype=torch.int32), pk.pair_axes((64,)), 1e4)
+    with pytest.raises(ValueError):
+        pk.rotate(None, None, cu, pk.pair_axes((64,)), 1e4)
+    with pytest.raises(ValueError):
+        pk.page_attend(q, (k, k), cu, cu, cu, 1)
