@@ -95,11 +95,26 @@ void plan_blocks(ExactArgs& a, bool fp32, bool paged) {
   }
 }
 
-size_t part_bytes(const ExactArgs& a, bool fp32, size_t* ml) {
-  if (a.splits == 1) return 0;
-  const size_t rows = (size_t)a.Hkv * a.blocks * a.splits * (fp32 ? EX_ROWS_F32 : EX_ROWS);
-  *ml = rows * D * 4;
-  return rows * (D + 3) * 4;
+// The workspace's parts, from `base` on (may be null); its size.
+size_t lay_out(ExactArgs& a, bool fp32, uint8_t* base) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    uint8_t* p = base ? base + off : nullptr;
+    off += (bytes + 255) & ~(size_t)255;
+    return p;
+  };
+  if (a.few) {
+    const size_t rows = (size_t)a.few * 2 * EX_FEW;
+    a.few_o = (float*)take(rows * D * 4);
+    a.few_ml = (float*)take(rows * 3 * 4);
+    a.few_meta = (int32_t*)take((size_t)a.few * 4 * 4);
+  }
+  if (a.splits > 1) {
+    const size_t rows = (size_t)a.Hkv * a.blocks * a.splits * (fp32 ? EX_ROWS_F32 : EX_ROWS);
+    a.part_o = (float*)take(rows * D * 4);
+    a.part_ml = (float*)take(rows * 3 * 4);
+  }
+  return off;
 }
 
 protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a, const char* who) {
@@ -126,7 +141,13 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   a.stride = p->table_stride;
   a.shift = log2i(p->pages.page_size);
   a.num_pages = p->pages.num_pages;
-  plan_blocks(a, h.dtype == PROTOKV_KV_FP32, true);
+  const bool fp32 = h.dtype == PROTOKV_KV_FP32;
+  if (!fp32) {  // requests of few rows go to a kernel of their own, the others to row blocks
+    const int64_t tiles = (((int64_t)a.stride << a.shift) + 31) / 32;
+    a.few = (int)std::min<int64_t>(EX_FEW_WGS, ((int64_t)a.Hkv * a.n * tiles + 7) / 8);
+  }
+  a.splits = 1;
+  if (fp32 || (int64_t)a.max_add * a.grp > EX_FEW) plan_blocks(a, fp32, true);
   if ((int64_t)a.blocks * a.Hkv * a.splits * 8 >= (1ll << 31))
     return fail(PROTOKV_E_UNSUPPORTED, who, "too many row blocks for one launch");
   return PROTOKV_OK;
@@ -274,8 +295,7 @@ protokv_status protokv_page_attend_workspace(const protokv_page_attend_args* p, 
   if (!p || !bytes) return fail(PROTOKV_E_INVALID, who, "args and bytes must be non-NULL");
   ExactArgs a{};
   protokv_status s = page_attend_shape(p, a, who);
-  size_t ml;
-  if (s == PROTOKV_OK) *bytes = part_bytes(a, p->kv_dtype == PROTOKV_KV_FP32, &ml);
+  if (s == PROTOKV_OK) *bytes = lay_out(a, p->kv_dtype == PROTOKV_KV_FP32, nullptr);
   return s;
 })
 
@@ -294,15 +314,13 @@ protokv_status protokv_page_attend(const protokv_page_attend_args* p, void* stre
   if (!p->kv_len || !p->table || off4(p->kv_len) || off4(p->table))
     return fail(PROTOKV_E_INVALID, who, "kv_len and table must be non-NULL and aligned to 4 bytes");
   const bool fp32 = h.dtype == PROTOKV_KV_FP32;
-  size_t ml = 0;
-  const size_t need = part_bytes(a, fp32, &ml);
+  const size_t need = lay_out(a, fp32, nullptr);
   if (need) {
     if (!p->workspace) return fail(PROTOKV_E_WORKSPACE, who, "workspace is NULL");
     if ((uintptr_t)p->workspace % 256) return fail(PROTOKV_E_WORKSPACE, who, "workspace must be 256-byte aligned");
     if (p->workspace_bytes < need)
       return fail(PROTOKV_E_WORKSPACE, who, ("workspace too small: need " + std::to_string(need) + " bytes").c_str());
-    a.part_o = (float*)p->workspace;
-    a.part_ml = (float*)((uint8_t*)p->workspace + ml);
+    lay_out(a, fp32, (uint8_t*)p->workspace);
   }
   a.q = p->q;
   a.k = p->pages.k;

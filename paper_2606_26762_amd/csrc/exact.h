@@ -18,6 +18,8 @@ constexpr int EX_ROWS = 256;      // query rows per workgroup of the bf16 kernel
 constexpr int EX_ROWS_F32 = 32;   // query rows per wave of the float32 kernel
 constexpr int EX_MAX_SPLITS = 16;
 constexpr int EX_MIN_TILES = 8;   // 64-key (bf16) or 32-key (float32) tiles that a context split has at least
+constexpr int EX_FEW = 32;        // rows per kv head of a request that the few-rows kernel takes
+constexpr int EX_FEW_WGS = 256;   // workgroups of the few-rows kernel, at most
 constexpr int MAX_REQUESTS = 8192;
 constexpr int MAX_AXES = 8;
 
@@ -35,7 +37,12 @@ struct ExactArgs {
   int n, total, max_add;
   int Hq, Hkv, grp;
   int stride, shift, num_pages;  // block table row, log2 page size
-  int blocks;  // row-block indices per kv head
+  // few-rows kernel: two partials per workgroup [workgroup][2][32][D], [..][3], and
+  // the split item that begins in a workgroup (see k_exact_few)
+  float *few_o, *few_ml;
+  int32_t* few_meta;
+  int few;     // its workgroups (0: not launched, the row blocks take every request)
+  int blocks;  // row-block indices per kv head (0: no row blocks)
   int splits;  // most context splits of a row block
 };
 
