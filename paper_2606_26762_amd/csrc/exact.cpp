@@ -104,7 +104,7 @@ size_t lay_out(ExactArgs& a, bool fp32, uint8_t* base) {
     return p;
   };
   if (a.few) {
-    const size_t rows = (size_t)a.few * 2 * EX_FEW;
+    const size_t rows = (size_t)a.few * 2 * a.few_rows;
     a.few_o = (float*)take(rows * D * 4);
     a.few_ml = (float*)take(rows * 3 * 4);
     a.few_meta = (int32_t*)take((size_t)a.few * 4 * 4);
@@ -144,7 +144,9 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   const bool fp32 = h.dtype == PROTOKV_KV_FP32;
   if (!fp32) {  // requests of few rows go to a kernel of their own, the others to row blocks
     const int64_t tiles = (((int64_t)a.stride << a.shift) + 31) / 32;
-    a.few = (int)std::min<int64_t>(EX_FEW_WGS, ((int64_t)a.Hkv * a.n * tiles + 7) / 8);
+    const int64_t waves = std::max<int64_t>(1, ((int64_t)a.Hkv * a.n * tiles + EX_FEW_TILES - 1) / EX_FEW_TILES);
+    a.few = a.n ? (int)std::min<int64_t>(EX_FEW_WAVES, (waves + 3) / 4 * 4) : 0;
+    a.few_rows = (int)std::min<int64_t>(EX_FEW, (int64_t)a.max_add * a.grp);
   }
   a.splits = 1;
   if (fp32 || (int64_t)a.max_add * a.grp > EX_FEW) plan_blocks(a, fp32, true);

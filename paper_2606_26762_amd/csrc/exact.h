@@ -19,7 +19,8 @@ constexpr int EX_ROWS_F32 = 32;   // query rows per wave of the float32 kernel
 constexpr int EX_MAX_SPLITS = 16;
 constexpr int EX_MIN_TILES = 8;   // 64-key (bf16) or 32-key (float32) tiles that a context split has at least
 constexpr int EX_FEW = 32;        // rows per kv head of a request that the few-rows kernel takes
-constexpr int EX_FEW_WGS = 256;   // workgroups of the few-rows kernel, at most
+constexpr int EX_FEW_WAVES = 2048;  // waves of the few-rows kernel, at most (two to a SIMD)
+constexpr int EX_FEW_TILES = 2;   // 32-key tiles that a wave of it has at least
 constexpr int MAX_REQUESTS = 8192;
 constexpr int MAX_AXES = 8;
 
@@ -37,11 +38,11 @@ struct ExactArgs {
   int n, total, max_add;
   int Hq, Hkv, grp;
   int stride, shift, num_pages;  // block table row, log2 page size
-  // few-rows kernel: two partials per workgroup [workgroup][2][32][D], [..][3], and
-  // the split item that begins in a workgroup (see k_exact_few)
+  // few-rows kernel: two partials per wave [wave][2][few_rows][D], [..][3], and the
+  // split item that begins in a wave (see k_exact_few)
   float *few_o, *few_ml;
   int32_t* few_meta;
-  int few;     // its workgroups (0: not launched, the row blocks take every request)
+  int few, few_rows;  // its waves (0: not launched, the row blocks take every request), its rows at most
   int blocks;  // row-block indices per kv head (0: no row blocks)
   int splits;  // most context splits of a row block
 };

@@ -129,6 +129,48 @@ __device__ __forceinline__ void store4(const ExactArgs& a, size_t row, int d, f3
   }
 }
 
+// A hidden key has weight 0, but 0 x inf and 0 x NaN are not 0.  Where a tile with
+// hidden keys holds such values they are taken out of the product (0 in their
+// place), and two more products with a 1 where a value was +inf or NaN, or -inf or
+// NaN, tell which outputs they belong to: those with a positive weight on one.
+// Two bfloat16 at a time, flags in each half's bit 15 (no compares: their masks
+// would not fit the scalar registers).
+__device__ __forceinline__ uint32_t odd_flags(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint32_t odd_flags(v8i16 v) {
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  return odd_flags(w[0]) | odd_flags(w[1]) | odd_flags(w[2]) | odd_flags(w[3]);
+}
+constexpr uint32_t ODD = 0x80008000u;
+// WHAT 0: the values without the odd ones; 1, -1: a 1 for each of that sign
+template <int WHAT>
+__device__ __forceinline__ bf16x8 odd_operand(v8i16 v) {
+  u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t odd = odd_flags(w[i]) & ODD;
+    if (WHAT == 0) {
+      w[i] &= ~((odd >> 15) * 0xFFFFu);
+    } else {
+      const uint32_t nan = ((w[i] & 0x007F007Fu) + 0x007F007Fu) << 8;
+      w[i] = ((odd & (nan | (WHAT > 0 ? ~w[i] : w[i]))) >> 15) * 0x3F80u;
+    }
+  }
+  return __builtin_bit_cast(bf16x8, w);
+}
+// 0, of which the compiler does not know it: what is read at an address with it
+// added is read anew, so that the passes below do not keep each other's operands
+__device__ __forceinline__ int anew() {
+  int z = 0;
+  asm volatile("" : "+v"(z));
+  return z;
+}
+template <int SIGN>
+__device__ __forceinline__ void add_odd(f32x16& o, const f32x16& hits) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[i] += hits[i] > 0.f ? (SIGN > 0 ? INFINITY : -INFINITY) : 0.f;
+}
+
 // Barrier for LDS traffic only: outstanding global loads are not waited for.
 __device__ __forceinline__ void ex_barrier() {
   __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
@@ -295,53 +337,47 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     l2 += part[0] + part[1];
     // V^T operand of 32-dim block b, 16-key step st: positions half * 8 + i are
     // keys 16 st + 4 half + {0..3} (i < 4) and + 8 (i >= 4), as P's registers are
-    auto read_v = [&](int b, int st) {
-      const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + b * 4096 + st * 1024));
-      const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + b * 4096 + st * 1024 + 512));
+    auto read_v = [&](int b, int st, int z = 0) {
+      const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + z + b * 4096 + st * 1024));
+      const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + z + b * 4096 + st * 1024 + 512));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
     if constexpr (MASK) {
-      // A masked key has weight 0, but 0 x inf and 0 x NaN are not 0.  If the tile
-      // holds such a value, the products are formed for one token's rows at a time,
-      // with the keys that it does not see set to 0.
-      bool odd = false;
+      uint32_t odd = 0;
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int st = 0; st < 4; ++st) {
           const v8i16 v = read_v(b, st);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) odd |= (v[i] & 0x7F80) == 0x7F80;
+          odd |= odd_flags(v);
+          oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<0>(v), pb[st], oacc[b], 0, 0, 0);
         }
-      if (__ballot(odd)) {  // uniform
-        for (int tk = wtok0; tk <= wtok1; ++tk) {  // uniform
-          const int lim = it.off + tk - t * EX_KEYS - 4 * half;
-          const bool mine = rvalid && tok == tk;
+      if (__ballot((odd & ODD) != 0)) {  // uniform
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            f32x16 acc = zero;
+        for (int b = 0; b < 4; ++b) {
+          f32x16 hits = zero;
+          int z = anew();
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {
-              v8i16 v = read_v(b, st);
+          for (int st = 0; st < 4; ++st)
+            hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<1>(read_v(b, st, z)), pb[st], hits, 0, 0, 0);
+          add_odd<1>(oacc[b], hits);
+          __builtin_amdgcn_sched_barrier(0);
+          hits = zero;
+          z = anew();
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int c = 16 * st + 8 * (i >> 2) + (i & 3);
-                if (c > lim || (PAGED && ((bad >> c) & 1))) v[i] = 0;
-              }
-              acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pb[st], acc, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) oacc[b][i] = mine ? oacc[b][i] + acc[i] : oacc[b][i];
-          }
+          for (int st = 0; st < 4; ++st)
+            hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<-1>(read_v(b, st, z)), pb[st], hits, 0, 0, 0);
+          add_odd<-1>(oacc[b], hits);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        return;
       }
+    } else {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+          oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, read_v(b, st)), pb[st], oacc[b], 0, 0, 0);
     }
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-        oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, read_v(b, st)), pb[st], oacc[b], 0, 0, 0);
   };
 
   if constexpr (PAGED) {
@@ -565,36 +601,41 @@ __global__ __launch_bounds__(256, 2) void k_exact_f32(ExactArgs a) {
       part[i & 3] += s[i];
     }
     lrun += (part[0] + part[1]) + (part[2] + part[3]);
-    bool odd = false;
-    if (masked) {  // 0 x inf is not 0: as in the bf16 kernel
+    if (masked) {
+      uint32_t odd = 0;  // bit 31
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
-          odd |= (__float_as_uint(v0[i][b]) & 0x7F800000u) == 0x7F800000u ||
-                 (__float_as_uint(v1[i][b]) & 0x7F800000u) == 0x7F800000u;
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (__ballot(odd)) {  // uniform
-      for (int tk = wtok0; tk <= wtok1; ++tk) {  // uniform
-        const int lim = it.off + tk - t * EX_KEYS32 - 4 * half;
-        const bool mine = rvalid && tok == tk;
+          odd |= ((__float_as_uint(v0[i][b]) & 0x7F800000u) + 0x00800000u) | ((__float_as_uint(v1[i][b]) & 0x7F800000u) + 0x00800000u);
+      if (__ballot((int)odd < 0)) {  // uniform: what is odd goes into the sums at once and out of the values
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          f32x16 acc = zero;
+          f32x16 hits = zero;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int c = 8 * (i >> 2) + (i & 3);
-            const bool hide = c > lim || ((badm >> c) & 1);
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(hide ? 0.f : (i < 8 ? v0 : v1)[i & 7][b], s[i], acc, 0, 0, 0);
+            const float x = (i < 8 ? v0 : v1)[i & 7][b];
+            hits = __builtin_amdgcn_mfma_f32_32x32x2f32(x == INFINITY || x != x ? 1.f : 0.f, s[i], hits, 0, 0, 0);
           }
+          add_odd<1>(oacc[b], hits);
+          __builtin_amdgcn_sched_barrier(0);
+          hits = zero;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) oacc[b][i] = mine ? oacc[b][i] + acc[i] : oacc[b][i];
+          for (int i = 0; i < 16; ++i) {
+            const float x = (i < 8 ? v0 : v1)[i & 7][b];
+            hits = __builtin_amdgcn_mfma_f32_32x32x2f32(x == -INFINITY || x != x ? 1.f : 0.f, s[i], hits, 0, 0, 0);
+          }
+          add_odd<-1>(oacc[b], hits);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            v0[i][b] = fabsf(v0[i][b]) < INFINITY ? v0[i][b] : 0.f;
+            v1[i][b] = fabsf(v1[i][b]) < INFINITY ? v1[i][b] : 0.f;
+          }
         }
       }
-      load_k(kp, 1, k1);
-      continue;
     }
+    __builtin_amdgcn_sched_barrier(0);
     weigh(v0, s, 0, oacc);
     __builtin_amdgcn_sched_barrier(0);
     load_k(kp, 1, k1);
@@ -666,103 +707,104 @@ __global__ __launch_bounds__(256) void k_exact_join(ExactArgs a) {
 // bf16, requests of at most 32 rows per kv head (single tokens of an answer).
 // What they cost is reading the cache once, so the keys are shared out evenly:
 // the 32-key tiles of all (request, kv head) items, laid end to end, are cut into
-// equal runs, one per workgroup, whatever the requests' lengths.  A workgroup goes
-// through its run item by item; its eight waves take the item's tiles in turn,
-// each by itself (K rows straight into the A operand, V rows through registers
-// into the wave's LDS for the transposed reads, the next tile's loads in flight),
-// and merge once per item.  An item within one run is written out; of one that
-// runs on, each workgroup leaves a partial (at most two per workgroup: the item it
-// ends in, slot 1, and the one it continues, slot 0), and the workgroup that the
-// item begins in notes it for k_exact_few_join.
-constexpr int FW_W = 8;                  // waves
-constexpr int FW_VB = 32 * 64 + 64;      // bytes of one 32-dim block of a V tile (64 of padding: bank spread)
-constexpr int FW_LDS = FW_W * 66 * 64 * 4;  // the merge; the waves' V tiles lie in it too
-static_assert(FW_W * 4 * FW_VB <= FW_LDS && FW_LDS <= 150000, "LDS layout");
+// equal runs, one per wave, whatever the requests' lengths.  A wave goes through
+// its run item by item and needs no other wave: K rows straight into the A
+// operand, V rows straight into the wave's LDS for the transposed reads, the next
+// tile's loads in flight.  An item within one run is written out; of one
+// that runs on, each wave leaves a partial (at most two per wave: the item it ends
+// in, slot 1, and the one it continues, slot 0), and the wave that the item begins
+// in notes it for k_exact_few_join.
+constexpr int FW_W = 4;              // waves per workgroup
+constexpr int FW_VB = 32 * 64 + 64;  // bytes of one 32-dim block of a V tile (64 of padding: bank spread)
 
-__device__ __forceinline__ void few_lds_order() { asm volatile("" ::: "memory"); }  // a wave's LDS operations run in order
-
-__global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_LDS];
-  __shared__ long long s_pre[FW_W * 64 + 1];  // tiles per kv head before each request of a chunk
-  __shared__ long long s_wsum[FW_W];
-  constexpr int NT = FW_W * 64;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int m = lane & 31, half = lane >> 5;
-  struct Req {
-    int s0, add, rows, kv;
-  };
-  auto req_of = [&](int i) {
-    Req r;
-    const int c0 = min(max(a.cu[i], 0), a.total), c1 = min(max(a.cu[i + 1], 0), a.total);
-    r.s0 = c0;
-    r.add = max(c1 - c0, 0);
-    r.rows = (int)min((long long)min(r.add, a.max_add) * a.grp, (long long)EX_FEW + 1);
-    r.kv = min(max(a.kv_len[i], 0), a.stride << a.shift);
-    return r;
-  };
-  // tiles of a request: one even if its rows see nothing, 0 if it is not this kernel's
-  auto tiles_of = [&](const Req& r) { return r.rows < 1 || r.rows > EX_FEW ? 0 : max(1, (r.kv + 31) / 32); };
-  // running sums of chunk c's tiles, from `before` on, into s_pre; the sum after it
-  auto scan_chunk = [&](int c, long long before) {
-    const int i = c * NT + tid;
-    long long x = i < a.n ? tiles_of(req_of(i)) : 0;
+// What k_exact_few takes of request i.
+struct Few {
+  int s0, add, rows, kv, tiles;  // tiles: one even if its rows see nothing, 0 if it is not that kernel's
+};
+__device__ __forceinline__ Few few_of(const ExactArgs& a, int i) {
+  Few r;
+  const int c0 = min(max(a.cu[i], 0), a.total), c1 = min(max(a.cu[i + 1], 0), a.total);
+  r.s0 = c0;
+  r.add = max(c1 - c0, 0);
+  r.rows = (int)min((long long)min(r.add, a.max_add) * a.grp, (long long)EX_FEW + 1);
+  r.kv = min(max(a.kv_len[i], 0), a.stride << a.shift);
+  r.tiles = r.rows < 1 || r.rows > EX_FEW ? 0 : max(1, (r.kv + 31) / 32);
+  return r;
+}
+__device__ __forceinline__ long long lane_ll(long long x, int l) {
+  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)x, l), hi = __builtin_amdgcn_readlane((int)(x >> 32), l);
+  return (long long)((unsigned long long)hi << 32 | lo);
+}
+// inclusive running sum over the wave
+__device__ __forceinline__ long long wave_sum(long long x) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const long long y = __shfl_up(x, d, 64);
-      if (lane >= d) x += y;
-    }
-    __syncthreads();  // s_pre and s_wsum are free
-    if (lane == 63) s_wsum[wave] = x;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) x += s_wsum[w];
-    s_pre[tid + 1] = before + x;
-    if (tid == 0) s_pre[0] = before;
-    __syncthreads();
-    return s_pre[NT];
-  };
-  const int chunks = (a.n + NT - 1) / NT;
-  long long total = 0;
-  for (int c = 0; c < chunks; ++c) total = scan_chunk(c, total);
-  const long long N = total * a.Hkv;
-  // a run is at least a tile for each wave
-  const long long wgs = min((long long)gridDim.x, (N + FW_W - 1) / FW_W);
-  const long long per = wgs ? (N + wgs - 1) / wgs : 1;
-  const long long x0 = min(N, blockIdx.x * per), x1 = min(N, x0 + per);
-  int32_t* meta = a.few_meta + blockIdx.x * 4;
-  bool noted = false;
-
+  for (int d = 1; d < 64; d *= 2) {
+    const long long y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+__global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2][4 * FW_VB];  // the V tile in use and the next
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int w = blockIdx.x * FW_W + wave;
+  const int m = lane & 31, half = lane >> 5;
+  int32_t* meta = a.few_meta + w * 4;
+  // total tiles and this wave's run: lane l sums the requests of the l-th of 64 blocks
+  const int per64 = (a.n + 63) / 64;
+  long long mine = 0;
+  for (int j = 0; j < per64; ++j) {
+    const int i = lane * per64 + j;
+    if (i < a.n) mine += few_of(a, i).tiles;
+  }
+  long long upto = wave_sum(mine);
+  const long long N = lane_ll(upto, 63) * a.Hkv;
+  const long long waves = (long long)gridDim.x * FW_W;
+  const long long per = max((N + waves - 1) / waves, (long long)EX_FEW_TILES);
+  const long long x1 = min(N, (w + 1) * per);
+  long long x = w * per;
+  if (lane == 0) meta[0] = -1;
+  if (x >= N) return;  // uniform, and nothing below synchronises waves
+  int i0;               // first request of the 64 in the lanes
+  long long before;     // tiles before it
+  {
+    const int l = __popcll(__ballot((upto - mine) * a.Hkv <= x)) - 1;
+    i0 = __builtin_amdgcn_readfirstlane(l) * per64;
+    before = lane_ll(upto - mine, __builtin_amdgcn_readfirstlane(l));
+  }
   const uint8_t* kb = (const uint8_t*)a.k;
   const uint8_t* vb = (const uint8_t*)a.v;
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  uint8_t* mem = s_mem + wave * 4 * FW_VB;
   const int grp16 = lane >> 4, s16 = lane & 15;
-  const uint8_t* vl = mem + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
+  const uint8_t* vl0 = s_mem[wave][0] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
   const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
 
   // tiles [ta, tb) of request i's kv head kvh; whole: that is all of them
-  auto item = [&](int i, const Req& rq, int kvh, int ta, int tb, bool whole, int slot) {
-    const int off = rq.kv - rq.add;
-    const bool rvalid = m < rq.rows;
+  auto item = [&](int i, int s0, int add, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
+    const int off = kv - add;
+    const bool rvalid = m < rows;
     const int tok = rvalid ? m / a.grp : 0;
     const int head = kvh * a.grp + (rvalid ? m - tok * a.grp : 0);
-    const size_t orow = (size_t)(rq.s0 + tok) * a.Hq + head;
+    const size_t orow = (size_t)(s0 + tok) * a.Hq + head;
     const int klim = rvalid ? off + tok : -1;
-    const int ntok = (rq.rows - 1) / a.grp + 1;
-    const int wfull = off + 1;
-    const int kend = min(max(off + ntok, 0), rq.kv);
-    const int tend = min(tb, (kend + 31) / 32);  // tiles behind the last row's last key are skipped
+    const int ntok = (rows - 1) / a.grp + 1;
+    const int wfull = off + 1;                          // keys that every row sees
+    const int kend = min(max(off + ntok, 0), kv);       // keys that some row sees
+    const int tend = min(tb, (kend + 31) / 32);
     const int32_t* row = a.table + (size_t)i * a.stride;
     bf16x8 bq[8];
     {
-      const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(rq.s0 + tok) * a.qs + head * (D * 2));
+      const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(s0 + tok) * a.qs + head * (D * 2));
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[2 * kk + half]);
     }
     f32x16 oacc[4] = {zero, zero, zero, zero};
     float mref = EX_NONE, l1 = 0.f, l2 = 0.f;
     auto id_of = [&](int t) { return row[min(t * 32 + m, kend - 1) >> a.shift]; };
-    // row index in the pages of this lane's key of tile t on page id; bad: no page
+    // row index in the pages of this lane's key of tile t on page id (a tensor of
+    // 2^31 rows would not fit the GPU); bad: no page, page 0 is read instead
     auto row_of = [&](int t, int id, bool& bad) {
       const int key = min(t * 32 + m, kend - 1);
       bad = (unsigned)id >= (unsigned)a.num_pages;
@@ -773,54 +815,54 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) kr[kk] = p[2 * kk + half];
     };
-    auto load_v = [&](int rw, u16x8 (&vr)[8]) {  // unit j: row 4 j + lane / 16, 16-byte chunk lane % 16
+    // V rows of the tile straight into the wave's LDS: instruction (b, g) takes 32-dim
+    // block b of rows 16 g .. + 15
+    auto load_v = [&](int rw, int buf) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned r = __builtin_amdgcn_ds_bpermute(4 * (lane >> 4) + 16 * j, rw);
-        vr[j] = (reinterpret_cast<const u16x8*>(vb) + (size_t)r * 16)[lane & 15];
+      for (int g = 0; g < 2; ++g) {
+        const unsigned r = __builtin_amdgcn_ds_bpermute(64 * g + (lane & ~3), rw);
+        const uint8_t* p = vb + (size_t)r * (D * 2) + (lane & 3) * 16;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) lds_dma16(p + b * 64, s_mem[wave][buf] + b * FW_VB + g * 1024);
       }
     };
-    int t = ta + wave;
-    if (t < tend) {
-      u16x8 kr[8], vr[8];
+    if (ta < tend) {
+      u16x8 kr[8];
       bool bad;
-      int rw = row_of(t, id_of(t), bad);
-      int id = id_of(min(t + FW_W, tend - 1));
-      load_v(rw, vr);
+      int rw = row_of(ta, id_of(ta), bad);
+      int id = id_of(min(ta + 1, tend - 1));
+      load_v(rw, ta & 1);
+      __builtin_amdgcn_sched_barrier(0);
       load_k(rw, kr);
-      for (; t < tend; t += FW_W) {
-        const int tn = min(t + FW_W, tend - 1);  // past the last tile the loads repeat it
-        bool nbad;
-        rw = row_of(tn, id, nbad);
-        id = id_of(min(tn + FW_W, tend - 1));
+      for (int t = ta; t < tend; ++t) {
+        const int tn = min(t + 1, tend - 1);  // past the last tile the loads repeat it
         const unsigned badm = (unsigned)__ballot(bad);
+        rw = row_of(tn, id, bad);
         const bool masked = (t + 1) * 32 > wfull || badm != 0;  // uniform
-        {
-          uint8_t* vw = mem + ((lane & 15) >> 2) * FW_VB + (lane >> 4) * 64 + (lane & 3) * 16;
-          few_lds_order();
-#pragma unroll
-          for (int j = 0; j < 8; ++j) *reinterpret_cast<u16x8*>(vw + j * 256) = vr[j];
-          few_lds_order();
-        }
-        bool odd = false;
-        if (masked) {  // 0 x inf is not 0: as in k_exact_bf16
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) odd |= (vr[j][e] & 0x7F80) == 0x7F80;
-        }
-        load_v(rw, vr);
         f32x16 s = zero;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
           s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[kk]), bq[kk], s, 0, 0, 0);
-        load_k(rw, kr);
-        const int rel = klim - t * 32 - 4 * half;
+        // Loads return in the order of their issue: V's are issued before K's of the
+        // same tile, so with K in the registers of the products V is in LDS.
+        asm volatile("" : "+v"(s) : : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 1 < tend) {  // uniform
+          id = id_of(min(tn + 1, tend - 1));
+          load_v(rw, (t + 1) & 1);  // read last by the products of tile t - 1
+          __builtin_amdgcn_sched_barrier(0);
+          load_k(rw, kr);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const uint8_t* vl = vl0 + (t & 1) * (4 * FW_VB);
         if (masked) {
+          const int rel = klim - t * 32 - 4 * half;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int c = 8 * (j >> 2) + (j & 3);
-            s[j] = c > rel || ((badm >> (c + 4 * half)) & 1) ? -INFINITY : s[j];
+          for (int j = 0; j < 16; ++j) s[j] = 8 * (j >> 2) + (j & 3) > rel ? -INFINITY : s[j];
+          if (badm) {
+            const unsigned bm = badm >> (4 * half);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[j] = (bm >> (8 * (j >> 2) + (j & 3))) & 1 ? -INFINITY : s[j];
           }
         }
         float tmax = -INFINITY;
@@ -854,30 +896,38 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
         }
         l1 += sum0 + sum1;
         l2 += part[0] + part[1];
-        auto read_v = [&](int b, int st) {
-          const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + b * FW_VB + st * 1024));
-          const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + b * FW_VB + st * 1024 + 512));
+        auto read_v = [&](int b, int st, int z = 0) {
+          const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + z + b * FW_VB + st * 1024));
+          const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + z + b * FW_VB + st * 1024 + 512));
           return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        if (__ballot(odd)) {  // uniform: one token's rows at a time, what it does not see set to 0
-          for (int tk = 0; tk < ntok; ++tk) {
-            const int lim = off + tk - t * 32 - 4 * half;
-            const bool mine = rvalid && tok == tk;
+        if (masked) {
+          uint32_t odd = 0;
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+              const v8i16 v = read_v(b, st);
+              odd |= odd_flags(v);
+              oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<0>(v), pb[st], oacc[b], 0, 0, 0);
+            }
+          if (__ballot((odd & ODD) != 0)) {  // uniform
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-              f32x16 acc = zero;
+              f32x16 hits = zero;
+              int z = anew();
 #pragma unroll
-              for (int st = 0; st < 2; ++st) {
-                v8i16 v = read_v(b, st);
+              for (int st = 0; st < 2; ++st)
+                hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<1>(read_v(b, st, z)), pb[st], hits, 0, 0, 0);
+              add_odd<1>(oacc[b], hits);
+              __builtin_amdgcn_sched_barrier(0);
+              hits = zero;
+              z = anew();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  const int c = 16 * st + 8 * (e >> 2) + (e & 3);
-                  if (c > lim || ((badm >> (c + 4 * half)) & 1)) v[e] = 0;
-                }
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pb[st], acc, 0, 0, 0);
-              }
-#pragma unroll
-              for (int e = 0; e < 16; ++e) oacc[b][e] = mine ? oacc[b][e] + acc[e] : oacc[b][e];
+              for (int st = 0; st < 2; ++st)
+                hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<-1>(read_v(b, st, z)), pb[st], hits, 0, 0, 0);
+              add_odd<-1>(oacc[b], hits);
+              __builtin_amdgcn_sched_barrier(0);
             }
           }
         } else {
@@ -887,160 +937,136 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
             for (int st = 0; st < 2; ++st)
               oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, read_v(b, st)), pb[st], oacc[b], 0, 0, 0);
         }
-        bad = nbad;
       }
     }
-    // merge of the eight waves, each relative to its own reference
     l1 += xor32(l1);
     l2 += xor32(l2);
-    ex_barrier();  // the tiles' LDS is reused (before this item: read out by the last)
-    float* part = reinterpret_cast<float*>(s_mem);
-    if (rvalid) {
+    if (!rvalid) return;
+    if (whole) {
+      const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
+      const Join j = join_of(l2 == 0.f ? -INFINITY : mref + log2f(l2), a.pl, orow);
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) part[(wave * 66 + b * 16 + j) * 64 + lane] = oacc[b][j];
-      part[(wave * 66 + 64) * 64 + lane] = mref;
-      part[(wave * 66 + 65) * 64 + lane] = half ? l2 : l1;  // both halves hold both sums
+        for (int e = 0; e < 4; ++e)
+          store4<0>(a, orow, b * 32 + e * 8 + half * 4,
+                    (f32x4){oacc[b][4 * e], oacc[b][4 * e + 1], oacc[b][4 * e + 2], oacc[b][4 * e + 3]} * inv, j);
+      if (half == 0 && a.lse) a.lse[orow] = j.lse;
+      return;
     }
-    ex_barrier();
-    float lse = 0.f;
-    if (rvalid) {
-      float M = EX_NONE, L1 = 0.f, L2 = 0.f, wgt[FW_W];
+    const size_t prow = ((size_t)w * 2 + slot) * a.few_rows + m;
 #pragma unroll
-      for (int w = 0; w < FW_W; ++w) M = fmaxf(M, part[(w * 66 + 64) * 64 + lane]);
+    for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int w = 0; w < FW_W; ++w) {
-        wgt[w] = __builtin_amdgcn_exp2f(part[(w * 66 + 64) * 64 + lane] - M);
-        L1 += wgt[w] * part[(w * 66 + 65) * 64 + m];
-        L2 += wgt[w] * part[(w * 66 + 65) * 64 + 32 + m];
-      }
-      const size_t prow = ((size_t)blockIdx.x * 2 + slot) * EX_FEW + m;
-      const float inv = whole ? (L1 > 0.f || L1 != L1 ? 1.0f / L1 : 0.f) : 1.0f;
-      Join j{1.f, 0.f, 0.f};
-      if (whole) j = join_of(L2 == 0.f ? -INFINITY : M + log2f(L2), a.pl, orow);
-      // wave w's registers 8 w .. 8 w + 7: two runs of four dims
-#pragma unroll
-      for (int run = 0; run < 2; ++run) {
-        f32x4 o;
-        const int i0 = wave * 8 + run * 4;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          o[e] = 0.f;
-#pragma unroll
-          for (int w = 0; w < FW_W; ++w) o[e] += wgt[w] * part[(w * 66 + i0 + e) * 64 + lane];
-        }
-        const int dim = (i0 >> 4) * 32 + ((i0 & 15) >> 2) * 8 + half * 4;
-        if (whole) store4<0>(a, orow, dim, o * inv, j);
-        else *reinterpret_cast<f32x4*>(a.few_o + prow * D + dim) = o;
-      }
-      if (wave == 0 && half == 0 && !whole) {
-        a.few_ml[prow * 3] = M;
-        a.few_ml[prow * 3 + 1] = L1;
-        a.few_ml[prow * 3 + 2] = L2;
-      }
-      lse = j.lse;
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(a.few_o + prow * D + b * 32 + e * 8 + half * 4) =
+            (f32x4){oacc[b][4 * e], oacc[b][4 * e + 1], oacc[b][4 * e + 2], oacc[b][4 * e + 3]};
+    if (half == 0) {
+      a.few_ml[prow * 3] = mref;
+      a.few_ml[prow * 3 + 1] = l1;
+      a.few_ml[prow * 3 + 2] = l2;
     }
-    ex_barrier();  // the merge is read out, and the prior's lse, which may be lse itself
-    if (whole && a.lse && wave == 0 && half == 0 && rvalid) a.lse[orow] = lse;
   };
 
-  long long x = x0;
-  for (int c = 0; c < chunks && x < x1; ++c) {
-    if (chunks > 1) scan_chunk(c, c ? s_pre[NT] : 0);
-    const int cnt = min(NT, a.n - c * NT);
-    while (x < x1 && x < s_pre[cnt] * a.Hkv) {
-      int r = 0, hi = cnt;  // the request that x is in: the last one that begins at or before it
-      while (hi - r > 1) {
-        const int mid = (r + hi) >> 1;
-        if (s_pre[mid] * a.Hkv <= x) r = mid;
-        else hi = mid;
-      }
-      r = __builtin_amdgcn_readfirstlane(r);
-      const long long first = s_pre[r] * a.Hkv;
-      const int T = __builtin_amdgcn_readfirstlane((int)(s_pre[r + 1] - s_pre[r]));
+  while (x < x1) {
+    Few q{};
+    if (i0 + lane < a.n) q = few_of(a, i0 + lane);
+    const long long incl = wave_sum(q.tiles), excl = incl - q.tiles;
+    const long long all = before + lane_ll(incl, 63);
+    while (x < x1 && x < all * a.Hkv) {
+      // the request that x is in: the last one that begins at or before it
+      const int r = __builtin_amdgcn_readfirstlane(__popcll(__ballot((before + excl) * a.Hkv <= x)) - 1);
+      const int T = __builtin_amdgcn_readlane(q.tiles, r);
+      const long long first = (before + lane_ll(excl, r)) * a.Hkv;
       const int kvh = __builtin_amdgcn_readfirstlane((int)((x - first) / T));
       const int ta = __builtin_amdgcn_readfirstlane((int)(x - first - (long long)kvh * T));
       const int tb = __builtin_amdgcn_readfirstlane((int)min((long long)T, ta + (x1 - x)));
-      const int i = c * NT + r;
-      Req rq = req_of(i);
-      rq.s0 = __builtin_amdgcn_readfirstlane(rq.s0);
-      rq.add = __builtin_amdgcn_readfirstlane(rq.add);
-      rq.rows = __builtin_amdgcn_readfirstlane(rq.rows);
-      rq.kv = __builtin_amdgcn_readfirstlane(rq.kv);
-      item(i, rq, kvh, ta, tb, ta == 0 && tb == T, ta == 0);
-      if (ta == 0 && tb < T) {
-        noted = true;
-        if (tid == 0) {
-          meta[0] = i;
-          meta[1] = kvh;
-          meta[2] = (int)((first + (long long)(kvh + 1) * T - 1) / per);  // the workgroup that it ends in
-        }
+      item(i0 + r, __builtin_amdgcn_readlane(q.s0, r), __builtin_amdgcn_readlane(q.add, r),
+           __builtin_amdgcn_readlane(q.rows, r), __builtin_amdgcn_readlane(q.kv, r), kvh, ta, tb, ta == 0 && tb == T,
+           ta == 0);
+      if (ta == 0 && tb < T && lane == 0) {
+        meta[0] = i0 + r;
+        meta[1] = kvh;
+        meta[2] = (int)((first + (long long)(kvh + 1) * T - 1) / per);  // the wave that it ends in
       }
       x += tb - ta;
     }
+    before = all;
+    i0 += 64;
   }
-  if (!noted && tid == 0) meta[0] = -1;
 }
 
-// Joins the partials of the item that begins in workgroup w of k_exact_few and
-// runs on: slot 1 of w, slot 0 of w + 1 .. last.  Workgroup = one row of it, 32
-// threads (four dims each) for every eighth partial.
-__global__ __launch_bounds__(256) void k_exact_few_join(ExactArgs a, int rows) {
-  __shared__ float s_m[4];
-  __shared__ f32x4 s_o[8][32];
-  __shared__ float s_l[8][2];
-  const int tid = threadIdx.x, w = blockIdx.x / rows, r = blockIdx.x % rows;
-  const int i = a.few_meta[w * 4];
-  if (i < 0) return;
-  const int kvh = a.few_meta[w * 4 + 1], count = a.few_meta[w * 4 + 2] - w + 1;  // at most EX_FEW_WGS
-  const int c0 = min(max(a.cu[i], 0), a.total), c1 = min(max(a.cu[i + 1], 0), a.total);
-  if (r >= min(c1 - c0, a.max_add) * a.grp) return;
-  auto prow = [&](int k) { return ((size_t)(w + k) * 2 + (k == 0)) * EX_FEW + r; };
-  float mx = tid < count ? a.few_ml[prow(tid) * 3] : EX_NONE;
+// Joins the partials of the items that begin in waves 8 b .. 8 b + 7 of
+// k_exact_few and run on: slot 1 of that wave, slot 0 of the next ones.
+// Workgroup = those items' row blockIdx.x % rows, 32 threads (four dims each)
+// for every sixteenth partial.
+constexpr int FJ_W = 8;
+constexpr int FJ_G = 16;
+__global__ __launch_bounds__(FJ_G * 32) void k_exact_few_join(ExactArgs a, int waves) {
+  __shared__ float s_m[FJ_G / 2];
+  __shared__ f32x4 s_o[FJ_G][32];
+  __shared__ float s_l[FJ_G][2];
+  const int tid = threadIdx.x, w0 = blockIdx.x / a.few_rows * FJ_W, r = blockIdx.x % a.few_rows;
+  int begins[FJ_W];
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
-  if ((tid & 63) == 0) s_m[tid >> 6] = mx;
-  __syncthreads();
-  const float M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  const int g = tid >> 5, d4 = tid & 31;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float l1 = 0.f, l2 = 0.f;
+  for (int e = 0; e < FJ_W; ++e) begins[e] = w0 + e < waves ? a.few_meta[(w0 + e) * 4] : -1;
+#pragma unroll
+  for (int e = 0; e < FJ_W; ++e) {
+    const int i = begins[e], w = w0 + e;
+    if (i < 0) continue;  // uniform, as is what follows
+    const int kvh = a.few_meta[w * 4 + 1], count = a.few_meta[w * 4 + 2] - w + 1;
+    const int c0 = min(max(a.cu[i], 0), a.total), c1 = min(max(a.cu[i + 1], 0), a.total);
+    if (r >= min(c1 - c0, a.max_add) * a.grp) continue;
+    auto prow = [&](int k) { return ((size_t)(w + k) * 2 + (k == 0)) * a.few_rows + r; };
+    float M = EX_NONE;
+    for (int k = tid; k < count; k += FJ_G * 32) M = fmaxf(M, a.few_ml[prow(k) * 3]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) M = fmaxf(M, __shfl_xor(M, d, 64));
+    __syncthreads();  // s_o, s_l, s_m are free
+    if ((tid & 63) == 0) s_m[tid >> 6] = M;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < FJ_G / 2; ++k) M = fmaxf(M, s_m[k]);
+    const int g = tid >> 5, d4 = tid & 31;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l1 = 0.f, l2 = 0.f;
 #pragma unroll 4
-  for (int k = g; k < count; k += 8) {
-    const size_t pr = prow(k);
-    const float wgt = __builtin_amdgcn_exp2f(a.few_ml[pr * 3] - M);
-    l1 += wgt * a.few_ml[pr * 3 + 1];
-    l2 += wgt * a.few_ml[pr * 3 + 2];
-    o += wgt * reinterpret_cast<const f32x4*>(a.few_o + pr * D)[d4];
+    for (int k = g; k < count; k += FJ_G) {
+      const size_t pr = prow(k);
+      const float wgt = __builtin_amdgcn_exp2f(a.few_ml[pr * 3] - M);
+      l1 += wgt * a.few_ml[pr * 3 + 1];
+      l2 += wgt * a.few_ml[pr * 3 + 2];
+      o += wgt * reinterpret_cast<const f32x4*>(a.few_o + pr * D)[d4];
+    }
+    s_o[g][d4] = o;
+    if (d4 == 0) {
+      s_l[g][0] = l1;
+      s_l[g][1] = l2;
+    }
+    __syncthreads();
+    if (g != 0) continue;
+    for (int k = 1; k < FJ_G; ++k) {
+      o += s_o[k][d4];
+      l1 += s_l[k][0];
+      l2 += s_l[k][1];
+    }
+    const int tok = r / a.grp;
+    const size_t orow = (size_t)(c0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp);
+    const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
+    const Join j = join_of(l2 == 0.f ? -INFINITY : M + log2f(l2), a.pl, orow);
+    store4<0>(a, orow, d4 * 4, o * inv, j);
+    if (d4 == 0 && a.lse) a.lse[orow] = j.lse;
   }
-  s_o[g][d4] = o;
-  if (d4 == 0) {
-    s_l[g][0] = l1;
-    s_l[g][1] = l2;
-  }
-  __syncthreads();
-  if (g != 0) return;
-  for (int k = 1; k < 8; ++k) {
-    o += s_o[k][d4];
-    l1 += s_l[k][0];
-    l2 += s_l[k][1];
-  }
-  const int tok = r / a.grp;
-  const size_t orow = (size_t)(c0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp);
-  const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
-  const Join j = join_of(l2 == 0.f ? -INFINITY : M + log2f(l2), a.pl, orow);
-  store4<0>(a, orow, d4 * 4, o * inv, j);
-  if (d4 == 0 && a.lse) a.lse[orow] = j.lse;
 }
 
 }  // namespace
 
 hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t st) {
   if (a.few) {
-    hipLaunchKernelGGL(k_exact_few, dim3(a.few), dim3(FW_W * 64), 0, st, a);
-    const int rows = (int)std::min<long long>(EX_FEW, (long long)a.max_add * a.grp);
-    hipLaunchKernelGGL(k_exact_few_join, dim3(a.few * rows), dim3(256), 0, st, a, rows);
+    const int wgs = (a.few + FW_W - 1) / FW_W;
+    hipLaunchKernelGGL(k_exact_few, dim3(wgs), dim3(FW_W * 64), 0, st, a);
+    hipLaunchKernelGGL(k_exact_few_join, dim3((wgs * FW_W + FJ_W - 1) / FJ_W * a.few_rows), dim3(FJ_G * 32), 0, st, a,
+                       wgs * FW_W);
   }
   const unsigned items = (unsigned)a.Hkv * a.blocks * a.splits;
   if (items == 0) return hipGetLastError();
