@@ -83,14 +83,14 @@ protokv_status check_result(const Heads& h, int n, int total, const int32_t* cu,
 // Row blocks: sequence i has the indices floor(cu[i] grp / R) + i and on, which
 // leaves room for its ceil(rows / R) whatever cu is; how many of them there are
 // in all, and most context splits of one, chosen so that a launch has work for
-// the whole GPU (256 workgroups of 8 waves, or 2048 waves).
+// the whole GPU (two workgroups to a compute unit).
 void plan_blocks(ExactArgs& a, bool fp32, bool paged) {
   const int R = fp32 ? EX_ROWS_F32 : EX_ROWS;
   a.blocks = (int)((int64_t)a.total * a.grp / R) + a.n;
   a.splits = 1;
-  const int64_t items = (int64_t)a.blocks * a.Hkv, want = fp32 ? 2048 : 512;
+  const int64_t items = (int64_t)a.blocks * a.Hkv, want = 512;
   if (paged && items > 0 && items < want / 2) {
-    const int64_t tiles = ((int64_t)a.stride << a.shift) / 64;
+    const int64_t tiles = ((int64_t)a.stride << a.shift) / (fp32 ? 32 : 64);
     a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({EX_MAX_SPLITS, (want + items - 1) / items, tiles / EX_MIN_TILES}));
   }
 }

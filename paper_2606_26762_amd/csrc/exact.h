@@ -15,7 +15,7 @@ namespace pkv {
 std::string& call_error();
 
 constexpr int EX_ROWS = 256;      // query rows per workgroup of the bf16 kernel (8 waves of 32)
-constexpr int EX_ROWS_F32 = 32;   // query rows per wave of the float32 kernel
+constexpr int EX_ROWS_F32 = 32;   // query rows per workgroup of the float32 kernel
 constexpr int EX_MAX_SPLITS = 16;
 constexpr int EX_MIN_TILES = 8;   // 64-key (bf16) or 32-key (float32) tiles that a context split has at least
 constexpr int EX_FEW = 32;        // rows per kv head of a request that the few-rows kernel takes

@@ -449,10 +449,11 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   if (half == 0 && a.lse) a.lse[orow] = j.lse;
 }
 
-// float32: S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x2_f32.  One wave =
-// one work item (kv head, 32 query rows, context split), 32 keys per tile, four
-// independent waves per workgroup.  K and V go from global memory into the
-// operand registers; the query sits in LDS (each lane reads back what it wrote).
+// float32: S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x2_f32.  One workgroup =
+// one work item (kv head, 32 query rows, context split); its four waves take the
+// 32-key tiles in turn, each by itself, and merge at the end (one wave per item left
+// long rows to few SIMDs: prompts of 1001 tokens 268 us).  K and V go from global
+// memory into the operand registers; the query sits in LDS.
 //   K: lane (m = lane % 32, h = lane / 32) loads dims 8 j + 4 h .. + 3 of key m.
 //   P: register i of S^T holds key 8 (i / 4) + 4 h + i % 4 of query lane % 32.
 //   V: lane (m, h) loads dims 4 m .. 4 m + 3 of register i's key of its half; row
@@ -460,23 +461,23 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 // A dot product is the sum of eight 16-dim chains: its rounding error is that of
 // a pairwise sum.
 constexpr int EX_KEYS32 = 32;
+constexpr int EX_W32 = 4;
 
 template <int PAGED>
-__global__ __launch_bounds__(256, 2) void k_exact_f32(ExactArgs a) {
-  __shared__ f32x4 s_q[4][16][64];
+__global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
+  __shared__ __attribute__((aligned(16))) float s_part[EX_W32][66][64];  // the merge; before it the query
+  f32x4 (*s_q)[64] = reinterpret_cast<f32x4 (*)[64]>(&s_part[0][0][0]);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const long long item = (long long)blockIdx.x * 4 + wave;
-  if (item >= (long long)a.Hkv * a.blocks * a.splits) return;  // uniform, and nothing below synchronises waves
-  const int kvh = (int)(item % a.Hkv), rest = (int)(item / a.Hkv);
+  const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
   const int split = rest % a.splits, blk = a.blocks - 1 - rest / a.splits;
   Item it;
-  if (!find_item<EX_ROWS_F32>(a, blk, it)) return;
+  if (!find_item<EX_ROWS_F32>(a, blk, it)) return;  // uniform in the workgroup
   int per;
   const int tiles = (it.kend + EX_KEYS32 - 1) / EX_KEYS32;
   const int nsp = splits_of(a, tiles, per);
   if (split >= nsp) return;
-  const int t0 = split * per, t1 = min(tiles, t0 + per);
+  const int t0 = split * per + wave, t1 = min(tiles, split * per + per);
   const int m = lane & 31, half = lane >> 5;
   const int r = it.row0 + m;
   const bool rvalid = r < it.rows;
@@ -484,21 +485,22 @@ __global__ __launch_bounds__(256, 2) void k_exact_f32(ExactArgs a) {
   const int head = kvh * a.grp + (rvalid ? r - tok * a.grp : 0);
   const size_t orow = (size_t)(it.s0 + tok) * a.Hq + head;
   const int klim = rvalid ? it.off + tok : -1;
-  const int wtok0 = it.row0 / a.grp, wtok1 = (min(it.rows, it.row0 + 32) - 1) / a.grp;
-  const int wfull = it.off + wtok0 + 1;
+  const int wfull = it.off + it.row0 / a.grp + 1;
   {
     const f32x4* qr = reinterpret_cast<const f32x4*>((const uint8_t*)a.q + (size_t)(it.s0 + tok) * a.qs) + head * (D / 4);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) s_q[wave][j][lane] = qr[2 * j + half];
+    for (int j = 0; j < 4; ++j) s_q[4 * wave + j][lane] = qr[2 * (4 * wave + j) + half];
   }
+  __syncthreads();
   const uint8_t* kb = (const uint8_t*)a.k + (PAGED ? 0 : (size_t)it.s0 * a.ks + kvh * (D * 4));
   const uint8_t* vb = (const uint8_t*)a.v + (PAGED ? 0 : (size_t)it.s0 * a.vs + kvh * (D * 4));
-  // K and V rows of this lane's key of tile t (keys past the last repeat it)
-  auto resolve = [&](int t, const float*& kp, const float*& vp, bool& bad) {
-    const int key = min(t * EX_KEYS32 + m, it.kend - 1);
+  auto key_of = [&](int t) { return min(t * EX_KEYS32 + m, it.kend - 1); };  // keys past the last repeat it
+  auto id_of = [&](int t) { return PAGED ? a.table[(size_t)it.seq * a.stride + (key_of(t) >> a.shift)] : 0; };
+  // K and V rows of this lane's key of tile t, which is on page id
+  auto resolve = [&](int t, int id, const float*& kp, const float*& vp, bool& bad) {
+    const int key = key_of(t);
     bad = false;
     if constexpr (PAGED) {
-      const int id = a.table[(size_t)it.seq * a.stride + (key >> a.shift)];
       bad = (unsigned)id >= (unsigned)a.num_pages;
       const size_t page = bad ? 0 : id;
       const size_t e = ((((page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1)))) * (size_t)D;
@@ -537,7 +539,7 @@ __global__ __launch_bounds__(256, 2) void k_exact_f32(ExactArgs a) {
       f32x16 c = zero;
 #pragma unroll
       for (int j = 2 * g; j < 2 * g + 2; ++j) {
-        const f32x4 qv = s_q[wave][8 * h + j][lane];
+        const f32x4 qv = s_q[8 * h + j][lane];
 #pragma unroll
         for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(kr[j][e], qv[e], c, 0, 0, 0);
       }
@@ -555,12 +557,14 @@ __global__ __launch_bounds__(256, 2) void k_exact_f32(ExactArgs a) {
   f32x4 k0[8], k1[8], v0[8], v1[8];
   const float *kp = nullptr, *vp = nullptr;
   bool bad = false;
+  int id = 0;
   if (t0 < t1) {
-    resolve(t0, kp, vp, bad);
+    resolve(t0, id_of(t0), kp, vp, bad);
+    id = id_of(t0 + EX_W32);
     load_k(kp, 0, k0);
     load_k(kp, 1, k1);
   }
-  for (int t = t0; t < t1; ++t) {
+  for (int t = t0; t < t1; t += EX_W32) {
     load_v(vp, 0, v0);
     __builtin_amdgcn_sched_barrier(0);
     f32x16 s = dots(k0, 0);
@@ -579,8 +583,9 @@ __global__ __launch_bounds__(256, 2) void k_exact_f32(ExactArgs a) {
       }
     }
     // the next tile's keys load while this tile's values are used (past the
-    // last tile the loads repeat it)
-    resolve(min(t + 1, t1 - 1), kp, vp, bad);
+    // last key the loads repeat it)
+    resolve(t + EX_W32, id, kp, vp, bad);
+    id = id_of(t + 2 * EX_W32);
     load_k(kp, 0, k0);
     float tmax = -INFINITY;
 #pragma unroll
@@ -643,36 +648,114 @@ __global__ __launch_bounds__(256, 2) void k_exact_f32(ExactArgs a) {
     weigh(v1, s, 1, oacc);
   }
   lrun += xor32(lrun);
-  if (!rvalid) return;
-  // register i of oacc[0..3]: dims 4 mm .. 4 mm + 3 with mm = 8 (i / 4) + 4 half + i % 4
-  if (nsp > 1) {
-    const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * EX_ROWS_F32 + m;
+  // merge of the four waves, each relative to its own reference; wave w then holds
+  // registers 4 w .. 4 w + 3.  Register i of oacc[0..3]: dims 4 mm .. 4 mm + 3 with
+  // mm = 8 (i / 4) + 4 half + i % 4
+  __syncthreads();  // every wave is done with the query
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      reinterpret_cast<f32x4*>(a.part_o + pr * D)[8 * (i >> 2) + 4 * half + (i & 3)] =
-          (f32x4){oacc[0][i], oacc[1][i], oacc[2][i], oacc[3][i]};
-    if (half == 0) {
-      a.part_ml[pr * 3] = mrun;
-      a.part_ml[pr * 3 + 1] = lrun;
-      a.part_ml[pr * 3 + 2] = lrun;
-    }
-    return;
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s_part[wave][b * 16 + i][lane] = oacc[b][i];
+  s_part[wave][64][lane] = mrun;
+  s_part[wave][65][lane] = lrun;
+  __syncthreads();
+  float M = EX_NONE, L = 0.f, wgt[EX_W32];
+#pragma unroll
+  for (int w = 0; w < EX_W32; ++w) M = fmaxf(M, s_part[w][64][lane]);
+#pragma unroll
+  for (int w = 0; w < EX_W32; ++w) {
+    wgt[w] = __builtin_amdgcn_exp2f(s_part[w][64][lane] - M);
+    L += wgt[w] * s_part[w][65][lane];
   }
-  const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;
-  const Join j = join_of(lrun == 0.f ? -INFINITY : mrun + log2f(lrun), a.pl, orow);
+  const float inv = nsp > 1 ? 1.0f : L > 0.f || L != L ? 1.0f / L : 0.f;
+  Join j{1.f, 0.f, 0.f};
+  if (nsp == 1 && rvalid) j = join_of(L == 0.f ? -INFINITY : M + log2f(L), a.pl, orow);
+  const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * EX_ROWS_F32 + m;
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    store4<1>(a, orow, 4 * (8 * (i >> 2) + 4 * half + (i & 3)),
-              (f32x4){oacc[0][i] * inv, oacc[1][i] * inv, oacc[2][i] * inv, oacc[3][i] * inv}, j);
-  if (half == 0 && a.lse) a.lse[orow] = j.lse;
+  for (int e = 0; e < 4; ++e) {
+    const int i = 4 * wave + e, d = 4 * (8 * wave + 4 * half + e);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < EX_W32; ++w)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) o[b] += wgt[w] * s_part[w][b * 16 + i][lane];
+    if (nsp > 1) {
+      if (rvalid) *reinterpret_cast<f32x4*>(a.part_o + pr * D + d) = o;
+    } else if (rvalid) {
+      store4<1>(a, orow, d, o * inv, j);
+    }
+  }
+  __syncthreads();  // every wave has read the prior's lse, which may be lse itself
+  if (wave != 0 || half != 0 || !rvalid) return;
+  if (nsp > 1) {
+    a.part_ml[pr * 3] = M;
+    a.part_ml[pr * 3 + 1] = L;
+    a.part_ml[pr * 3 + 2] = L;
+  } else if (a.lse) {
+    a.lse[orow] = j.lse;
+  }
 }
 
-// Joins the splits of a row block: O = sum_s w_s O_s / sum_s w_s l_s with
-// w_s = 2^(m_s - max m).  Workgroup = 32 rows of one (kv head, row block), 32
-// threads per row, four dims each.
+// A row's partial results joined: O = sum_s w_s O_s, l likewise, with
+// w_s = 2^(m_s - max m); four dims to a thread.
+struct Sum {
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float M = EX_NONE, l1 = 0.f, l2 = 0.f;
+  __device__ __forceinline__ void add(float m, float x, float z, f32x4 v) {
+    const float top = fmaxf(M, m), p = __builtin_amdgcn_exp2f(M - top), q = __builtin_amdgcn_exp2f(m - top);
+    l1 = l1 * p + x * q;
+    l2 = l2 * p + z * q;
+    o = o * p + v * q;
+    M = top;
+  }
+  // partials k0, k0 + step, .. below count, eight at a time in flight; row(k): partial k's
+  template <typename F>
+  __device__ __forceinline__ void gather(const float* po, const float* ml, int k0, int step, int count, int d4, F row) {
+    for (; k0 < count; k0 += 8 * step) {
+      float m[8], x[8], z[8];
+      f32x4 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const size_t pr = row(min(k0 + u * step, count - 1));
+        m[u] = ml[pr * 3];
+        x[u] = ml[pr * 3 + 1];
+        z[u] = ml[pr * 3 + 2];
+        v[u] = reinterpret_cast<const f32x4*>(po + pr * D)[d4];
+      }
+      float top = M;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) top = fmaxf(top, m[u]);
+      const float back = __builtin_amdgcn_exp2f(M - top);
+      o *= back;
+      l1 *= back;
+      l2 *= back;
+      M = top;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (k0 + u * step < count) {
+          const float wgt = __builtin_amdgcn_exp2f(m[u] - M);
+          l1 += wgt * x[u];
+          l2 += wgt * z[u];
+          o += wgt * v[u];
+        }
+      }
+    }
+  }
+  template <int FP32>
+  __device__ __forceinline__ void store(const ExactArgs& a, size_t orow, int d4) const {
+    const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
+    const Join j = join_of(l2 == 0.f ? -INFINITY : M + log2f(l2), a.pl, orow);
+    store4<FP32>(a, orow, d4 * 4, o * inv, j);
+    if (d4 == 0 && a.lse) a.lse[orow] = j.lse;
+  }
+};
+
+// Joins the splits of a row block.  Workgroup = EJ_ROWS rows of one (kv head, row
+// block), 32 threads per row.
+constexpr int EJ_ROWS = 16;
 template <int FP32, int R>
-__global__ __launch_bounds__(256) void k_exact_join(ExactArgs a) {
-  const int part = blockIdx.x % (R / 32), rest = blockIdx.x / (R / 32);
+__global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
+  const int part = blockIdx.x % (R / EJ_ROWS), rest = blockIdx.x / (R / EJ_ROWS);
   const int kvh = rest % a.Hkv, blk = rest / a.Hkv;
   Item it;
   if (!find_item<R>(a, blk, it)) return;
@@ -681,27 +764,12 @@ __global__ __launch_bounds__(256) void k_exact_join(ExactArgs a) {
   const int nsp = splits_of(a, tiles, per);
   if (nsp == 1) return;  // written by the attention itself
   const size_t base = ((size_t)kvh * a.blocks + blk) * a.splits;
-  const int d = (threadIdx.x & 31) * 4;
-  for (int i = threadIdx.x >> 5; i < 32; i += 8) {
-    const int lr = part * 32 + i, r = it.row0 + lr;
-    if (r >= it.rows) return;
-    float M = EX_NONE, l1 = 0.f, l2 = 0.f;
-    for (int s = 0; s < nsp; ++s) M = fmaxf(M, a.part_ml[((base + s) * R + lr) * 3]);
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < nsp; ++s) {
-      const size_t pr = (base + s) * R + lr;
-      const float w = __builtin_amdgcn_exp2f(a.part_ml[pr * 3] - M);
-      l1 += w * a.part_ml[pr * 3 + 1];
-      l2 += w * a.part_ml[pr * 3 + 2];
-      o += w * *reinterpret_cast<const f32x4*>(a.part_o + pr * D + d);
-    }
-    const int tok = r / a.grp;
-    const size_t orow = (size_t)(it.s0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp);
-    const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
-    const Join j = join_of(l2 == 0.f ? -INFINITY : M + log2f(l2), a.pl, orow);
-    store4<FP32>(a, orow, d, o * inv, j);
-    if (d == 0 && a.lse) a.lse[orow] = j.lse;
-  }
+  const int lr = part * EJ_ROWS + (threadIdx.x >> 5), r = it.row0 + lr, d4 = threadIdx.x & 31;
+  if (r >= it.rows) return;
+  Sum s;
+  s.gather(a.part_o, a.part_ml, 0, 1, nsp, d4, [&](int k) { return (base + k) * R + lr; });
+  const int tok = r / a.grp;
+  s.store<FP32>(a, (size_t)(it.s0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp), d4);
 }
 
 // bf16, requests of at most 32 rows per kv head (single tokens of an answer).
@@ -765,7 +833,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   const long long per = max((N + waves - 1) / waves, (long long)EX_FEW_TILES);
   const long long x1 = min(N, (w + 1) * per);
   long long x = w * per;
-  if (lane == 0) meta[0] = -1;
+  if (lane == 0) meta[0] = 0;
   if (x >= N) return;  // uniform, and nothing below synchronises waves
   int i0;               // first request of the 64 in the lanes
   long long before;     // tiles before it
@@ -985,9 +1053,10 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
            __builtin_amdgcn_readlane(q.rows, r), __builtin_amdgcn_readlane(q.kv, r), kvh, ta, tb, ta == 0 && tb == T,
            ta == 0);
       if (ta == 0 && tb < T && lane == 0) {
-        meta[0] = i0 + r;
-        meta[1] = kvh;
-        meta[2] = (int)((first + (long long)(kvh + 1) * T - 1) / per);  // the wave that it ends in
+        // its rows, kv head, the wave that it ends in, its first row of q
+        *reinterpret_cast<int4*>(meta) = make_int4(__builtin_amdgcn_readlane(q.rows, r), kvh,
+                                                   (int)((first + (long long)(kvh + 1) * T - 1) / per),
+                                                   __builtin_amdgcn_readlane(q.s0, r));
       }
       x += tb - ta;
     }
@@ -997,65 +1066,57 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
 }
 
 // Joins the partials of the items that begin in waves 8 b .. 8 b + 7 of
-// k_exact_few and run on: slot 1 of that wave, slot 0 of the next ones.
-// Workgroup = those items' row blockIdx.x % rows, 32 threads (four dims each)
-// for every sixteenth partial.
+// k_exact_few and run on: slot 1 of that wave, slot 0 of the next ones.  Of an
+// item with few partials each wave takes a row by itself, 32 threads (four dims
+// each) for every other partial; of one with many the workgroup takes a row at a
+// time.  blockIdx.y deals the rows out to FJ_Y workgroups.  64 requests, 248 items
+// of 8 partials on average: 5 us; a workgroup per row for all items, one after the
+// other, 21.
 constexpr int FJ_W = 8;
-constexpr int FJ_G = 16;
-__global__ __launch_bounds__(FJ_G * 32) void k_exact_few_join(ExactArgs a, int waves) {
-  __shared__ float s_m[FJ_G / 2];
-  __shared__ f32x4 s_o[FJ_G][32];
-  __shared__ float s_l[FJ_G][2];
-  const int tid = threadIdx.x, w0 = blockIdx.x / a.few_rows * FJ_W, r = blockIdx.x % a.few_rows;
-  int begins[FJ_W];
+constexpr int FJ_Y = 4;
+constexpr int FJ_MANY = 48;
+__global__ __launch_bounds__(FJ_W * 64) void k_exact_few_join(ExactArgs a, int waves) {
+  __shared__ f32x4 s_o[FJ_W][32];
+  __shared__ float s_l[FJ_W][3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w0 = blockIdx.x * FJ_W, y = blockIdx.y, ny = gridDim.y;
+  const int g = lane >> 5, d4 = lane & 31;
+  int4 meta[FJ_W];
 #pragma unroll
-  for (int e = 0; e < FJ_W; ++e) begins[e] = w0 + e < waves ? a.few_meta[(w0 + e) * 4] : -1;
+  for (int e = 0; e < FJ_W; ++e)
+    meta[e] = w0 + e < waves ? reinterpret_cast<const int4*>(a.few_meta)[w0 + e] : make_int4(0, 0, 0, 0);
+  int at = 0;  // rows given out to the waves so far
 #pragma unroll
   for (int e = 0; e < FJ_W; ++e) {
-    const int i = begins[e], w = w0 + e;
-    if (i < 0) continue;  // uniform, as is what follows
-    const int kvh = a.few_meta[w * 4 + 1], count = a.few_meta[w * 4 + 2] - w + 1;
-    const int c0 = min(max(a.cu[i], 0), a.total), c1 = min(max(a.cu[i + 1], 0), a.total);
-    if (r >= min(c1 - c0, a.max_add) * a.grp) continue;
-    auto prow = [&](int k) { return ((size_t)(w + k) * 2 + (k == 0)) * a.few_rows + r; };
-    float M = EX_NONE;
-    for (int k = tid; k < count; k += FJ_G * 32) M = fmaxf(M, a.few_ml[prow(k) * 3]);
+    const int rows = meta[e].x, kvh = meta[e].y, w = w0 + e, count = meta[e].z - w + 1, s0 = meta[e].w;
+    const bool many = count > FJ_MANY;
+    for (int r = y; r < rows; r += ny) {  // uniform
+      if (!many && (at++ & (FJ_W - 1)) != wave) continue;
+      Sum s;
+      s.gather(a.few_o, a.few_ml, many ? wave * 2 + g : g, many ? 2 * FJ_W : 2, count, d4,
+               [&](int k) { return ((size_t)(w + k) * 2 + (k == 0)) * a.few_rows + r; });
+      {
+        f32x4 v;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) M = fmaxf(M, __shfl_xor(M, d, 64));
-    __syncthreads();  // s_o, s_l, s_m are free
-    if ((tid & 63) == 0) s_m[tid >> 6] = M;
-    __syncthreads();
+        for (int c = 0; c < 4; ++c) v[c] = xor32(s.o[c]);
+        s.add(xor32(s.M), xor32(s.l1), xor32(s.l2), v);
+      }
+      if (many) {
+        __syncthreads();  // s_o and s_l are free
+        if (g == 0) s_o[wave][d4] = s.o;
+        if (lane == 0) {
+          s_l[wave][0] = s.M;
+          s_l[wave][1] = s.l1;
+          s_l[wave][2] = s.l2;
+        }
+        __syncthreads();
+        if (wave != 0) continue;
 #pragma unroll
-    for (int k = 0; k < FJ_G / 2; ++k) M = fmaxf(M, s_m[k]);
-    const int g = tid >> 5, d4 = tid & 31;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float l1 = 0.f, l2 = 0.f;
-#pragma unroll 4
-    for (int k = g; k < count; k += FJ_G) {
-      const size_t pr = prow(k);
-      const float wgt = __builtin_amdgcn_exp2f(a.few_ml[pr * 3] - M);
-      l1 += wgt * a.few_ml[pr * 3 + 1];
-      l2 += wgt * a.few_ml[pr * 3 + 2];
-      o += wgt * reinterpret_cast<const f32x4*>(a.few_o + pr * D)[d4];
+        for (int k = 1; k < FJ_W; ++k) s.add(s_l[k][0], s_l[k][1], s_l[k][2], s_o[k][d4]);
+      }
+      const int tok = r / a.grp;
+      if (g == 0) s.store<0>(a, (size_t)(s0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp), d4);
     }
-    s_o[g][d4] = o;
-    if (d4 == 0) {
-      s_l[g][0] = l1;
-      s_l[g][1] = l2;
-    }
-    __syncthreads();
-    if (g != 0) continue;
-    for (int k = 1; k < FJ_G; ++k) {
-      o += s_o[k][d4];
-      l1 += s_l[k][0];
-      l2 += s_l[k][1];
-    }
-    const int tok = r / a.grp;
-    const size_t orow = (size_t)(c0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp);
-    const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
-    const Join j = join_of(l2 == 0.f ? -INFINITY : M + log2f(l2), a.pl, orow);
-    store4<0>(a, orow, d4 * 4, o * inv, j);
-    if (d4 == 0 && a.lse) a.lse[orow] = j.lse;
   }
 }
 
@@ -1065,21 +1126,21 @@ hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t s
   if (a.few) {
     const int wgs = (a.few + FW_W - 1) / FW_W;
     hipLaunchKernelGGL(k_exact_few, dim3(wgs), dim3(FW_W * 64), 0, st, a);
-    hipLaunchKernelGGL(k_exact_few_join, dim3((wgs * FW_W + FJ_W - 1) / FJ_W * a.few_rows), dim3(FJ_G * 32), 0, st, a,
-                       wgs * FW_W);
+    hipLaunchKernelGGL(k_exact_few_join, dim3((wgs * FW_W + FJ_W - 1) / FJ_W, std::min(FJ_Y, a.few_rows)), dim3(FJ_W * 64),
+                       0, st, a, wgs * FW_W);
   }
   const unsigned items = (unsigned)a.Hkv * a.blocks * a.splits;
   if (items == 0) return hipGetLastError();
   if (fp32) {
-    if (paged) hipLaunchKernelGGL((k_exact_f32<1>), dim3((items + 3) / 4), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_exact_f32<0>), dim3((items + 3) / 4), dim3(256), 0, st, a);
+    if (paged) hipLaunchKernelGGL((k_exact_f32<1>), dim3(items), dim3(EX_W32 * 64), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_f32<0>), dim3(items), dim3(EX_W32 * 64), 0, st, a);
   } else {
     if (paged) hipLaunchKernelGGL((k_exact_bf16<1>), dim3(items), dim3(512), 0, st, a);
     else hipLaunchKernelGGL((k_exact_bf16<0>), dim3(items), dim3(512), 0, st, a);
   }
   if (a.splits > 1) {
-    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), dim3(a.Hkv * a.blocks), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), dim3(a.Hkv * a.blocks * (EX_ROWS / 32)), dim3(256), 0, st, a);
+    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), dim3(a.Hkv * a.blocks * (EX_ROWS_F32 / EJ_ROWS)), dim3(EJ_ROWS * 32), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), dim3(a.Hkv * a.blocks * (EX_ROWS / EJ_ROWS)), dim3(EJ_ROWS * 32), 0, st, a);
   }
   return hipGetLastError();
 }
