@@ -23,6 +23,7 @@ typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef short v8i16 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+typedef __attribute__((address_space(3))) const u16x8 lds_u16x8;
 typedef __attribute__((address_space(1))) const f32x4 gbl_f32x4;
 
 namespace {
@@ -182,20 +183,21 @@ constexpr int EX_TILE = EX_KEYS * D * 2;  // one K or V tile, 16 KB
 constexpr int EX_NBUF = 4;              // tile t computes while t + 1 .. t + 3 load
 constexpr int EX_IDS = 2048;            // page ids staged at a time
 
-// Workgroup = eight waves of 32 query rows each.  A tile of 64 keys sits in LDS
-// in two layouts under which every operand read is a per-lane base plus
-// compile-time offsets on distinct banks:
-//   K chunk-major: 16-byte chunk c (dims 8 c .. + 7) of row r at c * 1024 + r * 16;
-//   V by 32-dim block: dims 32 b .. + 31 of row r at b * 4096 + r * 64.
-// Tiles go straight from global memory into them (global_load_lds_dwordx4),
-// three tiles ahead.  S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x16_bf16,
+// Workgroup = eight waves of 32 query rows each.  Tiles of 64 keys go straight from
+// global memory into LDS (global_load_lds_dwordx4), two tiles ahead, four whole rows
+// to an instruction (16 bytes of 64 rows each, or 64 of 16, kept the address unit
+// busy for most of a tile's time).  Row r lies at r * 256 with its 16-byte chunks
+// permuted, chunk c of K at place c ^ (r % 16), of V at c ^ 4 (r % 4), so that the
+// operand reads (16 rows of one chunk; 4 rows of 4 chunks) fall on distinct banks.
+// S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x16_bf16,
 // V^T through ds_read_b64_tr_b16: each lane holds one query column, so the
 // softmax is lane-local plus one exchange with the partner lane.
 template <int PAGED>
 __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t s_kv[EX_NBUF][2][EX_TILE];
+  __shared__ __attribute__((aligned(256))) uint8_t s_kv[EX_NBUF][2][EX_TILE];
   __shared__ int32_t s_ids[PAGED ? EX_IDS : 1];
   __shared__ unsigned long long s_bad[8];  // keys of a tile on pages that are none
+  __shared__ __attribute__((aligned(256))) uint8_t s_zero[EX_TILE];  // V of a tile whose products are done already
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // kv heads innermost: workgroups are dealt round robin to the 8 XCDs, so a
@@ -248,55 +250,118 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     const size_t page = bad ? 0 : id;
     return ((((page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1)))) * (size_t)(D * 2);
   };
+  // this lane's part of the rows 4 wave + lane / 16 and + 32 of a tile
+  const int ckey = ((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)) * 16;
+  const int cval = ((lane & 15) ^ ((lane >> 4) << 2)) * 16;
   auto issue = [&](int t) {
     const int buf = t % EX_NBUF;
-    // keys past the last one repeat it (they are masked)
-    const int key_k = min(t * EX_KEYS + lane, it.kend - 1);
-    const int key_v = min(t * EX_KEYS + (wave & 3) * 16 + (lane >> 2), it.kend - 1);
-    const uint8_t *rk, *rv;
-    if constexpr (PAGED) {
-      bool bad, bad2;
-      rk = kb + paged_row(key_k, bad);
-      rv = vb + paged_row(key_v, bad2);
-      const unsigned long long bm = __ballot(bad);
-      if (wave == 0 && lane == 0) s_bad[t & 7] = bm;
-    } else {
-      rk = kb + (size_t)key_k * a.ks;
-      rv = vb + (size_t)key_v * a.vs;
-    }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const int i = wave + 8 * q;  // chunk of K; 32-dim block i / 4 of V, rows 16 (i % 4) .. + 15
-      lds_dma16(rk + i * 16, s_kv[buf][0] + i * 1024);
-      lds_dma16(rv + (i >> 2) * 64 + (lane & 3) * 16, s_kv[buf][1] + i * 1024);
+      // keys past the last one repeat it (they are masked)
+      const int key = min(t * EX_KEYS + 32 * q + 4 * wave + (lane >> 4), it.kend - 1);
+      const uint8_t *rk, *rv;
+      if constexpr (PAGED) {
+        bool bad;
+        const size_t at = paged_row(key, bad);
+        rk = kb + at;
+        rv = vb + at;
+      } else {
+        rk = kb + (size_t)key * a.ks;
+        rv = vb + (size_t)key * a.vs;
+      }
+      lds_dma16(rk + ckey, s_kv[buf][0] + (wave + 8 * q) * 1024);
+      lds_dma16(rv + cval, s_kv[buf][1] + (wave + 8 * q) * 1024);
+    }
+    if constexpr (PAGED) {
+      if (wave == 0) {
+        bool bad;
+        paged_row(min(t * EX_KEYS + lane, it.kend - 1), bad);
+        const unsigned long long bm = __ballot(bad);
+        if (lane == 0) s_bad[t & 7] = bm;
+      }
     }
   };
   const int grp16 = lane >> 4, s16 = lane & 15;
   const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
-  auto compute_tile = [&](int t, auto masked) {
-    constexpr bool MASK = decltype(masked)::value;
-    const uint8_t* kl = s_kv[t % EX_NBUF][0] + m * 16 + half * 1024;
-    const uint8_t* vl = s_kv[t % EX_NBUF][1] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
-    f32x16 s[2] = {zero, zero};
+  // One tile's work in two halves: products are the matrix ones (the last tile's
+  // P V, then this tile's K Q), weights() the softmax between them.
+  f32x16 s[2];
+  bf16x8 pb[4];
+  auto key_base = [&](int t) {
+    return (uint32_t)(uintptr_t)(lds_u16x8*)s_kv[t % EX_NBUF][0] + (m * 256 + ((m & 15) ^ half) * 16);
+  };
+  // K operand of key half h, 16-dim step kk: chunk 2 kk + half of key 32 h + m
+  auto read_k = [&](uint32_t kl, int h, int kk) {
+    return __builtin_bit_cast(bf16x8, *((lds_u16x8*)(uintptr_t)(kl ^ (kk * 32)) + h * 512));
+  };
+  // V^T operand of 32-dim block b, 16-key step st: positions half * 8 + i are
+  // keys 16 st + 4 half + {0..3} (i < 4) and + 8 (i >= 4), as P's registers are.
+  // Source lane i of 16 reads key i / 4 of its four, dims 4 (i % 4) .. + 3.
+  auto value_base = [&](const uint8_t* tile) {
+    return (uint32_t)(uintptr_t)(lds_v4i16*)tile + (4 * half + (s16 >> 2)) * 256 +
+           (((grp16 & 1) * 2 + ((s16 & 3) >> 1)) ^ ((s16 >> 2) << 2)) * 16 + (s16 & 1) * 8;
+  };
+  auto read_v = [&](uint32_t vl, int b, int st) {
+    lds_v4i16* p = (lds_v4i16*)(uintptr_t)(vl ^ (b * 64)) + st * 512;
+    const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
+    const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p + 256);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // Eight steps of four products, V's (O of tile tv) and K's (S of tile tk), the
+  // operands of each step read while the one before it is multiplied.
+  bool done = false;  // the last tile's P V is
+  auto products = [&](int tv, int tk, auto with_v, auto with_k) {
+    constexpr int F = decltype(with_v)::value ? 0 : 4, L = decltype(with_k)::value ? 8 : 4;
+    const uint32_t vl = value_base(done ? s_zero : s_kv[tv % EX_NBUF][1]), kl = key_base(tk);
+    bf16x8 op[2][4];
+    auto read = [&](int step) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int j = 0; j < 4; ++j)
+        op[step & 1][j] = step < 4 ? __builtin_bit_cast(bf16x8, read_v(vl, j, step)) : read_k(kl, j & 1, 2 * (step - 4) + (j >> 1));
+    };
+    read(F);
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        const bf16x8 ak = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u16x8*>(kl + kk * 2048 + h * 512));
-        s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak, bq[kk], s[h], 0, 0, 0);
+    for (int step = F; step < L; ++step) {
+      if (step + 1 < L) read(step + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (step < 4) {
+          oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], pb[step], oacc[j], 0, 0, 0);
+        } else {
+          const int kk = 2 * (step - 4) + (j >> 1);
+          s[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], bq[kk], kk ? s[j & 1] : zero, 0, 0, 0);
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // Softmax weights of tile t; true if its P V is done as well: hidden keys with
+  // infinite or NaN values.
+  auto weights = [&](int t) {
+    bool hidden = (t + 1) * EX_KEYS > wfull;
     unsigned long long bad = 0;
-    const int rel = klim - t * EX_KEYS - 4 * half;
-    if constexpr (MASK) {
-      if constexpr (PAGED) bad = s_bad[t & 7] >> (4 * half);
+    if constexpr (PAGED) {
+      bad = s_bad[t & 7];
+      hidden |= __builtin_amdgcn_readfirstlane((int)(bad != 0)) != 0;
+      bad >>= 4 * half;
+    }
+    if (hidden) {  // uniform
+      const int rel = klim - t * EX_KEYS - 4 * half;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int c = 32 * h + 8 * (i >> 2) + (i & 3);  // key c + 4 half of the tile
-          const bool hidden = c > rel || (PAGED && ((bad >> c) & 1));
-          s[h][i] = hidden ? -INFINITY : s[h][i];
+        for (int i = 0; i < 16; ++i)  // key 32 h + 8 (i / 4) + i % 4 + 4 half of the tile
+          s[h][i] = 32 * h + 8 * (i >> 2) + (i & 3) > rel ? -INFINITY : s[h][i];
+      if constexpr (PAGED) {
+        if (__ballot(bad != 0)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              s[h][i] = (bad >> (32 * h + 8 * (i >> 2) + (i & 3))) & 1 ? -INFINITY : s[h][i];
         }
+      }
     }
     float tmax = -INFINITY;
 #pragma unroll
@@ -316,7 +381,6 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
       for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
       mref = mnew;
     }
-    bf16x8 pb[4];
     float part[2] = {0.f, 0.f}, sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -335,57 +399,51 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     }
     l1 += sum0 + sum1;   // this half's keys; the halves meet at the end
     l2 += part[0] + part[1];
-    // V^T operand of 32-dim block b, 16-key step st: positions half * 8 + i are
-    // keys 16 st + 4 half + {0..3} (i < 4) and + 8 (i >= 4), as P's registers are
-    auto read_v = [&](int b, int st, int z = 0) {
-      const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + z + b * 4096 + st * 1024));
-      const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + z + b * 4096 + st * 1024 + 512));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    if constexpr (MASK) {
-      uint32_t odd = 0;
+    if (!hidden) return false;  // uniform
+    const uint32_t vl = value_base(s_kv[t % EX_NBUF][1]);
+    uint32_t odd = 0;
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < 4; ++b) {
 #pragma unroll
-        for (int st = 0; st < 4; ++st) {
-          const v8i16 v = read_v(b, st);
-          odd |= odd_flags(v);
-          oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<0>(v), pb[st], oacc[b], 0, 0, 0);
-        }
-      if (__ballot((odd & ODD) != 0)) {  // uniform
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          f32x16 hits = zero;
-          int z = anew();
-#pragma unroll
-          for (int st = 0; st < 4; ++st)
-            hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<1>(read_v(b, st, z)), pb[st], hits, 0, 0, 0);
-          add_odd<1>(oacc[b], hits);
-          __builtin_amdgcn_sched_barrier(0);
-          hits = zero;
-          z = anew();
-#pragma unroll
-          for (int st = 0; st < 4; ++st)
-            hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<-1>(read_v(b, st, z)), pb[st], hits, 0, 0, 0);
-          add_odd<-1>(oacc[b], hits);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int st = 0; st < 4; ++st)
-          oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, read_v(b, st)), pb[st], oacc[b], 0, 0, 0);
+      for (int st = 0; st < 4; ++st) odd |= odd_flags(read_v(vl, b, st));
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if (!__ballot((odd & ODD) != 0)) return false;  // uniform
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      f32x16 hits = zero;
+      uint32_t vz = vl + anew();
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<0>(read_v(vz, b, st)), pb[st], hits, 0, 0, 0);
+      oacc[b] += hits;
+      __builtin_amdgcn_sched_barrier(0);
+      hits = zero;
+      vz = vl + anew();
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<1>(read_v(vz, b, st)), pb[st], hits, 0, 0, 0);
+      add_odd<1>(oacc[b], hits);
+      __builtin_amdgcn_sched_barrier(0);
+      hits = zero;
+      vz = vl + anew();
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<-1>(read_v(vz, b, st)), pb[st], hits, 0, 0, 0);
+      add_odd<-1>(oacc[b], hits);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return true;
   };
 
   if constexpr (PAGED) {
     if (t0 < t1) load_ids(t0);
   }
+#pragma unroll
+  for (int i = 0; i < EX_TILE / 8192; ++i) reinterpret_cast<uint4*>(s_zero)[tid + i * 512] = make_uint4(0, 0, 0, 0);
   wait_vm<0>();  // the query operands are in registers before any tile is in flight
   ex_barrier();
-  for (int t = t0; t < t0 + 3 && t < t1; ++t) {
+  for (int t = t0; t < t0 + 2 && t < t1; ++t) {
     if constexpr (PAGED) {
       if (t > t0 && t % tpc == 0) {  // uniform
         ex_barrier();
@@ -395,27 +453,67 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     }
     issue(t);
   }
-  for (int t = t0; t < t1; ++t) {
-    // this wave's loads of tile t have landed; those of t + 1, t + 2 may be in flight
-    if (t + 2 < t1) wait_vm<8>();
-    else if (t + 1 < t1) wait_vm<4>();
+  // Waves w and w + 4 share a SIMD.  Waves 0 - 3 form the products of tile t in phase
+  // 2 t and its weights in phase 2 t + 1, waves 4 - 7 one phase later, so that in
+  // every phase one wave of a SIMD has the matrix core and the other the VALU (in
+  // step, both wait for the one and then for the other: 852 TFLOP/s over 8192 keys).
+  // A barrier begins each phase.  Tile t + 2 is issued at phase 2 t, where V of tile
+  // t - 2, last read in phase 2 t - 1, has left its buffer, and has landed by 2 t + 4.
+  auto even = [&](int t) {  // the barrier before phase 2 t
+    __builtin_amdgcn_sched_barrier(0);
+    if (t + 1 < t1) wait_vm<4>();  // this wave's loads of tile t have landed, those of t + 1 may be in flight
     else wait_vm<0>();
     ex_barrier();
-    // buffer (t + 3) % 4 held tile t - 1, finished by every wave before this barrier
-    if (t + 3 < t1) {
+    if (t + 2 < t1) {
       if constexpr (PAGED) {
-        if ((t + 3) % tpc == 0) {  // uniform
-          load_ids(t + 3);
+        if ((t + 2) % tpc == 0) {  // uniform
+          load_ids(t + 2);
           ex_barrier();
         }
       }
-      issue(t + 3);
+      issue(t + 2);
     }
-    if (!wvalid || t * EX_KEYS >= wend) continue;  // uniform: nothing of the tile is seen
-    bool mask = (t + 1) * EX_KEYS > wfull;
-    if constexpr (PAGED) mask |= __builtin_amdgcn_readfirstlane((int)(s_bad[t & 7] != 0));
-    if (mask) compute_tile(t, std::true_type{});
-    else compute_tile(t, std::false_type{});
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto odd_phase = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    ex_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // the tiles of which this wave's rows see something are t0 .. tw - 1
+  const int tw = wvalid ? max(t0, min(t1, (wend + EX_KEYS - 1) / EX_KEYS)) : t0;
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  const bool late = wave >= 4;  // uniform
+  auto first_barrier = [&](int t) {
+    if (late) odd_phase();
+    else even(t);
+  };
+  auto second_barrier = [&](int t) {
+    if (!late) odd_phase();
+    else if (t < t1) even(t + 1);
+  };
+  if (late) even(t0);
+  int t = t0;
+  if (t < tw) {
+    first_barrier(t);
+    products(t, t, no, yes);
+    second_barrier(t);
+    done = weights(t);
+    for (++t; t < tw; ++t) {
+      first_barrier(t);
+      products(t - 1, t, yes, yes);
+      second_barrier(t);
+      done = weights(t);
+    }
+    first_barrier(t);
+    products(t - 1, t, yes, no);
+    second_barrier(t);
+    ++t;
+  }
+  for (; t <= t1; ++t) {
+    first_barrier(t);
+    second_barrier(t);
   }
   if (!wvalid) return;
   l1 += xor32(l1);
