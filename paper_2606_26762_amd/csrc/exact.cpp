@@ -106,13 +106,13 @@ size_t lay_out(ExactArgs& a, bool fp32, uint8_t* base) {
   if (a.few) {
     const size_t rows = (size_t)a.few * 2 * a.few_rows;
     a.few_o = (float*)take(rows * D * 4);
-    a.few_ml = (float*)take(rows * 3 * 4);
+    a.few_ml = (float*)take(rows * 2 * 4);
     a.few_meta = (int32_t*)take((size_t)a.few * 4 * 4);
   }
   if (a.splits > 1) {
     const size_t rows = (size_t)a.Hkv * a.blocks * a.splits * (fp32 ? EX_ROWS_F32 : EX_ROWS);
     a.part_o = (float*)take(rows * D * 4);
-    a.part_ml = (float*)take(rows * 3 * 4);
+    a.part_ml = (float*)take(rows * 2 * 4);
   }
   return off;
 }

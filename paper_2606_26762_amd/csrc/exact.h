@@ -33,12 +33,12 @@ struct ExactArgs {
   const void* po;         // prior, or null
   const float* pl;
   const int32_t *cu, *kv_len, *table;
-  float *part_o, *part_ml;  // [kv head][row block][split][row][D] and [..][3]: m, l of the rounded weights, l
+  float *part_o, *part_ml;  // [kv head][row block][split][row][D] and [..][2]: m, l
   long long qs, ks, vs;     // bytes between rows
   int n, total, max_add;
   int Hq, Hkv, grp;
   int stride, shift, num_pages;  // block table row, log2 page size
-  // few-rows kernel: two partials per wave [wave][2][few_rows][D], [..][3], and the
+  // few-rows kernel: two partials per wave [wave][2][few_rows][D], [..][2], and the
   // split item that begins in a wave (see k_exact_few)
   float *few_o, *few_ml;
   int32_t* few_meta;

@@ -231,9 +231,9 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   }
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   f32x16 oacc[4] = {zero, zero, zero, zero};
-  // l1: sum of the weights as rounded for the PV product (normalises o: a row with
-  // one key returns its value exactly); l2: of the unrounded ones (for lse)
-  float mref = EX_NONE, l1 = 0.f, l2 = 0.f;
+  // (a row's first reference is its first tile's maximum, so a row with one key
+  // has weight 1 on it and returns its value exactly)
+  float mref = EX_NONE, lrun = 0.f;
 
   const uint8_t* kb = (const uint8_t*)a.k + (PAGED ? 0 : (size_t)it.s0 * a.ks + kvh * (D * 2));
   const uint8_t* vb = (const uint8_t*)a.v + (PAGED ? 0 : (size_t)it.s0 * a.vs + kvh * (D * 2));
@@ -253,8 +253,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   // this lane's part of the rows 4 wave + lane / 16 and + 32 of a tile
   const int ckey = ((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)) * 16;
   const int cval = ((lane & 15) ^ ((lane >> 4) << 2)) * 16;
-  auto issue = [&](int t) {
-    const int buf = t % EX_NBUF;
+  const uint8_t *next_k[2], *next_v[2];  // where the parts of the tile to be loaded next lie
+  auto locate = [&](int t) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       // keys past the last one repeat it (they are masked)
@@ -269,8 +269,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
         rk = kb + (size_t)key * a.ks;
         rv = vb + (size_t)key * a.vs;
       }
-      lds_dma16(rk + ckey, s_kv[buf][0] + (wave + 8 * q) * 1024);
-      lds_dma16(rv + cval, s_kv[buf][1] + (wave + 8 * q) * 1024);
+      next_k[q] = rk + ckey;
+      next_v[q] = rv + cval;
     }
     if constexpr (PAGED) {
       if (wave == 0) {
@@ -281,8 +281,17 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
       }
     }
   };
+  auto load = [&](int t, int part) {  // one of the four instructions that load tile t
+    const int q = part >> 1;
+    if (part & 1) lds_dma16(next_v[q], s_kv[t % EX_NBUF][1] + (wave + 8 * q) * 1024);
+    else lds_dma16(next_k[q], s_kv[t % EX_NBUF][0] + (wave + 8 * q) * 1024);
+  };
+  auto issue = [&](int t) {
+    locate(t);
+#pragma unroll
+    for (int part = 0; part < 4; ++part) load(t, part);
+  };
   const int grp16 = lane >> 4, s16 = lane & 15;
-  const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
   // One tile's work in two halves: products are the matrix ones (the last tile's
   // P V, then this tile's K Q), weights() the softmax between them.
   f32x16 s[2];
@@ -309,8 +318,10 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   };
   // Eight steps of four products, V's (O of tile tv) and K's (S of tile tk), the
   // operands of each step read while the one before it is multiplied.
+  // Tile tk + 2's four loads go out between the steps.
   bool done = false;  // the last tile's P V is
   auto products = [&](int tv, int tk, auto with_v, auto with_k) {
+    const bool more = tk + 2 < t1;  // uniform
     constexpr int F = decltype(with_v)::value ? 0 : 4, L = decltype(with_k)::value ? 8 : 4;
     const uint32_t vl = value_base(done ? s_zero : s_kv[tv % EX_NBUF][1]), kl = key_base(tk);
     bf16x8 op[2][4];
@@ -323,6 +334,13 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 #pragma unroll
     for (int step = F; step < L; ++step) {
       if (step + 1 < L) read(step + 1);
+      if (more) {
+        if (L - F == 8) {
+          if (step & 1) load(tk + 2, step >> 1);
+        } else {
+          load(tk + 2, step & 3);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -375,30 +393,21 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     if (__ballot(grow)) {  // uniform
       const float mnew = grow ? tmax : mref;
       const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
-      l1 *= alpha;
-      l2 *= alpha;
+      lrun *= alpha;
 #pragma unroll
       for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
       mref = mnew;
     }
-    float part[2] = {0.f, 0.f}, sum0 = 0.f, sum1 = 0.f;
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float p = __builtin_amdgcn_exp2f(fmaf(s[h][i], EX_SCALE, -mref));
-        part[i & 1] += p;
+        part[i & 3] += p;
         pb[2 * h + (i >> 3)][i & 7] = (__bf16)p;
       }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      sum0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 0, 1), ones2, sum0, false);
-      sum1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 2, 3), ones2, sum1, false);
-      sum0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 4, 5), ones2, sum0, false);
-      sum1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 6, 7), ones2, sum1, false);
-    }
-    l1 += sum0 + sum1;   // this half's keys; the halves meet at the end
-    l2 += part[0] + part[1];
+    lrun += (part[0] + part[1]) + (part[2] + part[3]);  // this half's keys; the halves meet at the end
     if (!hidden) return false;  // uniform
     const uint32_t vl = value_base(s_kv[t % EX_NBUF][1]);
     uint32_t odd = 0;
@@ -436,48 +445,43 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     return true;
   };
 
-  if constexpr (PAGED) {
-    if (t0 < t1) load_ids(t0);
-  }
 #pragma unroll
   for (int i = 0; i < EX_TILE / 8192; ++i) reinterpret_cast<uint4*>(s_zero)[tid + i * 512] = make_uint4(0, 0, 0, 0);
   wait_vm<0>();  // the query operands are in registers before any tile is in flight
-  ex_barrier();
-  for (int t = t0; t < t0 + 2 && t < t1; ++t) {
+  for (int t = t0; t < t0 + 3 && t < t1; ++t) {
     if constexpr (PAGED) {
-      if (t > t0 && t % tpc == 0) {  // uniform
+      if (t == t0 || t % tpc == 0) {  // uniform
         ex_barrier();
         load_ids(t);
         ex_barrier();
       }
     }
-    issue(t);
+    if (t < t0 + 2) issue(t);
+    else locate(t);
   }
   // Waves w and w + 4 share a SIMD.  Waves 0 - 3 form the products of tile t in phase
   // 2 t and its weights in phase 2 t + 1, waves 4 - 7 one phase later, so that in
   // every phase one wave of a SIMD has the matrix core and the other the VALU (in
-  // step, both wait for the one and then for the other: 852 TFLOP/s over 8192 keys).
-  // A barrier begins each phase.  Tile t + 2 is issued at phase 2 t, where V of tile
-  // t - 2, last read in phase 2 t - 1, has left its buffer, and has landed by 2 t + 4.
+  // step, both wait for the one and then for the other).  A barrier begins each phase.
+  // Tile t + 2 is loaded beside the products of tile t, from phase 2 t on, where V of
+  // tile t - 2, last read in phase 2 t - 1, has left its buffer, and has landed by
+  // phase 2 t + 4; its rows are located after the weights of tile t - 1.
   auto even = [&](int t) {  // the barrier before phase 2 t
     __builtin_amdgcn_sched_barrier(0);
     if (t + 1 < t1) wait_vm<4>();  // this wave's loads of tile t have landed, those of t + 1 may be in flight
     else wait_vm<0>();
     ex_barrier();
-    if (t + 2 < t1) {
-      if constexpr (PAGED) {
-        if ((t + 2) % tpc == 0) {  // uniform
-          load_ids(t + 2);
-          ex_barrier();
-        }
-      }
-      issue(t + 2);
-    }
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto odd_phase = [&]() {
+  auto odd_phase = [&](int t) {  // the barrier before phase 2 t + 1
     __builtin_amdgcn_sched_barrier(0);
     ex_barrier();
+    if constexpr (PAGED) {
+      if (t + 3 < t1 && (t + 3) % tpc == 0) {  // uniform
+        load_ids(t + 3);
+        ex_barrier();
+      }
+    }
     __builtin_amdgcn_sched_barrier(0);
   };
   // the tiles of which this wave's rows see something are t0 .. tw - 1
@@ -486,12 +490,15 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   constexpr std::false_type no{};
   const bool late = wave >= 4;  // uniform
   auto first_barrier = [&](int t) {
-    if (late) odd_phase();
+    if (late) odd_phase(t);
     else even(t);
   };
   auto second_barrier = [&](int t) {
-    if (!late) odd_phase();
+    if (!late) odd_phase(t);
     else if (t < t1) even(t + 1);
+  };
+  auto find_next = [&](int t) {
+    if (t + 3 < t1) locate(t + 3);
   };
   if (late) even(t0);
   int t = t0;
@@ -500,24 +507,30 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     products(t, t, no, yes);
     second_barrier(t);
     done = weights(t);
+    find_next(t);
     for (++t; t < tw; ++t) {
       first_barrier(t);
       products(t - 1, t, yes, yes);
       second_barrier(t);
       done = weights(t);
+      find_next(t);
     }
     first_barrier(t);
     products(t - 1, t, yes, no);
     second_barrier(t);
+    find_next(t);
     ++t;
   }
   for (; t <= t1; ++t) {
     first_barrier(t);
+    if (t + 2 < t1)
+#pragma unroll
+      for (int part = 0; part < 4; ++part) load(t + 2, part);
     second_barrier(t);
+    find_next(t);
   }
   if (!wvalid) return;
-  l1 += xor32(l1);
-  l2 += xor32(l2);
+  lrun += xor32(lrun);
   if (nsp > 1) {
     const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * EX_ROWS + wave * 32 + m;
     if (rvalid) {
@@ -528,16 +541,15 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
           *reinterpret_cast<f32x4*>(a.part_o + pr * D + b * 32 + i * 8 + half * 4) =
               (f32x4){oacc[b][4 * i], oacc[b][4 * i + 1], oacc[b][4 * i + 2], oacc[b][4 * i + 3]};
       if (half == 0) {
-        a.part_ml[pr * 3] = mref;
-        a.part_ml[pr * 3 + 1] = l1;
-        a.part_ml[pr * 3 + 2] = l2;
+        a.part_ml[pr * 2] = mref;
+        a.part_ml[pr * 2 + 1] = lrun;
       }
     }
     return;
   }
   if (!rvalid) return;
-  const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;  // no key: 0; a NaN stays one
-  const Join j = join_of(l2 == 0.f ? -INFINITY : mref + log2f(l2), a.pl, orow);
+  const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;  // no key: 0; a NaN stays one
+  const Join j = join_of(lrun == 0.f ? -INFINITY : mref + log2f(lrun), a.pl, orow);
 #pragma unroll
   for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -786,9 +798,8 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
   __syncthreads();  // every wave has read the prior's lse, which may be lse itself
   if (wave != 0 || half != 0 || !rvalid) return;
   if (nsp > 1) {
-    a.part_ml[pr * 3] = M;
-    a.part_ml[pr * 3 + 1] = L;
-    a.part_ml[pr * 3 + 2] = L;
+    a.part_ml[pr * 2] = M;
+    a.part_ml[pr * 2 + 1] = L;
   } else if (a.lse) {
     a.lse[orow] = j.lse;
   }
@@ -798,11 +809,10 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
 // w_s = 2^(m_s - max m); four dims to a thread.
 struct Sum {
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float M = EX_NONE, l1 = 0.f, l2 = 0.f;
-  __device__ __forceinline__ void add(float m, float x, float z, f32x4 v) {
+  float M = EX_NONE, l = 0.f;
+  __device__ __forceinline__ void add(float m, float x, f32x4 v) {
     const float top = fmaxf(M, m), p = __builtin_amdgcn_exp2f(M - top), q = __builtin_amdgcn_exp2f(m - top);
-    l1 = l1 * p + x * q;
-    l2 = l2 * p + z * q;
+    l = l * p + x * q;
     o = o * p + v * q;
     M = top;
   }
@@ -810,14 +820,13 @@ struct Sum {
   template <typename F>
   __device__ __forceinline__ void gather(const float* po, const float* ml, int k0, int step, int count, int d4, F row) {
     for (; k0 < count; k0 += 8 * step) {
-      float m[8], x[8], z[8];
+      float m[8], x[8];
       f32x4 v[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const size_t pr = row(min(k0 + u * step, count - 1));
-        m[u] = ml[pr * 3];
-        x[u] = ml[pr * 3 + 1];
-        z[u] = ml[pr * 3 + 2];
+        m[u] = ml[pr * 2];
+        x[u] = ml[pr * 2 + 1];
         v[u] = reinterpret_cast<const f32x4*>(po + pr * D)[d4];
       }
       float top = M;
@@ -825,15 +834,13 @@ struct Sum {
       for (int u = 0; u < 8; ++u) top = fmaxf(top, m[u]);
       const float back = __builtin_amdgcn_exp2f(M - top);
       o *= back;
-      l1 *= back;
-      l2 *= back;
+      l *= back;
       M = top;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         if (k0 + u * step < count) {
           const float wgt = __builtin_amdgcn_exp2f(m[u] - M);
-          l1 += wgt * x[u];
-          l2 += wgt * z[u];
+          l += wgt * x[u];
           o += wgt * v[u];
         }
       }
@@ -841,8 +848,8 @@ struct Sum {
   }
   template <int FP32>
   __device__ __forceinline__ void store(const ExactArgs& a, size_t orow, int d4) const {
-    const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
-    const Join j = join_of(l2 == 0.f ? -INFINITY : M + log2f(l2), a.pl, orow);
+    const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+    const Join j = join_of(l == 0.f ? -INFINITY : M + log2f(l), a.pl, orow);
     store4<FP32>(a, orow, d4 * 4, o * inv, j);
     if (d4 == 0 && a.lse) a.lse[orow] = j.lse;
   }
@@ -945,7 +952,6 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const int grp16 = lane >> 4, s16 = lane & 15;
   const uint8_t* vl0 = s_mem[wave][0] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
-  const bf16x2 ones2 = {(__bf16)1.0f, (__bf16)1.0f};
 
   // tiles [ta, tb) of request i's kv head kvh; whole: that is all of them
   auto item = [&](int i, int s0, int add, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
@@ -967,7 +973,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
       for (int kk = 0; kk < 8; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[2 * kk + half]);
     }
     f32x16 oacc[4] = {zero, zero, zero, zero};
-    float mref = EX_NONE, l1 = 0.f, l2 = 0.f;
+    float mref = EX_NONE, lrun = 0.f;
     auto id_of = [&](int t) { return row[min(t * 32 + m, kend - 1) >> a.shift]; };
     // row index in the pages of this lane's key of tile t on page id (a tensor of
     // 2^31 rows would not fit the GPU); bad: no page, page 0 is read instead
@@ -1039,29 +1045,20 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
         if (__ballot(grow)) {  // uniform
           const float mnew = grow ? tmax : mref;
           const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
-          l1 *= alpha;
-          l2 *= alpha;
+          lrun *= alpha;
 #pragma unroll
           for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
           mref = mnew;
         }
         bf16x8 pb[2];
-        float part[2] = {0.f, 0.f}, sum0 = 0.f, sum1 = 0.f;
+        float part[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const float p = __builtin_amdgcn_exp2f(fmaf(s[j], EX_SCALE, -mref));
           part[j & 1] += p;
           pb[j >> 3][j & 7] = (__bf16)p;
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          sum0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 0, 1), ones2, sum0, false);
-          sum1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 2, 3), ones2, sum1, false);
-          sum0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 4, 5), ones2, sum0, false);
-          sum1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pb[j], pb[j], 6, 7), ones2, sum1, false);
-        }
-        l1 += sum0 + sum1;
-        l2 += part[0] + part[1];
+        lrun += part[0] + part[1];
         auto read_v = [&](int b, int st, int z = 0) {
           const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + z + b * FW_VB + st * 1024));
           const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vl + z + b * FW_VB + st * 1024 + 512));
@@ -1105,12 +1102,11 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
         }
       }
     }
-    l1 += xor32(l1);
-    l2 += xor32(l2);
+    lrun += xor32(lrun);
     if (!rvalid) return;
     if (whole) {
-      const float inv = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
-      const Join j = join_of(l2 == 0.f ? -INFINITY : mref + log2f(l2), a.pl, orow);
+      const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;
+      const Join j = join_of(lrun == 0.f ? -INFINITY : mref + log2f(lrun), a.pl, orow);
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -1128,9 +1124,8 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
         *reinterpret_cast<f32x4*>(a.few_o + prow * D + b * 32 + e * 8 + half * 4) =
             (f32x4){oacc[b][4 * e], oacc[b][4 * e + 1], oacc[b][4 * e + 2], oacc[b][4 * e + 3]};
     if (half == 0) {
-      a.few_ml[prow * 3] = mref;
-      a.few_ml[prow * 3 + 1] = l1;
-      a.few_ml[prow * 3 + 2] = l2;
+      a.few_ml[prow * 2] = mref;
+      a.few_ml[prow * 2 + 1] = lrun;
     }
   };
 
@@ -1175,7 +1170,7 @@ constexpr int FJ_Y = 4;
 constexpr int FJ_MANY = 48;
 __global__ __launch_bounds__(FJ_W * 64) void k_exact_few_join(ExactArgs a, int waves) {
   __shared__ f32x4 s_o[FJ_W][32];
-  __shared__ float s_l[FJ_W][3];
+  __shared__ float s_l[FJ_W][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int w0 = blockIdx.x * FJ_W, y = blockIdx.y, ny = gridDim.y;
   const int g = lane >> 5, d4 = lane & 31;
@@ -1197,20 +1192,19 @@ __global__ __launch_bounds__(FJ_W * 64) void k_exact_few_join(ExactArgs a, int w
         f32x4 v;
 #pragma unroll
         for (int c = 0; c < 4; ++c) v[c] = xor32(s.o[c]);
-        s.add(xor32(s.M), xor32(s.l1), xor32(s.l2), v);
+        s.add(xor32(s.M), xor32(s.l), v);
       }
       if (many) {
         __syncthreads();  // s_o and s_l are free
         if (g == 0) s_o[wave][d4] = s.o;
         if (lane == 0) {
           s_l[wave][0] = s.M;
-          s_l[wave][1] = s.l1;
-          s_l[wave][2] = s.l2;
+          s_l[wave][1] = s.l;
         }
         __syncthreads();
         if (wave != 0) continue;
 #pragma unroll
-        for (int k = 1; k < FJ_W; ++k) s.add(s_l[k][0], s_l[k][1], s_l[k][2], s_o[k][d4]);
+        for (int k = 1; k < FJ_W; ++k) s.add(s_l[k][0], s_l[k][1], s_o[k][d4]);
       }
       const int tok = r / a.grp;
       if (g == 0) s.store<0>(a, (size_t)(s0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp), d4);
