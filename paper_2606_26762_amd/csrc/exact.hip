@@ -316,24 +316,24 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p + 256);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  // Eight steps of four products, V's (O of tile tv) and K's (S of tile tk), the
-  // operands of each step read while the one before it is multiplied.
+  // Eight steps of four products, V's (O of tile tv) and K's (S of tile tk); behind
+  // each product the same one's operand of the next step is read (a step's eight
+  // transposed reads in a row left the matrix core waiting a fifth of its time).
   // Tile tk + 2's four loads go out between the steps.
   bool done = false;  // the last tile's P V is
   auto products = [&](int tv, int tk, auto with_v, auto with_k) {
     const bool more = tk + 2 < t1;  // uniform
     constexpr int F = decltype(with_v)::value ? 0 : 4, L = decltype(with_k)::value ? 8 : 4;
     const uint32_t vl = value_base(done ? s_zero : s_kv[tv % EX_NBUF][1]), kl = key_base(tk);
+    __builtin_amdgcn_s_setprio(1);
     bf16x8 op[2][4];
-    auto read = [&](int step) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        op[step & 1][j] = step < 4 ? __builtin_bit_cast(bf16x8, read_v(vl, j, step)) : read_k(kl, j & 1, 2 * (step - 4) + (j >> 1));
+    auto read = [&](int step, int j) {
+      op[step & 1][j] = step < 4 ? __builtin_bit_cast(bf16x8, read_v(vl, j, step)) : read_k(kl, j & 1, 2 * (step - 4) + (j >> 1));
     };
-    read(F);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) read(F, j);
 #pragma unroll
     for (int step = F; step < L; ++step) {
-      if (step + 1 < L) read(step + 1);
       if (more) {
         if (L - F == 8) {
           if (step & 1) load(tk + 2, step >> 1);
@@ -341,18 +341,21 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
           load(tk + 2, step & 3);
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
         if (step < 4) {
           oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], pb[step], oacc[j], 0, 0, 0);
         } else {
           const int kk = 2 * (step - 4) + (j >> 1);
           s[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], bq[kk], kk ? s[j & 1] : zero, 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (step + 1 < L) read(step + 1, j);
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(0);
   };
   // Softmax weights of tile t; true if its P V is done as well: hidden keys with
   // infinite or NaN values.
