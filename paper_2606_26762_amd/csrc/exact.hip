@@ -181,7 +181,7 @@ __device__ __forceinline__ void ex_barrier() {
 constexpr int EX_KEYS = 64;             // keys per tile
 constexpr int EX_TILE = EX_KEYS * D * 2;  // one K or V tile, 16 KB
 constexpr int EX_NBUF = 4;              // tile t computes while t + 1 .. t + 3 load
-constexpr int EX_IDS = 2048;            // page ids staged at a time
+constexpr int EX_IDS = 1024;            // page ids staged at a time
 
 // Workgroup = eight waves of 32 query rows each.  Tiles of 64 keys go straight from
 // global memory into LDS (global_load_lds_dwordx4), two tiles ahead, four whole rows
@@ -195,7 +195,7 @@ constexpr int EX_IDS = 2048;            // page ids staged at a time
 template <int PAGED>
 __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   __shared__ __attribute__((aligned(256))) uint8_t s_kv[EX_NBUF][2][EX_TILE];
-  __shared__ int32_t s_ids[PAGED ? EX_IDS : 1];
+  __shared__ int32_t s_ids[2][PAGED ? EX_IDS : 1];  // two runs of page ids, in turn
   __shared__ unsigned long long s_bad[8];  // keys of a tile on pages that are none
   __shared__ __attribute__((aligned(256))) uint8_t s_zero[EX_TILE];  // V of a tile whose products are done already
   const int tid = threadIdx.x, lane = tid & 63;
@@ -241,11 +241,11 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   auto load_ids = [&](int t) {  // the run that tile t is in
     const int e0 = (t / tpc) * EX_IDS, n = min(EX_IDS, ((it.kend - 1) >> a.shift) + 1 - e0);
     const int32_t* row = a.table + (size_t)it.seq * a.stride + e0;
-    for (int i = tid; i < n; i += 512) s_ids[i] = row[i];
+    for (int i = tid; i < n; i += 512) s_ids[(t / tpc) & 1][i] = row[i];
   };
   // byte offset of key's row; bad: its page is none (page 0 is read instead)
   auto paged_row = [&](int key, bool& bad) {
-    const int id = s_ids[(key >> a.shift) & (EX_IDS - 1)];
+    const int e = key >> a.shift, id = s_ids[(e / EX_IDS) & 1][e & (EX_IDS - 1)];
     bad = (unsigned)id >= (unsigned)a.num_pages;
     const size_t page = bad ? 0 : id;
     return ((((page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1)))) * (size_t)(D * 2);
@@ -294,8 +294,15 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   const int grp16 = lane >> 4, s16 = lane & 15;
   // One tile's work in two halves: products are the matrix ones (the last tile's
   // P V, then this tile's K Q), weights() the softmax between them.
-  f32x16 s[2];
-  bf16x8 pb[4];
+  f32x16 s[2];     // scores, then weights
+  bf16x8 p_next;   // the first step's weights
+  // P operand of 16-key step st: the weights in bfloat16
+  auto weight_operand = [&](int st) {
+    bf16x8 p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = (__bf16)s[st >> 1][(st & 1) * 8 + i];
+    return p;
+  };
   auto key_base = [&](int t) {
     return (uint32_t)(uintptr_t)(lds_u16x8*)s_kv[t % EX_NBUF][0] + (m * 256 + ((m & 15) ^ half) * 16);
   };
@@ -326,12 +333,14 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     constexpr int F = decltype(with_v)::value ? 0 : 4, L = decltype(with_k)::value ? 8 : 4;
     const uint32_t vl = value_base(done ? s_zero : s_kv[tv % EX_NBUF][1]), kl = key_base(tk);
     __builtin_amdgcn_s_setprio(1);
-    bf16x8 op[2][4];
+    bf16x8 op[2][4], p[2];
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
     auto read = [&](int step, int j) {
       op[step & 1][j] = step < 4 ? __builtin_bit_cast(bf16x8, read_v(vl, j, step)) : read_k(kl, j & 1, 2 * (step - 4) + (j >> 1));
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j) read(F, j);
+    p[0] = p_next;
 #pragma unroll
     for (int step = F; step < L; ++step) {
       if (more) {
@@ -345,15 +354,24 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
       for (int j = 0; j < 4; ++j) {
         __builtin_amdgcn_sched_barrier(0);
         if (step < 4) {
-          oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], pb[step], oacc[j], 0, 0, 0);
+          oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], p[step & 1], oacc[j], 0, 0, 0);
         } else {
           const int kk = 2 * (step - 4) + (j >> 1);
           s[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], bq[kk], kk ? s[j & 1] : zero, 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
         if (step + 1 < L) read(step + 1, j);
+        if (step < 4) {  // the next step's weights, and the sum of this one's
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            if (step < 3) p[(step + 1) & 1][2 * j + e] = (__bf16)s[(step + 1) >> 1][((step + 1) & 1) * 8 + 2 * j + e];
+            part[2 * (j & 1) + e] += s[step >> 1][(step & 1) * 8 + 2 * j + e];
+            asm volatile("" : "+v"(part[2 * (j & 1) + e]));  // here, beside the products
+          }
+        }
       }
     }
+    if (F == 0) lrun += (part[0] + part[1]) + (part[2] + part[3]);  // this half's keys; the halves meet at the end
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(0);
   };
@@ -401,16 +419,11 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
       for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
       mref = mnew;
     }
-    float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[h][i], EX_SCALE, -mref));
-        part[i & 3] += p;
-        pb[2 * h + (i >> 3)][i & 7] = (__bf16)p;
-      }
-    lrun += (part[0] + part[1]) + (part[2] + part[3]);  // this half's keys; the halves meet at the end
+      for (int i = 0; i < 16; ++i) s[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], EX_SCALE, -mref));
+    p_next = weight_operand(0);
     if (!hidden) return false;  // uniform
     const uint32_t vl = value_base(s_kv[t % EX_NBUF][1]);
     uint32_t odd = 0;
@@ -427,21 +440,21 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
       uint32_t vz = vl + anew();
 #pragma unroll
       for (int st = 0; st < 4; ++st)
-        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<0>(read_v(vz, b, st)), pb[st], hits, 0, 0, 0);
+        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<0>(read_v(vz, b, st)), weight_operand(st), hits, 0, 0, 0);
       oacc[b] += hits;
       __builtin_amdgcn_sched_barrier(0);
       hits = zero;
       vz = vl + anew();
 #pragma unroll
       for (int st = 0; st < 4; ++st)
-        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<1>(read_v(vz, b, st)), pb[st], hits, 0, 0, 0);
+        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<1>(read_v(vz, b, st)), weight_operand(st), hits, 0, 0, 0);
       add_odd<1>(oacc[b], hits);
       __builtin_amdgcn_sched_barrier(0);
       hits = zero;
       vz = vl + anew();
 #pragma unroll
       for (int st = 0; st < 4; ++st)
-        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<-1>(read_v(vz, b, st)), pb[st], hits, 0, 0, 0);
+        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<-1>(read_v(vz, b, st)), weight_operand(st), hits, 0, 0, 0);
       add_odd<-1>(oacc[b], hits);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -450,40 +463,33 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 
 #pragma unroll
   for (int i = 0; i < EX_TILE / 8192; ++i) reinterpret_cast<uint4*>(s_zero)[tid + i * 512] = make_uint4(0, 0, 0, 0);
+  if constexpr (PAGED) {
+    // the runs of tiles t0 .. t0 + 3
+    if (t0 < t1) load_ids(t0);
+    if ((t0 + 3) / tpc != t0 / tpc && t0 + 3 < t1) load_ids(t0 + 3);
+  }
   wait_vm<0>();  // the query operands are in registers before any tile is in flight
+  ex_barrier();
   for (int t = t0; t < t0 + 3 && t < t1; ++t) {
-    if constexpr (PAGED) {
-      if (t == t0 || t % tpc == 0) {  // uniform
-        ex_barrier();
-        load_ids(t);
-        ex_barrier();
-      }
-    }
     if (t < t0 + 2) issue(t);
     else locate(t);
   }
-  // Waves w and w + 4 share a SIMD.  Waves 0 - 3 form the products of tile t in phase
-  // 2 t and its weights in phase 2 t + 1, waves 4 - 7 one phase later, so that in
-  // every phase one wave of a SIMD has the matrix core and the other the VALU (in
-  // step, both wait for the one and then for the other).  A barrier begins each phase.
-  // Tile t + 2 is loaded beside the products of tile t, from phase 2 t on, where V of
-  // tile t - 2, last read in phase 2 t - 1, has left its buffer, and has landed by
-  // phase 2 t + 4; its rows are located after the weights of tile t - 1.
-  auto even = [&](int t) {  // the barrier before phase 2 t
+  // Waves w and w + 4 share a SIMD.  In period t waves 0 - 3 form the products of tile
+  // t, then its weights, and waves 4 - 7 the weights of tile t - 1, then the products
+  // of tile t, so that one wave of a SIMD has the matrix core while the other has the
+  // VALU (in step, both wait for the one and then for the other).  A barrier begins
+  // each period.  Tile t + 2 is loaded beside the products of tile t: V of tile t - 2,
+  // last read in period t - 1, has left its buffer, and the tile is read from period
+  // t + 2 on.
+  auto even = [&](int t) {  // the barrier before period t
     __builtin_amdgcn_sched_barrier(0);
     if (t + 1 < t1) wait_vm<4>();  // this wave's loads of tile t have landed, those of t + 1 may be in flight
     else wait_vm<0>();
     ex_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  auto odd_phase = [&](int t) {  // the barrier before phase 2 t + 1
-    __builtin_amdgcn_sched_barrier(0);
-    ex_barrier();
     if constexpr (PAGED) {
-      if (t + 3 < t1 && (t + 3) % tpc == 0) {  // uniform
-        load_ids(t + 3);
-        ex_barrier();
-      }
+      // page ids from tile t + 4 on, located in period t + 1 at the earliest, in the
+      // place of those of tiles up to t + 3 - tpc (tpc >= 16)
+      if (t + 4 < t1 && (t + 4) % tpc == 0) load_ids(t + 4);  // uniform
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -493,12 +499,10 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   constexpr std::false_type no{};
   const bool late = wave >= 4;  // uniform
   auto first_barrier = [&](int t) {
-    if (late) odd_phase(t);
-    else even(t);
+    if (!late) even(t);
   };
   auto second_barrier = [&](int t) {
-    if (!late) odd_phase(t);
-    else if (t < t1) even(t + 1);
+    if (late && t < t1) even(t + 1);
   };
   auto find_next = [&](int t) {
     if (t + 3 < t1) locate(t + 3);
