@@ -81,17 +81,24 @@ protokv_status check_result(const Heads& h, int n, int total, const int32_t* cu,
 }
 
 // Row blocks: sequence i has the indices floor(cu[i] grp / R) + i and on, which
-// leaves room for its ceil(rows / R) whatever cu is; how many of them there are
-// in all, and most context splits of one, chosen so that a launch has work for
-// the whole GPU (two workgroups to a compute unit).
+// leaves room for its ceil(rows / R) whatever cu is; and most context splits of one:
+// the number with the least rounds of workgroups (`slots` run at a time) times key
+// tiles, where splitting costs a workgroup the time of `join` tiles for its partial
+// (4 x 512 tokens over 16 k, 224 blocks: 3 splits 540 us, 1 split PENDING).
 void plan_blocks(ExactArgs& a, bool fp32, bool paged) {
   const int R = fp32 ? EX_ROWS_F32 : EX_ROWS;
   a.blocks = (int)((int64_t)a.total * a.grp / R) + a.n;
   a.splits = 1;
-  const int64_t items = (int64_t)a.blocks * a.Hkv, want = 512;
-  if (paged && items > 0 && items < want / 2) {
-    const int64_t tiles = ((int64_t)a.stride << a.shift) / (fp32 ? 32 : 64);
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({EX_MAX_SPLITS, (want + items - 1) / items, tiles / EX_MIN_TILES}));
+  const int64_t items = (int64_t)a.blocks * a.Hkv, slots = fp32 ? 512 : 256, join = fp32 ? 4 : 6;
+  if (!paged || items == 0 || items >= 4 * slots) return;
+  const int64_t tiles = ((int64_t)a.stride << a.shift) / (fp32 ? 32 : 64);
+  int64_t best = INT64_MAX;
+  for (int s = 1; s <= EX_MAX_SPLITS && (s == 1 || s <= tiles / EX_MIN_TILES); ++s) {
+    const int64_t cost = (items * s + slots - 1) / slots * ((tiles + s - 1) / s + (s > 1 ? join : 0));
+    if (cost < best) {
+      best = cost;
+      a.splits = s;
+    }
   }
 }
 
