@@ -80,24 +80,35 @@ protokv_status check_result(const Heads& h, int n, int total, const int32_t* cu,
   return PROTOKV_OK;
 }
 
-// Row blocks: sequence i has the indices floor(cu[i] grp / R) + i and on, which
-// leaves room for its ceil(rows / R) whatever cu is; and most context splits of one:
-// the number with the least rounds of workgroups (`slots` run at a time) times key
-// tiles, where splitting costs a workgroup the time of `join` tiles for its partial
-// (4 x 512 tokens over 16 k, 224 blocks: 3 splits 540 us, 1 split PENDING).
+// Row blocks of R rows: sequence i has the indices floor(cu[i] grp / R) + i and on,
+// which leaves room for its ceil(rows / R) whatever cu is.  R and, over pages, the
+// most context splits of a block are those with the least time by this count, in
+// tenths of a 64-key tile's time in the form of 256 rows (about 2 us): a tile takes
+// 10 (128 rows, two waves to a row's keys: 6; float32: a tile of 32 keys, 10), a
+// workgroup 40 to start and to end (50 with the waves' merge), a split 60 more for its
+// partial; `slots` workgroups run at a time.  Prompts see half their keys on
+// average and take at least as long as their last rows.  Measured, 28 / 4 heads: one
+// prompt of 1500 tokens 43 us by 256 rows, 34 by 128; eight of 200 17 and 25; one of
+// 4000 115 and 146; 4 x 512 tokens over 16 k in 3 splits 540, unsplit 484.
 void plan_blocks(ExactArgs& a, bool fp32, bool paged) {
-  const int R = fp32 ? EX_ROWS_F32 : EX_ROWS;
-  a.blocks = (int)((int64_t)a.total * a.grp / R) + a.n;
-  a.splits = 1;
-  const int64_t items = (int64_t)a.blocks * a.Hkv, slots = fp32 ? 512 : 256, join = fp32 ? 4 : 6;
-  if (!paged || items == 0 || items >= 4 * slots) return;
-  const int64_t tiles = ((int64_t)a.stride << a.shift) / (fp32 ? 32 : 64);
+  const int64_t slots = fp32 ? 512 : 256;
+  const int64_t keys = paged ? (int64_t)a.stride << a.shift : ((int64_t)a.total + a.n - 1) / std::max(a.n, 1);
+  const int64_t tiles = (keys + (fp32 ? 31 : 63)) / (fp32 ? 32 : 64);
   int64_t best = INT64_MAX;
-  for (int s = 1; s <= EX_MAX_SPLITS && (s == 1 || s <= tiles / EX_MIN_TILES); ++s) {
-    const int64_t cost = (items * s + slots - 1) / slots * ((tiles + s - 1) / s + (s > 1 ? join : 0));
-    if (cost < best) {
-      best = cost;
-      a.splits = s;
+  for (int half = 0; half <= (fp32 ? 0 : 1); ++half) {
+    const int R = fp32 ? EX_ROWS_F32 : EX_ROWS >> half;
+    const int blocks = (int)((int64_t)a.total * a.grp / R) + a.n;
+    const int64_t items = (int64_t)blocks * a.Hkv, unit = half ? 6 : 10, ends = half ? 50 : 40;
+    for (int s = 1; s <= (paged ? EX_MAX_SPLITS : 1) && (s == 1 || s <= tiles / EX_MIN_TILES); ++s) {
+      const int64_t rounds = (items * s + slots - 1) / slots;
+      const int64_t cost = paged ? rounds * ((tiles + s - 1) / s * unit + ends + (s > 1 ? 60 : 0))
+                                 : std::max(tiles * unit + ends, rounds * (tiles * unit / 2 + ends));
+      if (cost < best) {
+        best = cost;
+        a.rows = R;
+        a.blocks = blocks;
+        a.splits = s;
+      }
     }
   }
 }
@@ -117,7 +128,7 @@ size_t lay_out(ExactArgs& a, bool fp32, uint8_t* base) {
     a.few_meta = (int32_t*)take((size_t)a.few * 4 * 4);
   }
   if (a.splits > 1) {
-    const size_t rows = (size_t)a.Hkv * a.blocks * a.splits * (fp32 ? EX_ROWS_F32 : EX_ROWS);
+    const size_t rows = (size_t)a.Hkv * a.blocks * a.splits * a.rows;
     a.part_o = (float*)take(rows * D * 4);
     a.part_ml = (float*)take(rows * 2 * 4);
   }

@@ -14,7 +14,7 @@ namespace pkv {
 // Message of the last failure without a handle on this thread (protokv.cpp).
 std::string& call_error();
 
-constexpr int EX_ROWS = 256;      // query rows per workgroup of the bf16 kernel (8 waves of 32)
+constexpr int EX_ROWS = 256;      // query rows per workgroup of the bf16 kernel (8 waves of 32), or half as many
 constexpr int EX_ROWS_F32 = 32;   // query rows per workgroup of the float32 kernel
 constexpr int EX_MAX_SPLITS = 16;
 constexpr int EX_MIN_TILES = 8;   // 64-key (bf16) or 32-key (float32) tiles that a context split has at least
@@ -43,6 +43,7 @@ struct ExactArgs {
   float *few_o, *few_ml;
   int32_t* few_meta;
   int few, few_rows;  // its waves (0: not launched, the row blocks take every request), its rows at most
+  int rows;    // query rows of a row block
   int blocks;  // row-block indices per kv head (0: no row blocks)
   int splits;  // most context splits of a row block
 };

@@ -192,7 +192,7 @@ constexpr int EX_IDS = 1024;            // page ids staged at a time
 // S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x16_bf16,
 // V^T through ds_read_b64_tr_b16: each lane holds one query column, so the
 // softmax is lane-local plus one exchange with the partner lane.
-template <int PAGED>
+template <int PAGED, int KH>
 __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   __shared__ __attribute__((aligned(256))) uint8_t s_kv[EX_NBUF][2][EX_TILE];
   __shared__ int32_t s_ids[2][PAGED ? EX_IDS : 1];  // two runs of page ids, in turn
@@ -205,7 +205,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
   const int split = rest % a.splits, blk = a.blocks - 1 - rest / a.splits;
   Item it;
-  if (!find_item<EX_ROWS>(a, blk, it)) return;  // uniform in the workgroup
+  constexpr int ROWS = EX_ROWS / KH;
+  if (!find_item<ROWS>(a, blk, it)) return;  // uniform in the workgroup
   int per;
   const int tiles = (it.kend + EX_KEYS - 1) / EX_KEYS;
   const int nsp = splits_of(a, tiles, per);
@@ -213,7 +214,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   const int t0 = split * per, t1 = min(tiles, t0 + per);
 
   const int m = lane & 31, half = lane >> 5;
-  const int rw = it.row0 + wave * 32, r = rw + m;
+  const int kh = KH == 2 ? wave >> 2 : 0;  // key half of every tile that this wave takes
+  const int rw = it.row0 + (wave % (8 / KH)) * 32, r = rw + m;
   const bool wvalid = rw < it.rows, rvalid = r < it.rows;  // wvalid is uniform
   const int tok = rvalid ? r / a.grp : 0;
   const int head = kvh * a.grp + (rvalid ? r - tok * a.grp : 0);
@@ -294,7 +296,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   const int grp16 = lane >> 4, s16 = lane & 15;
   // One tile's work in two halves: products are the matrix ones (the last tile's
   // P V, then this tile's K Q), weights() the softmax between them.
-  f32x16 s[2];     // scores, then weights
+  constexpr int NH = 2 / KH, NST = 4 / KH;  // a wave's 32-key halves and 16-key steps of a tile, and steps of K
+  f32x16 s[2];     // scores, then weights (KH = 2: of even and odd 16-dim steps, then all in the first)
   bf16x8 p_next;   // the first step's weights
   // P operand of 16-key step st: the weights in bfloat16
   auto weight_operand = [&](int st) {
@@ -304,7 +307,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     return p;
   };
   auto key_base = [&](int t) {
-    return (uint32_t)(uintptr_t)(lds_u16x8*)s_kv[t % EX_NBUF][0] + (m * 256 + ((m & 15) ^ half) * 16);
+    return (uint32_t)(uintptr_t)(lds_u16x8*)s_kv[t % EX_NBUF][0] + kh * 8192 + (m * 256 + ((m & 15) ^ half) * 16);
   };
   // K operand of key half h, 16-dim step kk: chunk 2 kk + half of key 32 h + m
   auto read_k = [&](uint32_t kl, int h, int kk) {
@@ -314,7 +317,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   // keys 16 st + 4 half + {0..3} (i < 4) and + 8 (i >= 4), as P's registers are.
   // Source lane i of 16 reads key i / 4 of its four, dims 4 (i % 4) .. + 3.
   auto value_base = [&](const uint8_t* tile) {
-    return (uint32_t)(uintptr_t)(lds_v4i16*)tile + (4 * half + (s16 >> 2)) * 256 +
+    return (uint32_t)(uintptr_t)(lds_v4i16*)tile + kh * 8192 + (4 * half + (s16 >> 2)) * 256 +
            (((grp16 & 1) * 2 + ((s16 & 3) >> 1)) ^ ((s16 >> 2) << 2)) * 16 + (s16 & 1) * 8;
   };
   auto read_v = [&](uint32_t vl, int b, int st) {
@@ -330,13 +333,15 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   bool done = false;  // the last tile's P V is
   auto products = [&](int tv, int tk, auto with_v, auto with_k) {
     const bool more = tk + 2 < t1;  // uniform
-    constexpr int F = decltype(with_v)::value ? 0 : 4, L = decltype(with_k)::value ? 8 : 4;
+    constexpr int F = decltype(with_v)::value ? 0 : NST, L = decltype(with_k)::value ? 2 * NST : NST;
     const uint32_t vl = value_base(done ? s_zero : s_kv[tv % EX_NBUF][1]), kl = key_base(tk);
     __builtin_amdgcn_s_setprio(1);
     bf16x8 op[2][4], p[2];
     float part[4] = {0.f, 0.f, 0.f, 0.f};
     auto read = [&](int step, int j) {
-      op[step & 1][j] = step < 4 ? __builtin_bit_cast(bf16x8, read_v(vl, j, step)) : read_k(kl, j & 1, 2 * (step - 4) + (j >> 1));
+      const int ks = step - NST;
+      op[step & 1][j] = ks < 0 ? __builtin_bit_cast(bf16x8, read_v(vl, j, step))
+                               : KH == 1 ? read_k(kl, j & 1, 2 * ks + (j >> 1)) : read_k(kl, 0, 4 * ks + j);
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j) read(F, j);
@@ -344,27 +349,25 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 #pragma unroll
     for (int step = F; step < L; ++step) {
       if (more) {
-        if (L - F == 8) {
-          if (step & 1) load(tk + 2, step >> 1);
-        } else {
-          load(tk + 2, step & 3);
-        }
+        constexpr int N = L - F;  // 8, 4 or 2 steps for the four loads
+        if (N == 2) load(tk + 2, 2 * (step - F));
+        if (N < 8 || ((step - F) & 1)) load(tk + 2, N == 8 ? (step - F) >> 1 : N == 4 ? step - F : 2 * (step - F) + 1);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         __builtin_amdgcn_sched_barrier(0);
-        if (step < 4) {
+        if (step < NST) {
           oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], p[step & 1], oacc[j], 0, 0, 0);
         } else {
-          const int kk = 2 * (step - 4) + (j >> 1);
-          s[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], bq[kk], kk ? s[j & 1] : zero, 0, 0, 0);
+          const int ks = step - NST, kk = KH == 1 ? 2 * ks + (j >> 1) : 4 * ks + j;
+          s[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[step & 1][j], bq[kk], kk < KH ? zero : s[j & 1], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
         if (step + 1 < L) read(step + 1, j);
-        if (step < 4) {  // the next step's weights, and the sum of this one's
+        if (step < NST) {  // the next step's weights, and the sum of this one's
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            if (step < 3) p[(step + 1) & 1][2 * j + e] = (__bf16)s[(step + 1) >> 1][((step + 1) & 1) * 8 + 2 * j + e];
+            if (step < NST - 1) p[(step + 1) & 1][2 * j + e] = (__bf16)s[(step + 1) >> 1][((step + 1) & 1) * 8 + 2 * j + e];
             part[2 * (j & 1) + e] += s[step >> 1][(step & 1) * 8 + 2 * j + e];
             asm volatile("" : "+v"(part[2 * (j & 1) + e]));  // here, beside the products
           }
@@ -378,24 +381,25 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   // Softmax weights of tile t; true if its P V is done as well: hidden keys with
   // infinite or NaN values.
   auto weights = [&](int t) {
+    if (KH == 2) s[0] += s[1];
     bool hidden = (t + 1) * EX_KEYS > wfull;
     unsigned long long bad = 0;
     if constexpr (PAGED) {
       bad = s_bad[t & 7];
       hidden |= __builtin_amdgcn_readfirstlane((int)(bad != 0)) != 0;
-      bad >>= 4 * half;
+      bad >>= 32 * kh + 4 * half;
     }
     if (hidden) {  // uniform
-      const int rel = klim - t * EX_KEYS - 4 * half;
+      const int rel = klim - t * EX_KEYS - 32 * kh - 4 * half;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < NH; ++h)
 #pragma unroll
         for (int i = 0; i < 16; ++i)  // key 32 h + 8 (i / 4) + i % 4 + 4 half of the tile
           s[h][i] = 32 * h + 8 * (i >> 2) + (i & 3) > rel ? -INFINITY : s[h][i];
       if constexpr (PAGED) {
         if (__ballot(bad != 0)) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < NH; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               s[h][i] = (bad >> (32 * h + 8 * (i >> 2) + (i & 3))) & 1 ? -INFINITY : s[h][i];
@@ -404,7 +408,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     }
     float tmax = -INFINITY;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < NH; ++h)
 #pragma unroll
       for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, s[h][i]);
     tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
@@ -420,7 +424,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
       mref = mnew;
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < NH; ++h)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], EX_SCALE, -mref));
     p_next = weight_operand(0);
@@ -430,7 +434,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
 #pragma unroll
-      for (int st = 0; st < 4; ++st) odd |= odd_flags(read_v(vl, b, st));
+      for (int st = 0; st < NST; ++st) odd |= odd_flags(read_v(vl, b, st));
       __builtin_amdgcn_sched_barrier(0);
     }
     if (!__ballot((odd & ODD) != 0)) return false;  // uniform
@@ -439,21 +443,21 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
       f32x16 hits = zero;
       uint32_t vz = vl + anew();
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
+      for (int st = 0; st < NST; ++st)
         hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<0>(read_v(vz, b, st)), weight_operand(st), hits, 0, 0, 0);
       oacc[b] += hits;
       __builtin_amdgcn_sched_barrier(0);
       hits = zero;
       vz = vl + anew();
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
+      for (int st = 0; st < NST; ++st)
         hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<1>(read_v(vz, b, st)), weight_operand(st), hits, 0, 0, 0);
       add_odd<1>(oacc[b], hits);
       __builtin_amdgcn_sched_barrier(0);
       hits = zero;
       vz = vl + anew();
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
+      for (int st = 0; st < NST; ++st)
         hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd_operand<-1>(read_v(vz, b, st)), weight_operand(st), hits, 0, 0, 0);
       add_odd<-1>(oacc[b], hits);
       __builtin_amdgcn_sched_barrier(0);
@@ -536,10 +540,34 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     second_barrier(t);
     find_next(t);
   }
-  if (!wvalid) return;
   lrun += xor32(lrun);
+  if constexpr (KH == 2) {
+    // the waves of key half 1 hand (reference, sum, O) to those of half 0, each
+    // relative to its own reference
+    float* part = reinterpret_cast<float*>(&s_kv[0][0][0]) + (wave & 3) * 66 * 64;
+    __syncthreads();  // every wave is done with the tiles
+    if (kh == 1) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) part[(b * 16 + i) * 64 + lane] = oacc[b][i];
+      part[64 * 64 + lane] = mref;
+      part[65 * 64 + lane] = lrun;
+    }
+    __syncthreads();
+    if (kh == 1) return;
+    const float m2 = part[64 * 64 + lane], M = fmaxf(mref, m2);
+    const float w1 = __builtin_amdgcn_exp2f(mref - M), w2 = __builtin_amdgcn_exp2f(m2 - M);
+    lrun = lrun * w1 + part[65 * 64 + lane] * w2;
+    mref = M;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) oacc[b][i] = oacc[b][i] * w1 + part[(b * 16 + i) * 64 + lane] * w2;
+  }
+  if (!wvalid) return;
   if (nsp > 1) {
-    const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * EX_ROWS + wave * 32 + m;
+    const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * ROWS + (r - it.row0);
     if (rvalid) {
 #pragma unroll
       for (int b = 0; b < 4; ++b)
@@ -1234,12 +1262,17 @@ hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t s
     if (paged) hipLaunchKernelGGL((k_exact_f32<1>), dim3(items), dim3(EX_W32 * 64), 0, st, a);
     else hipLaunchKernelGGL((k_exact_f32<0>), dim3(items), dim3(EX_W32 * 64), 0, st, a);
   } else {
-    if (paged) hipLaunchKernelGGL((k_exact_bf16<1>), dim3(items), dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((k_exact_bf16<0>), dim3(items), dim3(512), 0, st, a);
+    const bool half = a.rows == EX_ROWS / 2;
+    if (paged && half) hipLaunchKernelGGL((k_exact_bf16<1, 2>), dim3(items), dim3(512), 0, st, a);
+    else if (paged) hipLaunchKernelGGL((k_exact_bf16<1, 1>), dim3(items), dim3(512), 0, st, a);
+    else if (half) hipLaunchKernelGGL((k_exact_bf16<0, 2>), dim3(items), dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_bf16<0, 1>), dim3(items), dim3(512), 0, st, a);
   }
   if (a.splits > 1) {
-    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), dim3(a.Hkv * a.blocks * (EX_ROWS_F32 / EJ_ROWS)), dim3(EJ_ROWS * 32), 0, st, a);
-    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), dim3(a.Hkv * a.blocks * (EX_ROWS / EJ_ROWS)), dim3(EJ_ROWS * 32), 0, st, a);
+    const dim3 wgs(a.Hkv * a.blocks * (a.rows / EJ_ROWS)), threads(EJ_ROWS * 32);
+    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), wgs, threads, 0, st, a);
+    else if (a.rows == EX_ROWS) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), wgs, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2>), wgs, threads, 0, st, a);
   }
   return hipGetLastError();
 }
