@@ -160,14 +160,17 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   a.shift = log2i(p->pages.page_size);
   a.num_pages = p->pages.num_pages;
   const bool fp32 = h.dtype == PROTOKV_KV_FP32;
-  if (!fp32) {  // requests of few rows go to a kernel of their own, the others to row blocks
+  // requests of few rows go to a kernel of their own, the others to row blocks (a
+  // single request that may have more rows is left to them)
+  const bool many = (int64_t)a.max_add * a.grp > EX_FEW;
+  if (!fp32 && !(many && a.n == 1)) {
     const int64_t tiles = (((int64_t)a.stride << a.shift) + 31) / 32;
     const int64_t waves = std::max<int64_t>(1, ((int64_t)a.Hkv * a.n * tiles + EX_FEW_TILES - 1) / EX_FEW_TILES);
     a.few = a.n ? (int)std::min<int64_t>(EX_FEW_WAVES, (waves + 3) / 4 * 4) : 0;
     a.few_rows = (int)std::min<int64_t>(EX_FEW, (int64_t)a.max_add * a.grp);
   }
   a.splits = 1;
-  if (fp32 || (int64_t)a.max_add * a.grp > EX_FEW) plan_blocks(a, fp32, true);
+  if (fp32 || many) plan_blocks(a, fp32, true);
   if ((int64_t)a.blocks * a.Hkv * a.splits * 8 >= (1ll << 31))
     return fail(PROTOKV_E_UNSUPPORTED, who, "too many row blocks for one launch");
   return PROTOKV_OK;

@@ -53,15 +53,21 @@ __device__ __forceinline__ bool find_item(const ExactArgs& a, int b, Item& it) {
   const int lane = threadIdx.x & 63;
   auto entry = [&](int i) { return min(max(a.cu[i], 0), a.total); };
   auto first = [&](int c, int i) { return (int)((unsigned)(c * a.grp) / R) + i; };
-  int lo = 0, hi = a.n;
-  while (hi - lo > 1) {
+  int lo = 0, hi = a.n, c0, c1;
+  for (;;) {
     const int step = (hi - lo + 63) / 64, i = lo + lane * step;
-    const bool in = i < hi && first(entry(min(i, a.n)), i) <= b;
-    lo += (max(__popcll(__ballot(in)), 1) - 1) * step;
+    const int c = entry(min(i, a.n));
+    const bool in = i < hi && first(c, i) <= b;
+    const int l = max(__popcll(__ballot(in)), 1) - 1;
+    if (step == 1) {  // lane l has the entry, the next lane the one behind it
+      c0 = __builtin_amdgcn_readlane(c, l);
+      lo = __builtin_amdgcn_readfirstlane(lo + l);
+      c1 = l < 63 ? __builtin_amdgcn_readlane(c, l + 1) : __builtin_amdgcn_readfirstlane(entry(lo + 1));
+      break;
+    }
+    lo += l * step;
     hi = min(hi, lo + step);
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  const int c0 = __builtin_amdgcn_readfirstlane(entry(lo)), c1 = __builtin_amdgcn_readfirstlane(entry(lo + 1));
   const int blk = b - first(c0, lo);
   it.seq = lo;
   it.s0 = c0;
@@ -226,11 +232,6 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   const int wend = it.off + wtok1 + 1;   // keys that some row of it sees
 
   bf16x8 bq[8];
-  {
-    const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(it.s0 + tok) * a.qs + head * (D * 2));
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[2 * kk + half]);
-  }
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   f32x16 oacc[4] = {zero, zero, zero, zero};
   // (a row's first reference is its first tile's maximum, so a row with one key
@@ -472,12 +473,18 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     if (t0 < t1) load_ids(t0);
     if ((t0 + 3) / tpc != t0 / tpc && t0 + 3 < t1) load_ids(t0 + 3);
   }
-  wait_vm<0>();  // the query operands are in registers before any tile is in flight
   ex_barrier();
-  for (int t = t0; t < t0 + 3 && t < t1; ++t) {
-    if (t < t0 + 2) issue(t);
-    else locate(t);
+  // the first tile and the query together, the second tile once they are there: what
+  // the compiler waits for knows of no tile
+  if (t0 < t1) issue(t0);
+  {
+    const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(it.s0 + tok) * a.qs + head * (D * 2));
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[2 * kk + half]);
   }
+  wait_vm<0>();
+  if (t0 + 1 < t1) issue(t0 + 1);
+  if (t0 + 2 < t1) locate(t0 + 2);
   // Waves w and w + 4 share a SIMD.  In period t waves 0 - 3 form the products of tile
   // t, then its weights, and waves 4 - 7 the weights of tile t - 1, then the products
   // of tile t, so that one wave of a SIMD has the matrix core while the other has the
@@ -963,9 +970,11 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   // total tiles and this wave's run: lane l sums the requests of the l-th of 64 blocks
   const int per64 = (a.n + 63) / 64;
   long long mine = 0;
+  Few q{};
   for (int j = 0; j < per64; ++j) {
     const int i = lane * per64 + j;
-    if (i < a.n) mine += few_of(a, i).tiles;
+    if (i < a.n) q = few_of(a, i);
+    mine += i < a.n ? q.tiles : 0;
   }
   long long upto = wave_sum(mine);
   const long long N = lane_ll(upto, 63) * a.Hkv;
@@ -975,12 +984,12 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   long long x = w * per;
   if (lane == 0) meta[0] = 0;
   if (x >= N) return;  // uniform, and nothing below synchronises waves
-  int i0;               // first request of the 64 in the lanes
-  long long before;     // tiles before it
-  {
-    const int l = __popcll(__ballot((upto - mine) * a.Hkv <= x)) - 1;
-    i0 = __builtin_amdgcn_readfirstlane(l) * per64;
-    before = lane_ll(upto - mine, __builtin_amdgcn_readfirstlane(l));
+  int i0 = 0;            // first request of the 64 in the lanes
+  long long before = 0;  // tiles before it
+  if (per64 > 1) {
+    const int l = __builtin_amdgcn_readfirstlane(__popcll(__ballot((upto - mine) * a.Hkv <= x)) - 1);
+    i0 = l * per64;
+    before = lane_ll(upto - mine, l);
   }
   const uint8_t* kb = (const uint8_t*)a.k;
   const uint8_t* vb = (const uint8_t*)a.v;
@@ -1165,8 +1174,10 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   };
 
   while (x < x1) {
-    Few q{};
-    if (i0 + lane < a.n) q = few_of(a, i0 + lane);
+    if (per64 > 1) {  // else the lanes have them
+      q = Few{};
+      if (i0 + lane < a.n) q = few_of(a, i0 + lane);
+    }
     const long long incl = wave_sum(q.tiles), excl = incl - q.tiles;
     const long long all = before + lane_ll(incl, 63);
     while (x < x1 && x < all * a.Hkv) {

@@ -109,31 +109,42 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
 // PL_MAX, which no valid total reaches.
 // ---------------------------------------------------------------------------
 constexpr int PL_MAX = (1 << 30) - 1;  // two of them fit an int
-constexpr int PL_THREADS = 1024;
 
 __device__ __forceinline__ int sat_add(int x, int y) { return min(x + y, PL_MAX); }
 
-// Inclusive running sum over the workgroup's threads of x (0 <= x <= PL_MAX);
-// total: the sum of all.  Two barriers; s: 16 words.
-__device__ __forceinline__ int block_sum(int x, int* s, int& total) {
+// Inclusive running sums over the workgroup's threads of x and y (each 0 ..
+// PL_MAX); tx, ty: of all.  s: 2 NT / 64 words, free again two calls later with
+// another one in between.  One barrier.
+template <int NT>
+__device__ __forceinline__ void block_sums(int& x, int& y, int* s, int& tx, int& ty) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_up(x, d, 64);
-    if (lane >= d) x = sat_add(x, y);
+    const int u = __shfl_up(x, d, 64), v = __shfl_up(y, d, 64);
+    if (lane >= d) {
+      x = sat_add(x, u);
+      y = sat_add(y, v);
+    }
   }
-  if (lane == 63) s[wave] = x;
+  if (lane == 63) {
+    s[2 * wave] = x;
+    s[2 * wave + 1] = y;
+  }
   __syncthreads();
-  int before = 0;
-  total = 0;
+  int bx = 0, by = 0;
+  tx = ty = 0;
 #pragma unroll
-  for (int w = 0; w < PL_THREADS / 64; ++w) {
-    const int y = s[w];
-    if (w < wave) before = sat_add(before, y);
-    total = sat_add(total, y);
+  for (int w = 0; w < NT / 64; ++w) {
+    const int u = s[2 * w], v = s[2 * w + 1];
+    if (w < wave) {
+      bx = sat_add(bx, u);
+      by = sat_add(by, v);
+    }
+    tx = sat_add(tx, u);
+    ty = sat_add(ty, v);
   }
-  __syncthreads();  // s is free again
-  return sat_add(before, x);
+  x = sat_add(bx, x);
+  y = sat_add(by, y);
 }
 
 // Largest i in [0, n) with s[i] <= x (s non-decreasing, s[0] <= x).
@@ -147,44 +158,55 @@ __device__ __forceinline__ int find_at(const int* s, int n, int x) {
   return lo;
 }
 
-template <int NMAX>
-__global__ __launch_bounds__(PL_THREADS) void k_page_plan(protokv_page_plan_args a, int shift) {
+// NMAX: requests at most; KEEP: their lengths stay in LDS (else they are read anew).
+template <int NMAX, int NT, bool KEEP>
+__global__ __launch_bounds__(NT) void k_page_plan(protokv_page_plan_args a, int shift) {
   __shared__ int s_row[NMAX + 1];   // first row
   __shared__ int s_back[NMAX + 1];  // pages given back before request i
   __shared__ int s_take[NMAX + 1];  // pages asked for before request i
-  __shared__ int s_sum[PL_THREADS / 64];
+  __shared__ int s_ctx[KEEP ? NMAX : 1], s_add[KEEP ? NMAX : 1];
+  __shared__ int s_sum[3][2 * NT / 64];
   const int tid = threadIdx.x, n = a.num_requests, P1 = (1 << shift) - 1;
   const int span = a.table_stride << shift;  // tokens of a table row
   const int free0 = min(max(a.free_count[0], 0), a.num_pages);
-  auto ctx_of = [&](int i) { return min(max(a.ctx[i], 0), span); };
+  auto read_ctx = [&](int i) { return min(max(a.ctx[i], 0), span); };
+  auto ctx_of = [&](int i) { return KEEP ? s_ctx[i] : read_ctx(i); };
+  auto add_of = [&](int i) { return KEEP ? s_add[i] : a.add[i]; };
   auto pages_of = [&](long long x) { return (int)((x + P1) >> shift); };
-  // pages that request i lacks, or -1 if it cannot be granted whatever the stack holds
+  // pages that a request lacks, or -1 if it cannot be granted whatever the stack holds
   auto lacks = [&](int ctx, int add, int end) {
     if ((long long)ctx + add > span || end > a.max_tokens) return -1;
     return pages_of((long long)ctx + add) - pages_of(ctx);
   };
-  int rows = 0, back = 0, take = 0;  // of the requests so far
-  for (int i0 = 0; i0 < n; i0 += PL_THREADS) {
+  int rows = 0, back = 0, take = 0, turn = 0;  // of the requests so far
+  for (int i0 = 0; i0 < n; i0 += NT) {
     const int i = i0 + tid;
     int add = 0, ctx = 0;
     if (i < n) {
       add = a.add[i];
-      ctx = ctx_of(i);
+      ctx = read_ctx(i);
     }
-    int total;
-    const int mine = min(max(add, 0), PL_MAX);
-    const int end = sat_add(rows, block_sum(mine, s_sum, total));
-    rows = sat_add(rows, total);
-    const int give = add < 0 ? pages_of(ctx) : 0;
-    const int gave = sat_add(back, block_sum(give, s_sum, total));
-    back = sat_add(back, total);
-    const int need = add > 0 ? max(lacks(ctx, add, end), 0) : 0;
-    const int upto = sat_add(take, block_sum(need, s_sum, total));
-    take = sat_add(take, total);
+    int tx, ty;
+    int end = min(max(add, 0), PL_MAX), gave = add < 0 ? pages_of(ctx) : 0;
+    block_sums<NT>(end, gave, s_sum[turn], tx, ty);
+    turn = turn == 2 ? 0 : turn + 1;
+    end = sat_add(rows, end);
+    gave = sat_add(back, gave);
+    rows = sat_add(rows, tx);
+    back = sat_add(back, ty);
+    int upto = add > 0 ? max(lacks(ctx, add, end), 0) : 0, none = 0;
+    block_sums<NT>(upto, none, s_sum[turn], tx, ty);
+    turn = turn == 2 ? 0 : turn + 1;
+    upto = sat_add(take, upto);
+    take = sat_add(take, tx);
     if (i < n) {
       s_row[i + 1] = end;
       s_back[i + 1] = gave;
       s_take[i + 1] = upto;
+      if constexpr (KEEP) {
+        s_ctx[i] = ctx;
+        s_add[i] = add;
+      }
     }
   }
   if (tid == 0) s_row[0] = s_back[0] = s_take[0] = 0;
@@ -205,17 +227,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_page_plan(protokv_page_plan_args
   // page j of request i, which lacks the pages from `held` on
   auto taken = [&](int i, int j, int held) { return stacked(nfree - 1 - (s_take[i] + j - held)); };
 
-  const int gid = blockIdx.x * PL_THREADS + tid, gsize = gridDim.x * PL_THREADS;
-  // pages given back
-  for (int x = gid; x < nfree - free0; x += gsize) a.free_pages[free0 + x] = stacked(free0 + x);
-  // pages taken
-  for (int x = gid; x < min(take, nfree); x += gsize) {
-    const int i = find_at(s_take, n, x);
-    const int ctx = ctx_of(i), held = pages_of(ctx);
-    if (!granted(i, ctx, a.add[i])) continue;
-    const int j = held + x - s_take[i];
-    a.table[(size_t)i * a.table_stride + j] = taken(i, j, held);
-  }
+  const int gid = blockIdx.x * NT + tid, gsize = gridDim.x * NT;
   // rows
   for (int t = gid; t < a.max_tokens; t += gsize) {
     int slot = -1, pos = 0;
@@ -224,7 +236,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_page_plan(protokv_page_plan_args
       const int ctx = ctx_of(i), held = pages_of(ctx);
       const long long p = (long long)ctx + (t - s_row[i]);
       pos = (int)(p + (a.base ? a.base[i] : 0));
-      if (granted(i, ctx, a.add[i])) {
+      if (granted(i, ctx, add_of(i))) {
         const int j = (int)(p >> shift);
         const int page = j < held ? a.table[(size_t)i * a.table_stride + j] : taken(i, j, held);
         if ((unsigned)page < (unsigned)a.num_pages) slot = (page << shift) + (int)(p & P1);
@@ -233,36 +245,40 @@ __global__ __launch_bounds__(PL_THREADS) void k_page_plan(protokv_page_plan_args
     a.slots[t] = slot;
     if (a.positions) a.positions[t] = pos;
   }
-  if (blockIdx.x != 0) return;
-  // lengths; the pages of the granted requests and the count of the others
-  int used = 0, refused = 0;
-  for (int i0 = 0; i0 < n; i0 += PL_THREADS) {
-    const int i = i0 + tid;
-    int bad = 0, total;
-    if (i < n) {
-      const int ctx = ctx_of(i), add = a.add[i];
-      const bool ok = granted(i, ctx, add);
-      a.kv_len[i] = ok ? ctx + add : 0;
-      a.cu[i + 1] = min(s_row[i + 1], a.max_tokens);
-      if (ok && s_take[i + 1] > s_take[i]) used = max(used, s_take[i + 1]);
-      bad = add > 0 && !ok;
-    }
-    block_sum(bad, s_sum, total);
-    refused += total;
+  // pages taken
+  for (int x = gid; x < min(take, nfree); x += gsize) {
+    const int i = find_at(s_take, n, x);
+    const int ctx = ctx_of(i), held = pages_of(ctx);
+    if (!granted(i, ctx, add_of(i))) continue;
+    const int j = held + x - s_take[i];
+    a.table[(size_t)i * a.table_stride + j] = taken(i, j, held);
   }
-  // pages are granted from the front: the largest running sum of a granted request
-  // with pages of its own
-  int most = 0;
+  // pages given back
+  for (int x = gid; x < nfree - free0; x += gsize) a.free_pages[free0 + x] = stacked(free0 + x);
+  if (blockIdx.x != 0) return;
+  // lengths; the pages of the granted requests and the count of the others.  Pages
+  // are granted from the front: the largest running sum of a granted request with
+  // pages of its own.
+  __syncthreads();  // s_sum is free
+  int* s_end = s_sum[0];
+  if (tid < 2) s_end[tid] = 0;
   __syncthreads();
-  s_sum[tid & 15] = 0;
+  int used = 0, refused = 0;
+  for (int i = tid; i < n; i += NT) {
+    const int ctx = ctx_of(i), add = add_of(i);
+    const bool ok = granted(i, ctx, add);
+    a.kv_len[i] = ok ? ctx + add : 0;
+    a.cu[i + 1] = min(s_row[i + 1], a.max_tokens);
+    if (ok && s_take[i + 1] > s_take[i]) used = max(used, s_take[i + 1]);
+    refused += add > 0 && !ok;
+  }
+  if (used) atomicMax(&s_end[0], used);
+  if (refused) atomicAdd(&s_end[1], refused);
   __syncthreads();
-  atomicMax(&s_sum[0], min(used, nfree));
-  __syncthreads();
-  most = s_sum[0];
   if (tid == 0) {
     a.cu[0] = 0;
-    a.free_count_out[0] = nfree - most;
-    if (a.refused) a.refused[0] = refused;
+    a.free_count_out[0] = nfree - s_end[0];
+    if (a.refused) a.refused[0] = s_end[1];
   }
 }
 
@@ -282,11 +298,18 @@ hipError_t launch_rotate(const RotateArgs& a0, bool fp32, hipStream_t st) {
 
 hipError_t launch_page_plan(const protokv_page_plan_args& a, hipStream_t st) {
   const int shift = 31 - __builtin_clz((unsigned)a.page_size);
-  // four rows a thread, at most 64 workgroups
-  const long long work = (long long)a.max_tokens / (4 * PL_THREADS) + 1;
-  const unsigned blocks = (unsigned)(work < 64 ? work : 64);
-  if (a.num_requests <= 1024) hipLaunchKernelGGL((k_page_plan<1024>), dim3(blocks), dim3(PL_THREADS), 0, st, a, shift);
-  else hipLaunchKernelGGL((k_page_plan<MAX_REQUESTS>), dim3(blocks), dim3(PL_THREADS), 0, st, a, shift);
+  // a row a thread, at most 64 workgroups (each forms the sums of all requests); a
+  // small workgroup's barriers for few requests
+  auto blocks = [&](int threads) {
+    const long long b = ((long long)a.max_tokens + threads - 1) / threads;
+    return dim3((unsigned)(b < 64 ? b : 64));
+  };
+  if (a.num_requests <= 256)
+    hipLaunchKernelGGL((k_page_plan<256, 256, true>), blocks(256), dim3(256), 0, st, a, shift);
+  else if (a.num_requests <= 2048)
+    hipLaunchKernelGGL((k_page_plan<2048, 1024, true>), blocks(1024), dim3(1024), 0, st, a, shift);
+  else
+    hipLaunchKernelGGL((k_page_plan<MAX_REQUESTS, 1024, false>), blocks(1024), dim3(1024), 0, st, a, shift);
   return hipGetLastError();
 }
 

@@ -467,85 +467,93 @@ class ProtoKV:
 
 
 # -- exact attention around the readout (no handle) ---------------------------
+# One token's call takes a few microseconds on the GPU, so what these do in Python
+# counts: each tensor is looked at once.
 
 
-def _rows(t, name, dtype=None):
+def _device(t, stream) -> int:
+    """The current device, which a call's tensors and its stream must be on."""
+    import torch
+    d = t.get_device()
+    if d < 0:
+        raise ValueError("expected CUDA tensors")
+    if d != torch.cuda.current_device() or (stream is not None and stream.device_index != d):
+        raise ValueError(f"the tensors are on cuda:{d}; they and the stream must be on the current device")
+    return d
+
+
+def _raw_stream(stream, dev: int) -> int:
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _kv(dtype) -> int:
+    import torch
+    if dtype == torch.bfloat16:
+        return KV_BF16
+    if dtype == torch.float32:
+        return KV_FP32
+    raise ValueError(f"expected bfloat16 or float32, got {dtype}")
+
+
+def _rows(t, name, dtype=None, dev=None):
     """-> (pointer, row stride in elements) of token rows [N][heads][D]."""
-    import torch
-    if t.dim() != 3 or t.shape[2] != 128 or not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or (
-            dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name}: expected CUDA rows [N, heads, 128] in {dtype or 'bfloat16 or float32'}")
-    n, heads, _ = t.shape
-    if n > 0 and ((t.stride(2) != 1) or (heads > 1 and t.stride(1) != 128)):
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != 128 or (dtype is not None and t.dtype != dtype) or (
+            dev is not None and t.get_device() != dev):
+        raise ValueError(f"{name}: expected rows [N, heads, 128] in {dtype} on the current device, got "
+                         f"{t.dtype} {tuple(shape)} on {t.device}")
+    s0, s1, s2 = t.stride()
+    if shape[0] > 0 and (s2 != 1 or (shape[1] > 1 and s1 != 128)):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    return t.data_ptr(), t.stride(0) if n > 1 else heads * 128
+    return t.data_ptr(), s0 if shape[0] > 1 else shape[1] * 128
 
 
-def _ints(t, name, *shape):
-    """Pointer of a contiguous int32 CUDA tensor (None stays None)."""
-    import torch
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected a contiguous int32 CUDA tensor {shape}, got {t.dtype} {tuple(t.shape)}")
+def _flat(t, name, dtype, dev, *shape) -> int:
+    """Pointer of a contiguous tensor of that type and shape."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {shape} on the current device, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _here(*tensors):
-    """Refuses tensors of another device than the current one, where the call will run."""
-    import torch
-    d = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t is not False and t.device.index != d:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{d}")
-
-
-def _pages(pages, dtype, kv_heads):
+def _pages(pages, dtype, dev, kv_heads) -> Pages:
     """Pages of (k, v) [num_pages][kv heads][page size][D]."""
     k, v = pages
-    if k.dim() != 4 or k.shape != v.shape or k.shape[1] != kv_heads or k.shape[3] != 128:
+    shape = k.shape
+    if len(shape) != 4 or shape[1] != kv_heads or shape[3] != 128:
         raise ValueError(f"pages: expected k and v [num_pages, {kv_heads}, page_size, 128]")
-    for t in (k, v):
-        if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-            raise ValueError(f"pages: expected contiguous {dtype} CUDA tensors")
-    return Pages(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2])
+    return Pages(_flat(k, "pages", dtype, dev, *shape), _flat(v, "pages", dtype, dev, *shape), shape[0], shape[2])
 
 
-def _new(shape, dtype, like, stream):
+def _new(shape, dtype, dev, stream):
     """A tensor for a call on `stream`: allocated there, so that its memory is not
     reused before that stream's work is done."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    if stream.device.index != torch.cuda.current_device():
-        raise ValueError(f"the stream is on {stream.device}, not on the current device")
+        return torch.empty(shape, dtype=dtype, device=dev)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return torch.empty(shape, dtype=dtype, device=dev)
 
 
-def _result(q, out, lse, prior, stream):
-    """Outputs [N][Hq][D] and [N][Hq] (made where not given; lse=False: none) and the prior's pointers."""
+def _result(a, q, out, lse, prior, dev, stream):
+    """Outputs [N][Hq][D] and [N][Hq] (made where not given; lse=False: none) and the prior into a."""
     import torch
     n, hq, _ = q.shape
     if out is None:
-        out = _new((n, hq, 128), q.dtype, q, stream)
+        out = _new((n, hq, 128), q.dtype, dev, stream)
+        a.o = out.data_ptr()
+    else:
+        a.o = _flat(out, "out", q.dtype, dev, n, hq, 128)
     if lse is None:
-        lse = _new((n, hq), torch.float32, q, stream)
-    po, pl = prior if prior is not None else (None, None)
-    for t, name in ((out, "out"), (po, "prior")):
-        if t is not None and (tuple(t.shape) != (n, hq, 128) or t.dtype != q.dtype or not t.is_contiguous()):
-            raise ValueError(f"{name}: expected a contiguous {q.dtype} tensor {(n, hq, 128)}")
-    for t, name in ((lse, "lse"), (pl, "prior lse")):
-        if t is not None and t is not False and (
-                tuple(t.shape) != (n, hq) or t.dtype != torch.float32 or not t.is_contiguous()):
-            raise ValueError(f"{name}: expected a contiguous float32 tensor {(n, hq)}")
-    _here(q, out, lse, po, pl)
-    return out, lse, po.data_ptr() if po is not None else None, pl.data_ptr() if pl is not None else None
-
-
-def _kv(t):
-    import torch
-    return KV_FP32 if t.dtype == torch.float32 else KV_BF16
+        lse = _new((n, hq), torch.float32, dev, stream)
+        a.lse = lse.data_ptr()
+    elif lse is not False:
+        a.lse = _flat(lse, "lse", torch.float32, dev, n, hq)
+    if prior is not None:
+        a.prior_o = _flat(prior[0], "prior", q.dtype, dev, n, hq, 128)
+        a.prior_lse = _flat(prior[1], "prior lse", torch.float32, dev, n, hq)
+    return out, lse
 
 
 def pair_axes(sections: Sequence[int], interleaved: bool = False) -> bytes:
@@ -556,14 +564,14 @@ def pair_axes(sections: Sequence[int], interleaved: bool = False) -> bytes:
     if not 1 <= len(left) <= 8 or min(left) < 0 or sum(left) != 64:
         raise ValueError("pair_axes: 1 to 8 sections of 64 pairs in all")
     if not interleaved:
-        return bytes(a for a, n in enumerate(left) for _ in range(n))
-    out = []
+        return b"".join(bytes((a,)) * n for a, n in enumerate(left))
+    out, dealt = b"", 0
     while len(out) < 64:
-        for a, n in enumerate(left):
-            if n:
-                left[a] = n - 1
-                out.append(a)
-    return bytes(out)
+        live = [a for a, n in enumerate(left) if n > dealt]
+        rounds = min(left[a] for a in live) - dealt
+        out += bytes(live) * rounds
+        dealt += rounds
+    return out
 
 
 def rotate(q, k, positions, axes: bytes, theta: float, *, q_out=None, k_out=None, v=None, pages=None, slots=None,
@@ -573,50 +581,58 @@ def rotate(q, k, positions, axes: bytes, theta: float, *, q_out=None, k_out=None
     the same), axes from ``pair_axes``.  With pages=(k, v) tensors [num_pages][Hkv]
     [page_size][D] and slots int32 [N] the turned keys and v's rows are stored, and
     k_out is written only if given.  -> (q_out, k_out)"""
+    import torch
     some = q if q is not None else k
     if some is None:
         raise ValueError("rotate: neither q nor k")
-    n, dtype = some.shape[0], some.dtype
+    dev, dtype, n = _device(some, stream), some.dtype, some.shape[0]
     a = RotateArgs()
-    a.num_tokens, a.head_dim, a.kv_dtype = n, 128, _kv(some)
-    a.num_kv_heads = k.shape[1] if k is not None else 1
-    a.num_q_heads = q.shape[1] if q is not None else a.num_kv_heads
+    a.num_tokens, a.head_dim, a.kv_dtype = n, 128, _kv(dtype)
+    hk = a.num_kv_heads = k.shape[1] if k is not None else 1
+    a.num_q_heads = q.shape[1] if q is not None else hk
     if not isinstance(axes, bytes) or len(axes) != 64:
         raise ValueError("rotate: axes are 64 bytes (pair_axes)")
-    a.num_axes, a.axes, a.theta = max(axes) + 1, axes, theta
+    num_axes = a.num_axes = max(axes) + 1
+    a.axes, a.theta = axes, theta
     if positions.dim() == 1:
-        a.positions, a.position_stride = _ints(positions, "positions", n), 0
+        a.positions = _flat(positions, "positions", torch.int32, dev, n)
     else:
-        if positions.shape[0] < a.num_axes:
+        if positions.shape[0] < num_axes:
             raise ValueError("rotate: positions has fewer axes than axes names")
-        a.positions, a.position_stride = _ints(positions, "positions", positions.shape[0], n), n
+        a.positions, a.position_stride = _flat(positions, "positions", torch.int32, dev, positions.shape[0], n), n
     if q is not None:
-        a.q, a.q_stride = _rows(q, "q", dtype)
+        a.q, a.q_stride = _rows(q, "q", dtype, dev)
         if q_out is None:
-            q_out = _new(tuple(q.shape), dtype, q, stream)
-        elif q_out.shape != q.shape:
-            raise ValueError("rotate: q_out must have q's shape")
-        a.q_out, a.q_out_stride = _rows(q_out, "q_out", dtype)
+            q_out = _new((n, a.num_q_heads, 128), dtype, dev, stream)
+            a.q_out, a.q_out_stride = q_out.data_ptr(), a.num_q_heads * 128
+        else:
+            if q_out.shape != q.shape:
+                raise ValueError("rotate: q_out must have q's shape")
+            a.q_out, a.q_out_stride = _rows(q_out, "q_out", dtype, dev)
+    elif q_out is not None:
+        raise ValueError("rotate: q_out without q")
     if k is not None:
         if k.shape[0] != n:
             raise ValueError("rotate: q and k must have the same rows")
-        a.k, a.k_stride = _rows(k, "k", dtype)
+        a.k, a.k_stride = _rows(k, "k", dtype, dev)
         if k_out is None and pages is None:
-            k_out = _new(tuple(k.shape), dtype, k, stream)
+            k_out = _new((n, hk, 128), dtype, dev, stream)
         if k_out is not None:
             if k_out.shape != k.shape:
                 raise ValueError("rotate: k_out must have k's shape")
-            a.k_out, a.k_out_stride = _rows(k_out, "k_out", dtype)
+            a.k_out, a.k_out_stride = _rows(k_out, "k_out", dtype, dev)
+    elif k_out is not None:
+        raise ValueError("rotate: k_out without k")
     if pages is not None:
         if k is None or v is None or slots is None or v.shape != k.shape:
             raise ValueError("rotate: pages take k, v of its shape, and slots")
-        a.v, a.v_stride = _rows(v, "v", dtype)
-        p = _pages(pages, dtype, k.shape[1])
+        a.v, a.v_stride = _rows(v, "v", dtype, dev)
+        p = _pages(pages, dtype, dev, hk)
         a.pages = ctypes.pointer(p)
-        a.slots = _ints(slots, "slots", n)
-        _here(v, slots, *pages)
-    _here(q, k, positions, q_out, k_out)
-    _check(lib().protokv_rotate(ctypes.byref(a), _stream_ptr(stream)))
+        a.slots = _flat(slots, "slots", torch.int32, dev, n)
+    elif v is not None or slots is not None:
+        raise ValueError("rotate: v and slots need pages")
+    _check(lib().protokv_rotate(ctypes.byref(a), _raw_stream(stream, dev)))
     return q_out, k_out
 
 
@@ -631,20 +647,26 @@ def page_plan(ctx, add, table, free_pages, count, page_size: int, max_tokens: in
     """protokv_page_plan: one step's slots, positions and lengths from the requests'
     held (ctx) and new (add, < 0: over) tokens, int32 [n]; table int32 [n][width] and
     the stack free_pages [num_pages] are updated in place, count [1] is not
-    (count_out or a new tensor holds the pages left)."""
+    (count_out or a new tensor holds the pages left).  The results are parts of one
+    new tensor."""
     import torch
-    n = ctx.shape[0]
+    dev, i32, n = _device(ctx, stream), torch.int32, ctx.shape[0]
+    if max_tokens < 1:
+        raise ValueError("page_plan: max_tokens must be >= 1")
     out = PagePlan()
-    new = lambda m: _new(m, torch.int32, ctx, stream)  # noqa: E731
-    out.cu, out.kv_len, out.slots, out.positions, out.refused = new(n + 1), new(n), new(max_tokens), new(max_tokens), new(1)
-    out.count = new(1) if count_out is None else count_out
-    _here(ctx, add, table, free_pages, count, base, out.count)
-    a = PagePlanArgs(n, free_pages.shape[0], page_size, table.shape[1], max_tokens, _ints(ctx, "ctx", n),
-                     _ints(add, "add", n), _ints(base, "base", n), _ints(table, "table", n, table.shape[1]),
-                     _ints(free_pages, "free_pages", free_pages.shape[0]), _ints(count, "count", 1),
-                     _ints(out.count, "count_out", 1), out.cu.data_ptr(), out.kv_len.data_ptr(), out.slots.data_ptr(),
-                     out.positions.data_ptr(), out.refused.data_ptr())
-    _check(lib().protokv_page_plan(ctypes.byref(a), _stream_ptr(stream)))
+    out.cu, out.kv_len, out.slots, out.positions, out.refused, out.count = _new(
+        (2 * n + 2 * max_tokens + 3,), i32, dev, stream).split((n + 1, n, max_tokens, max_tokens, 1, 1))
+    if count_out is not None:
+        out.count = count_out
+    width, pages = table.shape[1], free_pages.shape[0]
+    cu = out.cu.data_ptr()
+    a = PagePlanArgs(n, pages, page_size, width, max_tokens, _flat(ctx, "ctx", i32, dev, n),
+                     _flat(add, "add", i32, dev, n), None if base is None else _flat(base, "base", i32, dev, n),
+                     _flat(table, "table", i32, dev, n, width), _flat(free_pages, "free_pages", i32, dev, pages),
+                     _flat(count, "count", i32, dev, 1), _flat(out.count, "count_out", i32, dev, 1),
+                     cu, cu + 4 * (n + 1), cu + 4 * (2 * n + 1), cu + 4 * (2 * n + 1 + max_tokens),
+                     cu + 4 * (2 * n + 1 + 2 * max_tokens))
+    _check(lib().protokv_page_plan(ctypes.byref(a), _raw_stream(stream, dev)))
     return out
 
 
@@ -652,20 +674,20 @@ def prompt_attend(q, k, v, cu, *, out=None, lse=None, prior=None, stream=None):
     """protokv_prompt_attend on token rows q [N][Hq][D], k, v [N][Hkv][D] (rows may be
     strided) of the packed sequences cu int32 [n+1]; prior: (o, lse) of the same rows
     over other keys, joined with the result.  -> (o, lse); lse=False: none."""
+    import torch
+    dev, dtype = _device(q, stream), q.dtype
     a = PromptArgs()
-    a.q, a.q_stride = _rows(q, "q")
-    a.k, a.k_stride = _rows(k, "k", q.dtype)
-    a.v, a.v_stride = _rows(v, "v", q.dtype)
+    a.q, a.q_stride = _rows(q, "q", dtype, dev)
+    a.k, a.k_stride = _rows(k, "k", dtype, dev)
+    a.v, a.v_stride = _rows(v, "v", dtype, dev)
     if k.shape != v.shape or k.shape[0] != q.shape[0]:
         raise ValueError("prompt_attend: q, k and v must have the same rows, k and v the same heads")
     a.total, a.num_q_heads, _ = q.shape
-    a.num_kv_heads, a.head_dim, a.kv_dtype = k.shape[1], 128, _kv(q)
+    a.num_kv_heads, a.head_dim, a.kv_dtype = k.shape[1], 128, _kv(dtype)
     a.num_seqs = cu.shape[0] - 1
-    a.cu = _ints(cu, "cu", cu.shape[0])
-    out, lse, a.prior_o, a.prior_lse = _result(q, out, lse, prior, stream)
-    a.o, a.lse = out.data_ptr(), lse.data_ptr() if lse is not False else None
-    _here(k, v, cu)
-    _check(lib().protokv_prompt_attend(ctypes.byref(a), _stream_ptr(stream)))
+    a.cu = _flat(cu, "cu", torch.int32, dev, cu.shape[0])
+    out, lse = _result(a, q, out, lse, prior, dev, stream)
+    _check(lib().protokv_prompt_attend(ctypes.byref(a), _raw_stream(stream, dev)))
     return out, lse
 
 
@@ -676,24 +698,25 @@ def page_attend(q, pages, table, cu, kv_len, max_add: int, *, out=None, lse=None
     [page_size][D] by the block table [n][width].  workspace: a uint8 tensor (None: one
     of this call's own).  -> (o, lse); lse=False: none."""
     import torch
+    dev, dtype, i32 = _device(q, stream), q.dtype, torch.int32
     a = PageAttendArgs()
-    a.q, a.q_stride = _rows(q, "q")
+    a.q, a.q_stride = _rows(q, "q", dtype, dev)
     a.total, a.num_q_heads, _ = q.shape
-    a.num_kv_heads, a.head_dim, a.kv_dtype = pages[0].shape[1], 128, _kv(q)
-    a.pages = _pages(pages, q.dtype, a.num_kv_heads)
-    n = a.num_requests = cu.shape[0] - 1
-    a.max_add, a.table_stride = max_add, table.shape[1]
-    a.cu, a.kv_len = _ints(cu, "cu", n + 1), _ints(kv_len, "kv_len", n)
-    a.table = _ints(table, "table", n, table.shape[1])
-    out, lse, a.prior_o, a.prior_lse = _result(q, out, lse, prior, stream)
-    a.o, a.lse = out.data_ptr(), lse.data_ptr() if lse is not False else None
-    _here(cu, kv_len, table, workspace, *pages)
+    a.num_kv_heads, a.head_dim, a.kv_dtype = pages[0].shape[1], 128, _kv(dtype)
+    a.pages = _pages(pages, dtype, dev, a.num_kv_heads)
+    n, width = cu.shape[0] - 1, table.shape[1]
+    a.num_requests, a.max_add, a.table_stride = n, max_add, width
+    a.cu, a.kv_len = _flat(cu, "cu", i32, dev, n + 1), _flat(kv_len, "kv_len", i32, dev, n)
+    a.table = _flat(table, "table", i32, dev, n, width)
+    out, lse = _result(a, q, out, lse, prior, dev, stream)
     if workspace is None:
         need = ctypes.c_size_t()
         _check(lib().protokv_page_attend_workspace(ctypes.byref(a), ctypes.byref(need)))
         if need.value:
-            workspace = _new(need.value, torch.uint8, q, stream)
+            workspace = _new((need.value,), torch.uint8, dev, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor on the current device")
     if workspace is not None:
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(lib().protokv_page_attend(ctypes.byref(a), _stream_ptr(stream)))
+    _check(lib().protokv_page_attend(ctypes.byref(a), _raw_stream(stream, dev)))
     return out, lse
