@@ -8,6 +8,7 @@
 // packed: row r of a sequence is token r / grp, query head kvh * grp + r % grp,
 // so every key tile serves all heads of the group.
 #include <algorithm>
+#include <type_traits>
 
 #include "exact.h"
 #include "pkv_internal.h"
@@ -15,8 +16,6 @@
 namespace pkv {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
@@ -94,15 +93,13 @@ __device__ __forceinline__ int splits_of(const ExactArgs& a, int tiles, int& per
   return max(1, (tiles + per - 1) / per);
 }
 
-// Weights of a row's own result (log2 of its sum: own2) and of the prior's, and
-// the log-sum-exp of both.
+// Weights of a row's own result (log2 of its sum: own2) and of the prior's (its
+// log-sum-exp p), and the log-sum-exp of both.
 struct Join {
   float own, prior, lse;
 };
-__device__ __forceinline__ Join join_of(float own2, const float* pl, size_t row) {
+__device__ __forceinline__ Join join_of(float own2, float p) {
   const float own = own2 * EX_LN2;
-  if (!pl) return {1.f, 0.f, own};
-  const float p = pl[row];
   if (p == -INFINITY) return {1.f, 0.f, own};
   if (own == -INFINITY) return {0.f, 1.f, p};
   const float m = fmaxf(own, p);
@@ -110,30 +107,45 @@ __device__ __forceinline__ Join join_of(float own2, const float* pl, size_t row)
   return {e1 / s, e2 / s, m + logf(s)};
 }
 
-// Four dims from dim d on of output row `row`: own value x (normalised) joined.
-template <int FP32>
-__device__ __forceinline__ void store4(const ExactArgs& a, size_t row, int d, f32x4 x, const Join& j) {
-  const size_t e = row * D + d;
-  if (a.pl && j.prior != 0.f) {  // an unread prior may hold anything
-    f32x4 p;
+// Output row `row` from N pieces of four dims of this lane, piece i at dim(i) with
+// the own value x(i) (normalised): joined with the prior, whose loads go out
+// together (one after the other, each beside its store, they were a third of a
+// short prompt's time).  -> the row's log-sum-exp.
+template <int FP32, int N, typename X, typename DIM>
+__device__ __forceinline__ float write_row(const ExactArgs& a, size_t row, float own2, X x, DIM dim) {
+  typedef __bf16 half4 __attribute__((ext_vector_type(4)));
+  auto store = [&](int i, f32x4 v) {
+    const size_t e = row * D + dim(i);
     if constexpr (FP32) {
-      p = *reinterpret_cast<const f32x4*>((const float*)a.po + e);
+      *reinterpret_cast<f32x4*>((float*)a.o + e) = v;
     } else {
-      const bf16x4 b = *reinterpret_cast<const bf16x4*>((const __bf16*)a.po + e);
+      half4 b;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = (float)b[i];
+      for (int c = 0; c < 4; ++c) b[c] = (__bf16)v[c];
+      *reinterpret_cast<half4*>((__bf16*)a.o + e) = b;
     }
+  };
+  if (!a.pl) {  // uniform
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = j.own == 0.f ? p[i] * j.prior : fmaf(p[i], j.prior, x[i] * j.own);
+    for (int i = 0; i < N; ++i) store(i, x(i));
+    return own2 * EX_LN2;
   }
-  if constexpr (FP32) {
-    *reinterpret_cast<f32x4*>((float*)a.o + e) = x;
-  } else {
-    bf16x4 b;
+  std::conditional_t<FP32 != 0, f32x4, half4> p[N];
+  const float pl = a.pl[row];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = (__bf16)x[i];
-    *reinterpret_cast<bf16x4*>((__bf16*)a.o + e) = b;
+  for (int i = 0; i < N; ++i) p[i] = *(reinterpret_cast<decltype(&p[0])>(const_cast<void*>(a.po)) + (row * D + dim(i)) / 4);
+  const Join j = join_of(own2, pl);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    f32x4 v = x(i);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float q = (float)p[i][c] * j.prior;
+      v[c] = j.prior == 0.f ? v[c] : j.own == 0.f ? q : fmaf(v[c], j.own, q);  // what has no weight may be anything
+    }
+    store(i, v);
   }
+  return j.lse;
 }
 
 // A hidden key has weight 0, but 0 x inf and 0 x NaN are not 0.  Where a tile with
@@ -591,14 +603,14 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   }
   if (!rvalid) return;
   const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;  // no key: 0; a NaN stays one
-  const Join j = join_of(lrun == 0.f ? -INFINITY : mref + log2f(lrun), a.pl, orow);
-#pragma unroll
-  for (int b = 0; b < 4; ++b)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      store4<0>(a, orow, b * 32 + i * 8 + half * 4,
-                (f32x4){oacc[b][4 * i] * inv, oacc[b][4 * i + 1] * inv, oacc[b][4 * i + 2] * inv, oacc[b][4 * i + 3] * inv}, j);
-  if (half == 0 && a.lse) a.lse[orow] = j.lse;
+  const float lse = write_row<0, 16>(
+      a, orow, lrun == 0.f ? -INFINITY : mref + log2f(lrun),
+      [&](int i) {
+        const int b = i >> 2, e = 4 * (i & 3);
+        return (f32x4){oacc[b][e], oacc[b][e + 1], oacc[b][e + 2], oacc[b][e + 3]} * inv;
+      },
+      [&](int i) { return (i >> 2) * 32 + (i & 3) * 8 + half * 4; });
+  if (half == 0 && a.lse) a.lse[orow] = lse;
 }
 
 // float32: S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x2_f32.  One workgroup =
@@ -820,21 +832,23 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
     L += wgt[w] * s_part[w][65][lane];
   }
   const float inv = nsp > 1 ? 1.0f : L > 0.f || L != L ? 1.0f / L : 0.f;
-  Join j{1.f, 0.f, 0.f};
-  if (nsp == 1 && rvalid) j = join_of(L == 0.f ? -INFINITY : M + log2f(L), a.pl, orow);
   const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * EX_ROWS_F32 + m;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int i = 4 * wave + e, d = 4 * (8 * wave + 4 * half + e);
+  auto dim = [&](int e) { return 4 * (8 * wave + 4 * half + e); };
+  auto merged = [&](int e) {
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < EX_W32; ++w)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) o[b] += wgt[w] * s_part[w][b * 16 + i][lane];
+      for (int b = 0; b < 4; ++b) o[b] += wgt[w] * s_part[w][b * 16 + 4 * wave + e][lane];
+    return o * inv;
+  };
+  float lse = 0.f;
+  if (rvalid) {
     if (nsp > 1) {
-      if (rvalid) *reinterpret_cast<f32x4*>(a.part_o + pr * D + d) = o;
-    } else if (rvalid) {
-      store4<1>(a, orow, d, o * inv, j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<f32x4*>(a.part_o + pr * D + dim(e)) = merged(e);
+    } else {
+      lse = write_row<1, 4>(a, orow, L == 0.f ? -INFINITY : M + log2f(L), merged, dim);
     }
   }
   __syncthreads();  // every wave has read the prior's lse, which may be lse itself
@@ -843,7 +857,7 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
     a.part_ml[pr * 2] = M;
     a.part_ml[pr * 2 + 1] = L;
   } else if (a.lse) {
-    a.lse[orow] = j.lse;
+    a.lse[orow] = lse;
   }
 }
 
@@ -890,10 +904,10 @@ struct Sum {
   }
   template <int FP32>
   __device__ __forceinline__ void store(const ExactArgs& a, size_t orow, int d4) const {
-    const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
-    const Join j = join_of(l == 0.f ? -INFINITY : M + log2f(l), a.pl, orow);
-    store4<FP32>(a, orow, d4 * 4, o * inv, j);
-    if (d4 == 0 && a.lse) a.lse[orow] = j.lse;
+    const f32x4 x = o * (l > 0.f || l != l ? 1.0f / l : 0.f);
+    const float lse = write_row<FP32, 1>(a, orow, l == 0.f ? -INFINITY : M + log2f(l), [&](int) { return x; },
+                                         [&](int) { return 4 * d4; });
+    if (d4 == 0 && a.lse) a.lse[orow] = lse;
   }
 };
 
@@ -1150,14 +1164,14 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
     if (!rvalid) return;
     if (whole) {
       const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;
-      const Join j = join_of(lrun == 0.f ? -INFINITY : mref + log2f(lrun), a.pl, orow);
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          store4<0>(a, orow, b * 32 + e * 8 + half * 4,
-                    (f32x4){oacc[b][4 * e], oacc[b][4 * e + 1], oacc[b][4 * e + 2], oacc[b][4 * e + 3]} * inv, j);
-      if (half == 0 && a.lse) a.lse[orow] = j.lse;
+      const float lse = write_row<0, 16>(
+          a, orow, lrun == 0.f ? -INFINITY : mref + log2f(lrun),
+          [&](int i) {
+            const int b = i >> 2, e = 4 * (i & 3);
+            return (f32x4){oacc[b][e], oacc[b][e + 1], oacc[b][e + 2], oacc[b][e + 3]} * inv;
+          },
+          [&](int i) { return (i >> 2) * 32 + (i & 3) * 8 + half * 4; });
+      if (half == 0 && a.lse) a.lse[orow] = lse;
       return;
     }
     const size_t prow = ((size_t)w * 2 + slot) * a.few_rows + m;
