@@ -494,7 +494,14 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[2 * kk + half]);
   }
+  // the prior is brought near: its lse, and the line 128 half .. of its row
+  float pl = -INFINITY, near_o = 0.f;
+  if (a.pl && rvalid) {
+    pl = a.pl[orow];
+    near_o = *reinterpret_cast<const float*>((const uint8_t*)a.po + orow * (D * 2) + half * 128);
+  }
   wait_vm<0>();
+  asm volatile("" ::"v"(near_o));
   if (t0 + 1 < t1) issue(t0 + 1);
   if (t0 + 2 < t1) locate(t0 + 2);
   // Waves w and w + 4 share a SIMD.  In period t waves 0 - 3 form the products of tile
@@ -584,6 +591,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) oacc[b][i] = oacc[b][i] * w1 + part[(b * 16 + i) * 64 + lane] * w2;
   }
+  if constexpr (KH == 1) ex_barrier();  // every wave is done with the tiles
   if (!wvalid) return;
   if (nsp > 1) {
     const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * ROWS + (r - it.row0);
@@ -601,16 +609,50 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     }
     return;
   }
-  if (!rvalid) return;
-  const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;  // no key: 0; a NaN stays one
-  const float lse = write_row<0, 16>(
-      a, orow, lrun == 0.f ? -INFINITY : mref + log2f(lrun),
-      [&](int i) {
-        const int b = i >> 2, e = 4 * (i & 3);
-        return (f32x4){oacc[b][e], oacc[b][e + 1], oacc[b][e + 2], oacc[b][e + 3]} * inv;
-      },
-      [&](int i) { return (i >> 2) * 32 + (i & 3) * 8 + half * 4; });
-  if (half == 0 && a.lse) a.lse[orow] = lse;
+  // Whole rows to an instruction in the output, and in the prior's loads, which go
+  // out first: O goes through the wave's own LDS, row m at m * 512 with its 16-byte
+  // pieces permuted, piece c at place c ^ m.  (Eight bytes of 64 places at a time:
+  // half of a short prompt's time with a prior.)
+  const int row = rvalid ? (int)orow : -1;
+  int rows[8];  // output row of this lane's piece of instruction k: row 4 k + lane / 16 of the wave
+#pragma unroll
+  for (int k = 0; k < 8; ++k) rows[k] = __builtin_amdgcn_ds_bpermute(4 * (4 * k + (lane >> 4)), row);
+  u16x8 prior[8];
+  if (a.pl) {  // uniform
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (rows[k] >= 0) prior[k] = reinterpret_cast<const u16x8*>(a.po)[(size_t)rows[k] * (D / 8) + (lane & 15)];
+  }
+  const float own2 = lrun == 0.f ? -INFINITY : mref + log2f(lrun);
+  const Join j = join_of(own2, pl);
+  // no key: 0; a NaN stays one
+  const float w = j.own == 0.f ? 0.f : (lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f) * j.own;
+  uint8_t* mine = &s_kv[0][0][0] + (KH == 2 ? (wave & 3) * (66 * 64 * 4) : wave * 16384);
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 o = {oacc[b][4 * i], oacc[b][4 * i + 1], oacc[b][4 * i + 2], oacc[b][4 * i + 3]};
+      const int c = b * 8 + i * 2 + half;
+      *reinterpret_cast<f32x4*>(mine + m * 512 + ((c ^ m) * 16)) = w == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : o * w;
+    }
+  if (half == 0 && rvalid && a.lse) a.lse[orow] = j.lse;
+  asm volatile("" ::: "memory");  // the wave's LDS operations run in order
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int lr = 4 * k + (lane >> 4), c = 2 * (lane & 15);
+    const float pw = a.pl ? __int_as_float(__builtin_amdgcn_ds_bpermute(4 * lr, __float_as_int(j.prior))) : 0.f;
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(mine + lr * 512 + ((c ^ lr) * 16));
+    const f32x4 hi = *reinterpret_cast<const f32x4*>(mine + lr * 512 + (((c + 1) ^ lr) * 16));
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float x = e < 4 ? lo[e & 3] : hi[e & 3];
+      if (a.pl) x = pw == 0.f ? x : fmaf((float)__builtin_bit_cast(bf16x8, prior[k])[e], pw, x);  // without weight it may be anything
+      o[e] = (__bf16)x;
+    }
+    if (rows[k] >= 0) reinterpret_cast<bf16x8*>(a.o)[(size_t)rows[k] * (D / 8) + (lane & 15)] = o;
+  }
 }
 
 // float32: S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x2_f32.  One workgroup =
