@@ -487,7 +487,7 @@ typedef struct {
   int32_t* table;         /* device [n][table_stride], in and out: page of tokens j * page_size .. */
   int32_t* free_pages;    /* device [num_pages], in and out: a stack of free pages */
   const int32_t* free_count;  /* device [1]: pages on the stack (taken within [0, num_pages]) */
-  int32_t* free_count_out;    /* device [1]: after the call; not free_count itself */
+  int32_t* free_count_out;    /* device [1]: after the call */
   int32_t* cu;            /* device [n + 1] out: first row of each request's new tokens */
   int32_t* kv_len;        /* device [n] out: ctx + add, 0 if refused or over */
   int32_t* slots;         /* device [max_tokens] out: slot of each new token, -1: none */
@@ -510,7 +510,8 @@ typedef struct {
  * see no key.  Its rows still count in cu.
  * cu is the running sum of max(add, 0), at most max_tokens.  slots and
  * positions are written whole: entries behind cu[n] are -1 and 0.
- * A slot whose page is outside [0, num_pages) is -1 as well. */
+ * A slot whose page is outside [0, num_pages) is -1 as well.
+ * Outputs must not overlap ctx, add, base and free_count, nor each other. */
 protokv_status protokv_page_plan(const protokv_page_plan_args* a, void* stream);
 
 typedef struct {

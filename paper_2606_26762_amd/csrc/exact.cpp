@@ -206,7 +206,12 @@ protokv_status protokv_page_plan(const protokv_page_plan_args* a, void* stream) 
     if (!p || off4(p)) return fail(PROTOKV_E_INVALID, who, "arrays must be non-NULL and aligned to 4 bytes");
   if (off4(a->base) || off4(a->positions) || off4(a->refused))
     return fail(PROTOKV_E_INVALID, who, "arrays must be aligned to 4 bytes");
-  if (a->free_count == a->free_count_out) return fail(PROTOKV_E_INVALID, who, "free_count_out must not be free_count");
+  // every workgroup reads the inputs while the first writes the outputs
+  const void* in[] = {a->ctx, a->add, a->base, a->free_count};
+  const void* out[] = {a->free_count_out, a->cu, a->kv_len, a->slots, a->positions, a->refused};
+  for (const void* p : in)
+    for (const void* q : out)
+      if (p && p == q) return fail(PROTOKV_E_INVALID, who, "an output must not be one of ctx, add, base and free_count");
   return device(launch_page_plan(*a, (hipStream_t)stream), who);
 })
 

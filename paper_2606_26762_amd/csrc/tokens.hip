@@ -118,14 +118,17 @@ __device__ __forceinline__ int sat_add(int x, int y) { return min(x + y, PL_MAX)
 template <int NT>
 __device__ __forceinline__ void block_sums(int& x, int& y, int* s, int& tx, int& ty) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int u = __shfl_up(x, d, 64), v = __shfl_up(y, d, 64);
-    if (lane >= d) {
-      x = sat_add(x, u);
-      y = sat_add(y, v);
-    }
-  }
+  // running sums of the wave: within rows of 16 lanes, then over the rows (row_bcast)
+#define PL_STEP(ctrl, rows)                                                     \
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false));    \
+  y = sat_add(y, __builtin_amdgcn_update_dpp(0, y, ctrl, rows, 0xf, false));
+  PL_STEP(0x111, 0xf)
+  PL_STEP(0x112, 0xf)
+  PL_STEP(0x114, 0xf)
+  PL_STEP(0x118, 0xf)
+  PL_STEP(0x142, 0xa)
+  PL_STEP(0x143, 0xc)
+#undef PL_STEP
   if (lane == 63) {
     s[2 * wave] = x;
     s[2 * wave + 1] = y;
@@ -227,34 +230,38 @@ __global__ __launch_bounds__(NT) void k_page_plan(protokv_page_plan_args a, int 
   // page j of request i, which lacks the pages from `held` on
   auto taken = [&](int i, int j, int held) { return stacked(nfree - 1 - (s_take[i] + j - held)); };
 
-  const int gid = blockIdx.x * NT + tid, gsize = gridDim.x * NT;
-  // rows
-  for (int t = gid; t < a.max_tokens; t += gsize) {
-    int slot = -1, pos = 0;
-    if (t < rows) {
-      const int i = find_at(s_row, n, t);
-      const int ctx = ctx_of(i), held = pages_of(ctx);
-      const long long p = (long long)ctx + (t - s_row[i]);
-      pos = (int)(p + (a.base ? a.base[i] : 0));
-      if (granted(i, ctx, add_of(i))) {
-        const int j = (int)(p >> shift);
-        const int page = j < held ? a.table[(size_t)i * a.table_stride + j] : taken(i, j, held);
-        if ((unsigned)page < (unsigned)a.num_pages) slot = (page << shift) + (int)(p & P1);
+  // one row, one page taken or one page given back to a thread at a time
+  const int ntake = min(take, nfree), nback = nfree - free0;
+  const long long all = (long long)a.max_tokens + ntake + nback;
+  for (long long w = (long long)blockIdx.x * NT + tid; w < all; w += (long long)gridDim.x * NT) {
+    if (w < a.max_tokens) {
+      const int t = (int)w;
+      int slot = -1, pos = 0;
+      if (t < rows) {
+        const int i = find_at(s_row, n, t);
+        const int ctx = ctx_of(i), held = pages_of(ctx);
+        const long long p = (long long)ctx + (t - s_row[i]);
+        pos = (int)(p + (a.base ? a.base[i] : 0));
+        if (granted(i, ctx, add_of(i))) {
+          const int j = (int)(p >> shift);
+          const int page = j < held ? a.table[(size_t)i * a.table_stride + j] : taken(i, j, held);
+          if ((unsigned)page < (unsigned)a.num_pages) slot = (page << shift) + (int)(p & P1);
+        }
       }
+      a.slots[t] = slot;
+      if (a.positions) a.positions[t] = pos;
+    } else if (w < (long long)a.max_tokens + ntake) {
+      const int x = (int)(w - a.max_tokens), i = find_at(s_take, n, x);
+      const int ctx = ctx_of(i), held = pages_of(ctx);
+      if (granted(i, ctx, add_of(i))) {
+        const int j = held + x - s_take[i];
+        a.table[(size_t)i * a.table_stride + j] = taken(i, j, held);
+      }
+    } else {
+      const int x = (int)(w - a.max_tokens - ntake);
+      a.free_pages[free0 + x] = stacked(free0 + x);
     }
-    a.slots[t] = slot;
-    if (a.positions) a.positions[t] = pos;
   }
-  // pages taken
-  for (int x = gid; x < min(take, nfree); x += gsize) {
-    const int i = find_at(s_take, n, x);
-    const int ctx = ctx_of(i), held = pages_of(ctx);
-    if (!granted(i, ctx, add_of(i))) continue;
-    const int j = held + x - s_take[i];
-    a.table[(size_t)i * a.table_stride + j] = taken(i, j, held);
-  }
-  // pages given back
-  for (int x = gid; x < nfree - free0; x += gsize) a.free_pages[free0 + x] = stacked(free0 + x);
   if (blockIdx.x != 0) return;
   // lengths; the pages of the granted requests and the count of the others.  Pages
   // are granted from the front: the largest running sum of a granted request with
@@ -298,10 +305,11 @@ hipError_t launch_rotate(const RotateArgs& a0, bool fp32, hipStream_t st) {
 
 hipError_t launch_page_plan(const protokv_page_plan_args& a, hipStream_t st) {
   const int shift = 31 - __builtin_clz((unsigned)a.page_size);
-  // a row a thread, at most 64 workgroups (each forms the sums of all requests); a
-  // small workgroup's barriers for few requests
+  // about a row or page a thread (every request may take or give some), at most 64
+  // workgroups (each forms the sums of all requests); for few requests a workgroup of
+  // four waves, whose barriers are short
   auto blocks = [&](int threads) {
-    const long long b = ((long long)a.max_tokens + threads - 1) / threads;
+    const long long b = ((long long)a.max_tokens + 4ll * a.num_requests + threads - 1) / threads;
     return dim3((unsigned)(b < 64 ? b : 64));
   };
   if (a.num_requests <= 256)

@@ -23,8 +23,7 @@ def _set(a, **kw):
 
 
 def plan(**kw):
-    a = pk.PagePlanArgs(4, 100, 16, 8, 64, *([GOOD] * 12))
-    a.free_count_out = GOOD + 64
+    a = pk.PagePlanArgs(4, 100, 16, 8, 64, *[GOOD + 4096 * i for i in range(12)])
     return _set(a, **kw)
 
 
@@ -36,7 +35,8 @@ def plan(**kw):
     (dict(ctx=None), 1), (dict(add=None), 1), (dict(table=None), 1), (dict(free_pages=None), 1),
     (dict(free_count=None), 1), (dict(free_count_out=None), 1), (dict(cu=None), 1), (dict(kv_len=None), 1),
     (dict(slots=None), 1), (dict(slots=GOOD + 2), 1), (dict(base=GOOD + 1), 1), (dict(refused=GOOD + 3), 1),
-    (dict(free_count_out=GOOD), 1)])
+    (dict(free_count_out=GOOD + 4096 * 5), 1), (dict(kv_len=GOOD), 1), (dict(cu=GOOD + 4096), 1),
+    (dict(positions=GOOD + 4096 * 2), 1)])
 def test_page_plan_refuses(kw, status):
     assert _status("page_plan", plan(**kw)) == status
     assert b"page_plan: " in pk.lib().protokv_last_error(None)

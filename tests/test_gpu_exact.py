@@ -231,6 +231,54 @@ def test_prompt_first_row_returns_its_value():
     assert bool(((lse.double() - want).abs() <= 1e-4).all())
 
 
+@pytest.mark.parametrize("lens,hq,hk", [([1300], 28, 4), ([700, 90], 16, 2)])
+def test_prompt_in_few_blocks(lens, hq, hk):
+    """So few rows that two waves share a row's keys; values of the first keys that
+    are infinite reach every row, one of a late key only those behind it."""
+    import torch
+    log(f"case: prompt in few blocks {lens}")
+    q, k, v, cu, o, lse = _prompt(lens, hq, hk, "bf16", 6)
+    _prompt(lens, hq, hk, "bf16", 7, prior=True)
+    v2 = v.clone()
+    v2[3, 0, 9] = -math.inf
+    v2[600, 0, 11] = math.nan
+    o2, lse2 = PK().prompt_attend(q, k, v2, cu)
+    g, L = hq // hk, lens[0]
+    assert torch.equal(lse2[:L], lse[:L])
+    assert bool((o2[3:L, :g, 9] == -math.inf).all()) and bool(o2[600:L, :g, 11].isnan().all())
+    assert bool(o2[:3, :g, 9].isfinite().all()) and bool(o2[:600, :g, 11].isfinite().all())
+    o2[:, :g, 9], o2[:, :g, 11] = o[:, :g, 9], o[:, :g, 11]
+    d = (o2[:L].double() - o[:L].double()).abs()
+    assert bool((d <= 2 * HB * (o[:L].double().abs() + 0.05)).all())
+
+
+@pytest.mark.parametrize("n", [3, 70])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_that_make_no_sense_stay_inside(dtype, n):
+    """cu that falls, is negative or passes the rows: whatever comes out, nothing
+    outside the results is written, and sequences that are in order are right."""
+    import torch
+    log(f"case: senseless cu {dtype} {n}")
+    pk, g = PK(), _g(8)
+    dt = _dt(dtype)
+    total, hq, hk, P = 200, 4, 2, 16
+    wild = [0, 60, 20, 900, -5, 2 ** 31 - 1, -2 ** 31, 130]
+    cu = _i32([wild[i % 8] for i in range(n + 1)])
+    q, k, v = (_randn(g, total, h, D, dtype=dt) for h in (hq, hk, hk))
+    big = torch.full((total + 400, hq, D), 7.5, dtype=dt, device="cuda")
+    bl = torch.full((total + 400, hq), 8.5, device="cuda")
+    o, lse = big[200:200 + total], bl[200:200 + total]
+    pk.prompt_attend(q, k, v, cu, out=o, lse=lse)
+    pages = tuple(_randn(g, 20, hk, P, D, dtype=dt) for _ in range(2))
+    table = torch.randint(-3, 25, (n, 9), generator=g, device="cuda").int()
+    lens = torch.randint(-50, 400, (n,), generator=g, device="cuda").int()
+    for add in (1, 200):
+        pk.page_attend(q, pages, table, cu, lens, add, out=o, lse=lse)
+    torch.cuda.synchronize()
+    for x, s in ((big, 7.5), (bl, 8.5)):
+        assert bool((x[:200] == s).all()) and bool((x[200 + total:] == s).all())
+
+
 # -- pages ------------------------------------------------------------------------
 
 
@@ -356,6 +404,15 @@ def test_pages_split_over_the_context(reqs):
     log(f"case: split context {reqs}")
     _paged(reqs, 7, 1, 16, "bf16", 17, prior=True)
     _paged(reqs, 4, 2, 32, "fp32", 17)
+
+
+def test_pages_of_many_requests():
+    """Thousands of requests, most with a token, some with none, a few with a chunk."""
+    log("case: pages of many requests")
+    rng = np.random.default_rng(21)
+    reqs = [(int(rng.integers(0, 90)), int(rng.choice([0, 1, 1, 1, 1, 2]))) for _ in range(2500)]
+    reqs[700], reqs[2400] = (300, 40), (10, 70)
+    _paged(reqs, 2, 1, 8, "bf16", 21)
 
 
 @pytest.mark.parametrize("P", [1, 2])
