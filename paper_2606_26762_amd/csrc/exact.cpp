@@ -165,7 +165,7 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   const bool many = (int64_t)a.max_add * a.grp > EX_FEW;
   if (!fp32 && !(many && a.n == 1)) {
     const int64_t tiles = (((int64_t)a.stride << a.shift) + 31) / 32;
-    const int64_t waves = std::max<int64_t>(1, ((int64_t)a.Hkv * a.n * tiles + EX_FEW_TILES - 1) / EX_FEW_TILES);
+    const int64_t waves = std::max<int64_t>(1, ((int64_t)a.Hkv * a.n * tiles + 1) / 2);
     a.few = a.n ? (int)std::min<int64_t>(EX_FEW_WAVES, (waves + 3) / 4 * 4) : 0;
     a.few_rows = (int)std::min<int64_t>(EX_FEW, (int64_t)a.max_add * a.grp);
   }

@@ -20,7 +20,6 @@ constexpr int EX_MAX_SPLITS = 16;
 constexpr int EX_MIN_TILES = 8;   // 64-key (bf16) or 32-key (float32) tiles that a context split has at least
 constexpr int EX_FEW = 32;        // rows per kv head of a request that the few-rows kernel takes
 constexpr int EX_FEW_WAVES = 2048;  // waves of the few-rows kernel, at most (two to a SIMD)
-constexpr int EX_FEW_TILES = 2;   // 32-key tiles that a wave of it has at least
 constexpr int MAX_REQUESTS = 8192;
 constexpr int MAX_AXES = 8;
 

@@ -1080,7 +1080,11 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   long long upto = wave_sum(mine);
   const long long N = lane_ll(upto, 63) * a.Hkv;
   const long long waves = (long long)gridDim.x * FW_W;
-  const long long per = max((N + waves - 1) / waves, (long long)EX_FEW_TILES);
+  // tiles of a run: at least 2, and as long as 16 are not reached as many as leave
+  // two waves to a compute unit, since more partials cost more than more loads in
+  // flight give (30 000 tokens, 4 kv heads, 2048 waves 32 us, 470 24; 8 x 8000, 7 rows
+  // 38 and 31, 32 rows 64 and 35; but 64 x 8000, 2048 waves 203, 512 231)
+  const long long per = max(max((N + waves - 1) / waves, min(16ll, (N + 511) / 512)), 2ll);
   const long long x1 = min(N, (w + 1) * per);
   long long x = w * per;
   if (lane == 0) meta[0] = 0;
@@ -1309,7 +1313,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
 // k_exact_few and run on: slot 1 of that wave, slot 0 of the next ones.  Of an
 // item with few partials each wave takes a row by itself, 32 threads (four dims
 // each) for every other partial; of one with many the workgroup takes a row at a
-// time.  blockIdx.y deals the rows out to FJ_Y workgroups.  64 requests, 248 items
+// time.  blockIdx.y deals the rows out.  64 requests, 248 items
 // of 8 partials on average: 5 us; a workgroup per row for all items, one after the
 // other, 21.
 constexpr int FJ_W = 8;
@@ -1365,8 +1369,10 @@ hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t s
   if (a.few) {
     const int wgs = (a.few + FW_W - 1) / FW_W;
     hipLaunchKernelGGL(k_exact_few, dim3(wgs), dim3(FW_W * 64), 0, st, a);
-    hipLaunchKernelGGL(k_exact_few_join, dim3((wgs * FW_W + FJ_W - 1) / FJ_W, std::min(FJ_Y, a.few_rows)), dim3(FJ_W * 64),
-                       0, st, a, wgs * FW_W);
+    // a workgroup per row and 8 waves, up to 2048 of them, at least four to 8 waves
+    const int parts = (wgs * FW_W + FJ_W - 1) / FJ_W;
+    hipLaunchKernelGGL(k_exact_few_join, dim3(parts, std::min(a.few_rows, std::max(FJ_Y, 2048 / parts))), dim3(FJ_W * 64), 0,
+                       st, a, wgs * FW_W);
   }
   const unsigned items = (unsigned)a.Hkv * a.blocks * a.splits;
   if (items == 0) return hipGetLastError();

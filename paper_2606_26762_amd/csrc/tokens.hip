@@ -293,10 +293,9 @@ __global__ __launch_bounds__(NT) void k_page_plan(protokv_page_plan_args a, int 
 
 hipError_t launch_rotate(const RotateArgs& a0, bool fp32, hipStream_t st) {
   RotateArgs a = a0;
-  // a wave per token and eight heads while that leaves the GPU (8192 waves) unfilled
-  const int groups = (a.Hq + 2 * a.Hkv + 7) / 8;
-  a.parts = 1;
-  while (a.parts < groups && (long long)a.N * a.parts < 8192) a.parts = a.parts * 2 < groups ? a.parts * 2 : groups;
+  // a wave per token and eight heads (a wave per token, 40 000 tokens of 32 + 8 heads:
+  // 156 us against 139)
+  a.parts = (a.Hq + 2 * a.Hkv + 7) / 8;
   const unsigned blocks = (unsigned)(((long long)a.N * a.parts + 3) / 4);
   if (fp32) hipLaunchKernelGGL((k_rotate<1>), dim3(blocks), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_rotate<0>), dim3(blocks), dim3(256), 0, st, a);
