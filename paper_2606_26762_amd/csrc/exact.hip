@@ -356,6 +356,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   constexpr int NH = 2 / KH, NST = 4 / KH;  // a wave's 32-key halves and 16-key steps of a tile, and steps of K
   f32x16 s[2];     // scores, then weights (KH = 2: of even and odd 16-dim steps, then all in the first)
   bf16x8 p_next;   // the first step's weights
+  bf16x8 v_next[4];  // and its V operands
   // P operand of 16-key step st: the weights in bfloat16
   auto weight_operand = [&](int st) {
     bf16x8 p;
@@ -401,7 +402,10 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
                                : KH == 1 ? read_k(kl, j & 1, 2 * ks + (j >> 1)) : read_k(kl, 0, 4 * ks + j);
     };
 #pragma unroll
-    for (int j = 0; j < 4; ++j) read(F, j);
+    for (int j = 0; j < 4; ++j) {
+      if (F == 0) op[0][j] = v_next[j];
+      else read(F, j);
+    }
     p[0] = p_next;
 #pragma unroll
     for (int step = F; step < L; ++step) {
@@ -431,6 +435,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
         }
       }
     }
+    if (tk + 3 < t1) locate(tk + 3);
     if (F == 0) lrun += (part[0] + part[1]) + (part[2] + part[3]);  // this half's keys; the halves meet at the end
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(0);
@@ -554,7 +559,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   // VALU (in step, both wait for the one and then for the other).  A barrier begins
   // each period.  Tile t + 2 is loaded beside the products of tile t: V of tile t - 2,
   // last read in period t - 1, has left its buffer, and the tile is read from period
-  // t + 2 on.
+  // t + 2 on; the rows of tile t + 3 are located behind them.
   auto even = [&](int t) {  // the barrier before period t
     __builtin_amdgcn_sched_barrier(0);
     if (t + 1 < t1) wait_vm<4>();  // this wave's loads of tile t have landed, those of t + 1 may be in flight
@@ -578,8 +583,10 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   auto second_barrier = [&](int t) {
     if (late && t < t1) even(t + 1);
   };
-  auto find_next = [&](int t) {
-    if (t + 3 < t1) locate(t + 3);
+  auto read_next = [&](int t) {  // the first V operands of tile t, whose weights are done
+    const uint32_t vl = value_base(done ? s_zero : s_kv[t % EX_NBUF][1]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v_next[j] = __builtin_bit_cast(bf16x8, read_v(vl, j, 0));
   };
   if (late) even(t0);
   int t = t0;
@@ -588,18 +595,17 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     products(t, t, no, yes);
     second_barrier(t);
     done = weights(t);
-    find_next(t);
+    read_next(t);
     for (++t; t < tw; ++t) {
       first_barrier(t);
       products(t - 1, t, yes, yes);
       second_barrier(t);
       done = weights(t);
-      find_next(t);
+      read_next(t);
     }
     first_barrier(t);
     products(t - 1, t, yes, no);
     second_barrier(t);
-    find_next(t);
     ++t;
   }
   for (; t <= t1; ++t) {
@@ -607,8 +613,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     if (t + 2 < t1)
 #pragma unroll
       for (int part = 0; part < 4; ++part) load(t + 2, part);
+    if (t + 3 < t1) locate(t + 3);
     second_barrier(t);
-    find_next(t);
   }
   lrun += xor32(lrun);
   if constexpr (KH == 2) {
