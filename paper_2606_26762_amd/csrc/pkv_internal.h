@@ -205,24 +205,6 @@ __device__ __forceinline__ uint32_t xor32_u(uint32_t v) {
 __device__ __forceinline__ float xor32(float v) { return __uint_as_float(xor32_u(__float_as_uint(v))); }
 __device__ __forceinline__ int xor32(int v) { return (int)xor32_u((uint32_t)v); }
 
-// cos and sin of the rotary angle pos * inv (inv = theta^(-2i/D)): the angle
-// in float64, whole turns taken off in float64, the rest (|r| <= pi) to
-// float32 sincos.  Stream positions reach 10^6 and more, where a float32
-// angle would already be off by tenths of a radian.
-__device__ __forceinline__ void rope_cs(double pos, double inv, float& c, float& s) {
-  const double a = pos * inv;
-  const double turns = rint(a * 0.15915494309189535);  // 1 / (2 pi)
-  const float r = (float)fma(-turns, 6.283185307179586, a);
-  sincosf(r, &s, &c);
-}
-
-// Rotate-half rotation of the pair (x1 = dim i, x2 = dim i + D/2):
-// lo = x1 c - x2 s, hi = x2 c + x1 s (float32, one rounding per operation).
-__device__ __forceinline__ void rope_pair(float x1, float x2, float c, float s, float& lo, float& hi) {
-  lo = x1 * c - x2 * s;
-  hi = x2 * c + x1 * s;
-}
-
 // s_waitcnt vmcnt(n) (expcnt / lgkmcnt not waited for)
 template <int N>
 __device__ __forceinline__ void wait_vm() {

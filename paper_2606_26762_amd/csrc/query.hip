@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "pkv_internal.h"
+#include "rope.h"
 
 namespace pkv {
 

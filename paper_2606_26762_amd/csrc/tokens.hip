@@ -2,6 +2,7 @@
 // protokv_page_plan) for gfx950.
 #include "exact.h"
 #include "pkv_internal.h"
+#include "rope.h"
 
 namespace pkv {
 
