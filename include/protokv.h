@@ -458,7 +458,8 @@ protokv_status protokv_profile_read(protokv_t h, protokv_kernel_times* out);
  * elements, head h at h * head_dim in it, so the three may be parts of one
  * projection's output.  Strides are multiples of 16 bytes, at least the heads'
  * size; pointers to rows and pages are aligned to 16 bytes, other arrays to 4.
- * Outputs without a stride are contiguous.  kv_dtype is the type of q, k, v,
+ * Outputs without a stride are contiguous; outputs overlap no input and no
+ * other output, but where a call says that they may.  kv_dtype is the type of q, k, v,
  * pages and o; head_dim is 128; num_q_heads is a multiple of num_kv_heads, at
  * most 256 times; query head h reads kv head h / (Hq / Hkv).
  *
@@ -515,7 +516,7 @@ typedef struct {
 protokv_status protokv_page_plan(const protokv_page_plan_args* a, void* stream);
 
 typedef struct {
-  int32_t num_tokens;     /* N, >= 0 */
+  int32_t num_tokens;     /* N, >= 0 (0: nothing is done); N times all heads below about 2^29 */
   int32_t num_q_heads, num_kv_heads, head_dim, kv_dtype;
   int32_t num_axes;       /* 1..8 */
   const int32_t* positions;  /* device: axis a of token t at positions[a * position_stride + t] */
@@ -562,7 +563,8 @@ typedef struct {
  * such as a layer of protokv_attend's) o and lse are those over both:
  * lse = log(e^own + e^prior), o weighted by e^(own - lse) and e^(prior - lse);
  * a prior_lse of -inf leaves prior_o unread.  o and lse may be the prior's
- * own arrays. */
+ * own arrays (o prior_o and lse prior_lse).  Fewer than 2^23 row blocks: rows * Hq
+ * / 128 and sequences * Hkv together. */
 protokv_status protokv_prompt_attend(const protokv_prompt_args* a, void* stream);
 
 typedef struct {

@@ -241,7 +241,7 @@ __device__ __forceinline__ void ex_barrier() {
 
 constexpr int EX_KEYS = 64;             // keys per tile
 constexpr int EX_TILE = EX_KEYS * D * 2;  // one K or V tile, 16 KB
-constexpr int EX_NBUF = 4;              // tile t computes while t + 1 .. t + 3 load
+constexpr int EX_NBUF = 4;              // tiles t - 1 and t in use, t + 1 and t + 2 loading
 constexpr int EX_IDS = 1024;            // page ids staged at a time
 
 // Workgroup = eight waves of 32 query rows each.  Tiles of 64 keys go straight from
@@ -253,6 +253,12 @@ constexpr int EX_IDS = 1024;            // page ids staged at a time
 // S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x16_bf16,
 // V^T through ds_read_b64_tr_b16: each lane holds one query column, so the
 // softmax is lane-local plus one exchange with the partner lane.
+// Bound by the matrix cores at the clock that their power leaves: 8192 tokens of
+// 32 / 8 heads 511 us, 1.08 PFLOP/s of what is seen (a plain product of 8192^3
+// reaches 1.12), 4 x 512 tokens over 16 384 of 28 / 4 heads 490 us, 1.0.  KH = 2:
+// two waves take a row's keys, half of every tile each; 128 rows to a workgroup, for
+// launches that 256 would leave in few rounds (the rule and its figures stand
+// with the host's block counts).
 template <int PAGED, int KH>
 __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   __shared__ __attribute__((aligned(256))) uint8_t s_kv[EX_NBUF][2][EX_TILE];
@@ -708,7 +714,10 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 // float32: S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x2_f32.  One workgroup =
 // one work item (kv head, 32 query rows, context split); its four waves take the
 // 32-key tiles in turn, each by itself, and merge at the end (one wave per item left
-// long rows to few SIMDs: prompts of 1001 tokens 268 us).  K and V go from global
+// long rows to few SIMDs: prompts of up to 1001 tokens 268 us against 153).  A float32
+// product carries 1/16 of a bfloat16 one's rate, so that the matrix cores bound it: they
+// are busy 82% of a workgroup's tiles, and half of a launch of three such prompts,
+// whose starts, merges and last workgroups they wait for.  K and V go from global
 // memory into the operand registers; the query sits in LDS.
 //   K: lane (m = lane % 32, h = lane / 32) loads dims 8 j + 4 h .. + 3 of key m.
 //   P: register i of S^T holds key 8 (i / 4) + 4 h + i % 4 of query lane % 32.
@@ -1005,7 +1014,8 @@ struct Sum {
 };
 
 // Joins the splits of a row block.  Workgroup = EJ_ROWS rows of one (kv head, row
-// block), 32 threads per row.
+// block), 32 threads per row.  A latency chain: block, references, partials (3 x 20
+// rows over 2500 tokens 4.9 us).
 constexpr int EJ_ROWS = 16;
 template <int FP32, int R>
 __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
@@ -1035,7 +1045,8 @@ __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
 // tile's loads in flight.  An item within one run is written out; of one
 // that runs on, each wave leaves a partial (at most two per wave: the item it ends
 // in, slot 1, and the one it continues, slot 0), and the wave that the item begins
-// in notes it for k_exact_few_join.
+// in notes it for k_exact_few_join.  64 requests over 1.07 GB of pages: 198 us, 5.4
+// TB/s; one over 1500 tokens 9.6 us, the chain of its two or three tiles.
 constexpr int FW_W = 4;              // waves per workgroup
 constexpr int FW_VB = 32 * 64 + 64;  // bytes of one 32-dim block of a V tile (64 of padding: bank spread)
 
@@ -1319,9 +1330,9 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
 // k_exact_few and run on: slot 1 of that wave, slot 0 of the next ones.  Of an
 // item with few partials each wave takes a row by itself, 32 threads (four dims
 // each) for every other partial; of one with many the workgroup takes a row at a
-// time.  blockIdx.y deals the rows out.  64 requests, 248 items
-// of 8 partials on average: 5 us; a workgroup per row for all items, one after the
-// other, 21.
+// time (FJ_MANY partials and more).  blockIdx.y deals the rows out.  64 requests, 2048
+// waves' partials: 10 us; one request 4.8; a workgroup per row for all items, one
+// after the other, 21 for the former.
 constexpr int FJ_W = 8;
 constexpr int FJ_Y = 4;
 constexpr int FJ_MANY = 48;

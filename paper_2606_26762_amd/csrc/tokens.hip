@@ -9,7 +9,9 @@ namespace pkv {
 namespace {
 
 // ---------------------------------------------------------------------------
-// Rotary positions.  One wave takes a token, or 1 / parts of its heads: lane i
+// Rotary positions: bound by the rows' bytes.  One wave takes 1 / parts of a
+// token's heads (4608 tokens of 32 + 8 + 8 bf16 heads, stored to pages: 20.4 us,
+// 5.5 TB/s; one token 2.8 us): lane i
 // forms the (cos, sin) of pair i once (angle and reduction in float64), hands
 // them round through LDS, and then eight lanes at a time turn a head: lane c of
 // eight holds dims 8 c .. + 7 and their partners 64 + 8 c .. + 7.  Heads are
@@ -107,7 +109,8 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
 // for all requests in its LDS (a few us; no second launch, nothing to wait for),
 // then the workgroups share the pages given back, the pages taken and the rows,
 // each of which finds its request by a search in the sums.  Sums saturate at
-// PL_MAX, which no valid total reaches.
+// PL_MAX, which no valid total reaches.  What bounds it is the chain of loads,
+// barriers and the search: 64 requests 3.5 us, 1500 11.2.
 // ---------------------------------------------------------------------------
 constexpr int PL_MAX = (1 << 30) - 1;  // two of them fit an int
 
@@ -292,11 +295,7 @@ __global__ __launch_bounds__(NT) void k_page_plan(protokv_page_plan_args a, int 
 
 }  // namespace
 
-hipError_t launch_rotate(const RotateArgs& a0, bool fp32, hipStream_t st) {
-  RotateArgs a = a0;
-  // a wave per token and eight heads (a wave per token, 40 000 tokens of 32 + 8 heads:
-  // 156 us against 139)
-  a.parts = (a.Hq + 2 * a.Hkv + 7) / 8;
+hipError_t launch_rotate(const RotateArgs& a, bool fp32, hipStream_t st) {
   const unsigned blocks = (unsigned)(((long long)a.N * a.parts + 3) / 4);
   if (fp32) hipLaunchKernelGGL((k_rotate<1>), dim3(blocks), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_rotate<0>), dim3(blocks), dim3(256), 0, st, a);

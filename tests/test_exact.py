@@ -160,3 +160,18 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         pk.rotate(None, None, cu, pk.pair_axes((64,)), 1e4)
     with pytest.raises(ValueError):
         pk.page_attend(q, (k, k), cu, cu, cu, 1)
+
+
+def test_launches_that_would_be_too_large_are_refused():
+    """A launch has fewer than 2^32 threads; counts that pass every other check."""
+    for name, a in (("prompt_attend", prompt(num_seqs=(1 << 24) - 1, num_q_heads=8, num_kv_heads=8, k_stride=1024,
+                                             v_stride=1024)),
+                    ("page_attend", page(num_requests=1 << 23, max_add=100)),
+                    ("rotate", rotate(num_tokens=1 << 27)), ("rotate", rotate(num_tokens=(1 << 25) + 1))):
+        assert _status(name, a) == 2, name
+        assert b"for one launch" in pk.lib().protokv_last_error(None) or b"2^29" in pk.lib().protokv_last_error(None)
+
+
+def test_rotate_of_no_tokens_needs_no_addresses():
+    """Empty tensors may have none."""
+    assert _status("rotate", rotate(num_tokens=0, q=None, k=None, v=None, q_out=None, positions=None, slots=None)) == 0

@@ -833,3 +833,135 @@ def test_question_and_answer_over_the_video_memory():
                 assert float((fo[:, head].double().cpu() - want).abs().max()) <= h.READOUT_ATOL + 2e-2
                 assert float((fl[:, head].double().cpu() - both).abs().max()) <= h.LSE_ATOL + 1e-4
         done += add
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("reqs,hq,hk", [
+    ([(40, 1)], 4, 2), ([(9000, 1), (5, 2)], 7, 1), ([(9000, 1)] * 2, 1, 1), ([(700, 150)], 6, 2), ([(12000, 40)], 4, 1),
+    ([(0, 600)] * 20, 8, 4)])
+def test_result_in_the_prior_s_own_arrays(reqs, hq, hk, dtype):
+    """o and lse written over the prior: one wave's rows, joined runs, row blocks,
+    context splits; the same bits as beside it."""
+    import torch
+    log(f"case: in place {reqs[:2]} heads {hq}/{hk} {dtype}")
+    pk, g = PK(), _g(51)
+    dt, P = _dt(dtype), 16
+    need = [(c + a + P - 1) // P for c, a in reqs]
+    width, pages = max(need), sum(need)
+    table = torch.full((len(reqs), width), -1, dtype=torch.int32, device="cuda")
+    order = torch.randperm(pages, generator=g, device="cuda").int()
+    for i, n in enumerate(need):
+        table[i, :n] = order[sum(need[:i]):sum(need[:i]) + n]
+    kv = tuple(_randn(g, pages, hk, P, D, dtype=dt) for _ in range(2))
+    add = [a for _, a in reqs]
+    total = sum(add)
+    cu, lens = _i32(np.cumsum([0] + add).tolist()), _i32([c + a for c, a in reqs])
+    q, po = (_randn(g, total, hq, D, dtype=dt) for _ in range(2))
+    pl = torch.randn(total, hq, generator=g, device="cuda") + 4
+    want_o, want_l = pk.page_attend(q, kv, table, cu, lens, max(add), prior=(po, pl))
+    o, lse = po.clone(), pl.clone()
+    pk.page_attend(q, kv, table, cu, lens, max(add), prior=(o, lse), out=o, lse=lse)
+    k, v = (_randn(g, total, hk, D, dtype=dt) for _ in range(2))
+    want_o2, want_l2 = pk.prompt_attend(q, k, v, cu, prior=(po, pl))
+    o2, lse2 = po.clone(), pl.clone()
+    pk.prompt_attend(q, k, v, cu, prior=(o2, lse2), out=o2, lse=lse2)
+    torch.cuda.synchronize()
+    assert torch.equal(o, want_o) and torch.equal(lse, want_l)
+    assert torch.equal(o2, want_o2) and torch.equal(lse2, want_l2)
+
+
+def test_no_rows_are_no_error():
+    """Empty tensors through the binding: nothing is launched, nothing is refused."""
+    import torch
+    log("case: no rows")
+    pk = PK()
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    q, k = torch.empty(0, 4, D, **bf), torch.empty(0, 2, D, **bf)
+    kv = tuple(torch.full((3, 2, 16, D), 2.0, **bf) for _ in range(2))
+    axes = pk.pair_axes((64,))
+    qo, ko = pk.rotate(q, k, _i32([]), axes, 1e4)
+    assert qo.shape == q.shape and ko.shape == k.shape
+    pk.rotate(q, k, _i32([]), axes, 1e4, v=k, pages=kv, slots=_i32([]))
+    for cu in (_i32([0]), _i32([0, 0])):
+        n = cu.shape[0] - 1
+        for o, lse in (pk.prompt_attend(q, k, k, cu),
+                       pk.page_attend(q, kv, torch.zeros(n, 2, dtype=torch.int32, device="cuda"), cu, _i32([5] * n), 1)):
+            assert o.shape == q.shape and lse.shape == (0, 4)
+    one = torch.ones(2, 4, D, **bf)
+    o = torch.full_like(one, 7.5)
+    pk.prompt_attend(one, one[:, :2], one[:, :2], _i32([0, 0]), out=o)   # rows, of no sequence
+    torch.cuda.synchronize()
+    assert bool((o == 7.5).all()) and all(bool((x == 2.0).all()) for x in kv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_prompts_captured_and_replayed_with_other_lengths(dtype):
+    """A graph of a rotation and a prompt's attention on a side stream, padded to its
+    sizes; lengths and rows change between the replays, with eager work in between."""
+    import torch
+    log(f"case: captured prompts {dtype}")
+    pk, g = PK(), _g(52)
+    dt, hq, hk, n, most = _dt(dtype), 6, 2, 3, 400
+    axes = pk.pair_axes((16, 24, 24))
+    qkv = torch.zeros(most, (hq + 2 * hk) * D, dtype=dt, device="cuda")
+    pos, cu = torch.zeros(3, most, dtype=torch.int32, device="cuda"), _i32([0] * (n + 1))
+    o = torch.empty(most, hq, D, dtype=dt, device="cuda")
+    lse = torch.empty(most, hq, device="cuda")
+
+    def step(out, l):
+        q, k, v = (x.unflatten(1, (-1, D)) for x in qkv.split([hq * D, hk * D, hk * D], dim=1))
+        qr, kr = pk.rotate(q, k, pos, axes, 1e6)
+        return pk.prompt_attend(qr, kr, v, cu, out=out, lse=l)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(o, lse)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(o, lse)
+    for lens in ([400, 0, 0], [1, 70, 129], [0, 0, 0], [33, 300, 2]):
+        qkv.copy_(_randn(g, *qkv.shape, dtype=dt))
+        pos.copy_(torch.randint(0, 4000, pos.shape, generator=g, device="cuda").int())
+        cu.copy_(_i32(np.cumsum([0] + lens).tolist()))
+        o.fill_(7.5)
+        lse.fill_(8.5)
+        want, wl = torch.full_like(o, 7.5), torch.full_like(lse, 8.5)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            step(want, wl)
+        side.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want) and torch.equal(lse, wl), f"lengths {lens}"
+        assert bool((o[sum(lens):] == 7.5).all())
+
+
+def test_plan_and_rotation_on_a_stream_of_their_own():
+    """The stream argument: the call waits for that stream's work, not the current one's."""
+    import torch
+    log("case: plan and rotation on a side stream")
+    pk, g = PK(), _g(53)
+    side = torch.cuda.Stream()
+    n, P, most = 40, 8, 200
+    args = []
+    for _ in range(2):
+        args.append((_i32([5 * i % 37 for i in range(n)]), _i32([i % 6 - (i % 11 == 3) * 7 for i in range(n)]),
+                     torch.arange(n * 8, device="cuda").int().view(n, 8) % 300,
+                     torch.arange(300, device="cuda").int().flip(0).contiguous(), _i32([50])))
+    q = _randn(g, most, 4, D, dtype=torch.bfloat16)
+    axes = pk.pair_axes((64,))
+    a = pk.page_plan(*args[0], P, most)
+    ra = pk.rotate(q, None, a.positions, axes, 1e4)[0]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        big = torch.randn(4000, 4000, device="cuda") @ torch.randn(4000, 4000, device="cuda")
+        q2 = q * 1
+    b = pk.page_plan(*args[1], P, most, stream=side)
+    rb = pk.rotate(q2, None, b.positions, axes, 1e4, stream=side)[0]
+    side.synchronize()
+    assert bool(big.isfinite().all())
+    for f in pk.PagePlan.__slots__:
+        assert torch.equal(getattr(a, f), getattr(b, f)), f
+    assert torch.equal(ra, rb) and all(torch.equal(x, y) for x, y in zip(args[0], args[1]))
