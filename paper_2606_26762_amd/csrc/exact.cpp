@@ -84,19 +84,19 @@ protokv_status check_result(const Heads& h, int n, int total, const int32_t* cu,
 // which leaves room for its ceil(rows / R) whatever cu is.  R and, over pages, the
 // most context splits of a block are those with the least time by this count, in
 // tenths of a 64-key tile's time in the form of 256 rows (about 2 us): a tile takes
-// 10 (128 rows, two waves to a row's keys: 6; float32: a tile of 32 keys, 10), a
-// workgroup 40 to start and to end (50 with the waves' merge), a split 60 more for its
-// partial; `slots` workgroups run at a time.  Prompts see half their keys on
+// 10 (128 rows, two waves to a row's keys: 6), a workgroup 40 to start and to end (50
+// with the waves' merge), a split 60 more for its partial; `slots` workgroups run at a time.  Prompts see half their keys on
 // average and take at least as long as their last rows.  Measured, 28 / 4 heads: one
 // prompt of 1500 tokens 43 us by 256 rows, 34 by 128; eight of 200 17 and 25; one of
 // 4000 115 and 146; 4 x 512 tokens over 16 k in 3 splits 540, unsplit 484.
-void plan_blocks(ExactArgs& a, bool fp32, bool paged) {
-  const int64_t slots = fp32 ? 512 : 256;
+void plan_blocks(ExactArgs& a, bool paged) {
+  const int64_t slots = 256;
   const int64_t keys = paged ? (int64_t)a.stride << a.shift : ((int64_t)a.total + a.n - 1) / std::max(a.n, 1);
-  const int64_t tiles = (keys + (fp32 ? 31 : 63)) / (fp32 ? 32 : 64);
+  const int64_t tiles = (keys + 63) / 64;
   int64_t best = INT64_MAX;
-  for (int half = 0; half <= (fp32 ? 0 : 1); ++half) {
-    const int R = fp32 ? EX_ROWS_F32 : EX_ROWS >> half;
+  a.min_tiles = EX_MIN_TILES;
+  for (int half = 0; half <= 1; ++half) {
+    const int R = EX_ROWS >> half;
     const int blocks = (int)((int64_t)a.total * a.grp / R) + a.n;
     const int64_t items = (int64_t)blocks * a.Hkv, unit = half ? 6 : 10, ends = half ? 50 : 40;
     for (int s = 1; s <= (paged ? EX_MAX_SPLITS : 1) && (s == 1 || s <= tiles / EX_MIN_TILES); ++s) {
@@ -109,6 +109,38 @@ void plan_blocks(ExactArgs& a, bool fp32, bool paged) {
         a.blocks = blocks;
         a.splits = s;
       }
+    }
+  }
+}
+
+// Row blocks of float32: 32 rows, whose waves take the 32-key tiles in turn, a tile
+// 20 tenths of the unit above by itself.  Two workgroups share a compute unit, and then
+// its matrix cores.  Over pages the splits with the least time by this count (3 chunks of
+// 20 tokens over 2500, 6 / 2 heads: nine tiles and more to a split 31 us, four 22; 8 single
+// tokens over 2000, 28 / 4 heads: 252 workgroups 31 us, 288 37).  Prompts: four waves, or
+// two, which leave less of a short row idle and merge less, where the launch lasts
+// several times as long as its longest rows (32 of 200 tokens, 28 / 4 heads: four waves 205
+// us, two 154; 4 of 800 223 and 214; but one of 1500 188 and 215, one of 200 20 and 27).
+void plan_blocks_f32(ExactArgs& a, bool paged) {
+  a.rows = EX_ROWS_F32;
+  a.blocks = (int)((int64_t)a.total * a.grp / EX_ROWS_F32) + a.n;
+  a.splits = 1;
+  a.min_tiles = EX_MIN_TILES_F32;
+  a.waves = 4;
+  const int64_t items = (int64_t)a.blocks * a.Hkv;
+  const int64_t keys = paged ? (int64_t)a.stride << a.shift : ((int64_t)a.total + a.n - 1) / std::max(a.n, 1);
+  const int64_t tiles = (keys + 31) / 32;
+  if (!paged) {
+    if (items > 512 && items >= 50 * tiles) a.waves = 2;
+    return;
+  }
+  int64_t best = INT64_MAX;
+  for (int s = 1; s <= EX_MAX_SPLITS_F32 && (s == 1 || s <= tiles / EX_MIN_TILES_F32); ++s) {
+    const int64_t turns = ((tiles + s - 1) / s + 3) / 4;  // tiles of a wave
+    const int64_t cost = (items * s + 255) / 256 * turns * 20 + (items * s + 511) / 512 * (s > 1 ? 80 : 40) + (s > 1 ? 25 + s / 2 : 0);
+    if (cost < best) {
+      best = cost;
+      a.splits = s;
     }
   }
 }
@@ -155,8 +187,9 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
     return fail(PROTOKV_E_UNSUPPORTED, who, "page_size must be a power of two in [1, 1024]");
   if ((int64_t)p->pages.num_pages * p->pages.page_size >= (1ll << 31))
     return fail(PROTOKV_E_UNSUPPORTED, who, "num_pages * page_size must be below 2^31");
-  if (p->table_stride < 1 || (int64_t)p->table_stride * p->pages.page_size >= (1ll << 31))
-    return fail(PROTOKV_E_INVALID, who, "table_stride must be >= 1 and table_stride * page_size below 2^31");
+  // (the places of a few tiles behind the last token are formed in 32 bits)
+  if (p->table_stride < 1 || (int64_t)p->table_stride * p->pages.page_size > (1ll << 31) - 2048)
+    return fail(PROTOKV_E_INVALID, who, "table_stride must be >= 1 and table_stride * page_size at most 2^31 - 2048");
   a.n = p->num_requests;
   a.total = p->total;
   a.max_add = p->max_add;
@@ -177,7 +210,8 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
     a.few_rows = (int)std::min<int64_t>(EX_FEW, (int64_t)a.max_add * a.grp);
   }
   a.splits = 1;
-  if (fp32 || many) plan_blocks(a, fp32, true);
+  if (fp32) plan_blocks_f32(a, true);
+  else if (many) plan_blocks(a, true);
   return check_grid(a, who);
 }
 
@@ -323,7 +357,8 @@ protokv_status protokv_prompt_attend(const protokv_prompt_args* p, void* stream)
   a.Hq = h.q;
   a.Hkv = h.kv;
   a.grp = h.q / h.kv;
-  plan_blocks(a, fp32, false);
+  if (fp32) plan_blocks_f32(a, false);
+  else plan_blocks(a, false);
   s = check_grid(a, who);
   if (s != PROTOKV_OK) return s;
   return device(launch_exact(a, fp32, false, (hipStream_t)stream), who);

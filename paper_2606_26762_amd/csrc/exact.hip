@@ -131,7 +131,7 @@ __device__ __forceinline__ bool find_dearest(const ExactArgs& a, int d, Item& it
 
 // Context splits of a block with `tiles` key tiles, and tiles of each.
 __device__ __forceinline__ int splits_of(const ExactArgs& a, int tiles, int& per) {
-  const int want = min(a.splits, max(1, tiles / EX_MIN_TILES));
+  const int want = min(a.splits, max(1, tiles / a.min_tiles));
   per = max(1, (tiles + want - 1) / want);
   return max(1, (tiles + per - 1) / per);
 }
@@ -712,9 +712,9 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 }
 
 // float32: S^T = K Q^T and O^T = V^T P on v_mfma_f32_32x32x2_f32.  One workgroup =
-// one work item (kv head, 32 query rows, context split); its four waves take the
+// one work item (kv head, 32 query rows, context split); its W waves take the
 // 32-key tiles in turn, each by itself, and merge at the end (one wave per item left
-// long rows to few SIMDs: prompts of up to 1001 tokens 268 us against 153).  A float32
+// long rows to few SIMDs: prompts of up to 1001 tokens 268 us, four waves 153, two 145).  A float32
 // product carries 1/16 of a bfloat16 one's rate, so that the matrix cores bound it: they
 // are busy 82% of a workgroup's tiles, and half of a launch of three such prompts,
 // whose starts, merges and last workgroups they wait for.  K and V go from global
@@ -726,11 +726,10 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 // A dot product is the sum of eight 16-dim chains: its rounding error is that of
 // a pairwise sum.
 constexpr int EX_KEYS32 = 32;
-constexpr int EX_W32 = 4;
 
-template <int PAGED>
-__global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
-  __shared__ __attribute__((aligned(16))) float s_part[EX_W32][66][64];  // the merge; before it the query
+template <int PAGED, int W>
+__global__ __launch_bounds__(W * 64, 2) void k_exact_f32(ExactArgs a) {
+  __shared__ __attribute__((aligned(16))) float s_part[W][66][64];  // the merge; before it the query
   f32x4 (*s_q)[64] = reinterpret_cast<f32x4 (*)[64]>(&s_part[0][0][0]);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -755,7 +754,7 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
   {
     const f32x4* qr = reinterpret_cast<const f32x4*>((const uint8_t*)a.q + (size_t)(it.s0 + tok) * a.qs) + head * (D / 4);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s_q[4 * wave + j][lane] = qr[2 * (4 * wave + j) + half];
+    for (int j = 0; j < 16 / W; ++j) s_q[16 / W * wave + j][lane] = qr[2 * (16 / W * wave + j) + half];
   }
   __syncthreads();
   const uint8_t* kb = (const uint8_t*)a.k + (PAGED ? 0 : (size_t)it.s0 * a.ks + kvh * (D * 4));
@@ -826,11 +825,11 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
   int id = 0;
   if (t0 < t1) {
     resolve(t0, id_of(t0), kp, vp, bad);
-    id = id_of(t0 + EX_W32);
+    id = id_of(t0 + W);
     load_k(kp, 0, k0);
     load_k(kp, 1, k1);
   }
-  for (int t = t0; t < t1; t += EX_W32) {
+  for (int t = t0; t < t1; t += W) {
     load_v(vp, 0, v0);
     __builtin_amdgcn_sched_barrier(0);
     f32x16 s = dots(k0, 0);
@@ -850,8 +849,8 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
     }
     // the next tile's keys load while this tile's values are used (past the
     // last key the loads repeat it)
-    resolve(t + EX_W32, id, kp, vp, bad);
-    id = id_of(t + 2 * EX_W32);
+    resolve(t + W, id, kp, vp, bad);
+    id = id_of(t + 2 * W);
     load_k(kp, 0, k0);
     float tmax = -INFINITY;
 #pragma unroll
@@ -914,8 +913,8 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
     weigh(v1, s, 1, oacc);
   }
   lrun += xor32(lrun);
-  // merge of the four waves, each relative to its own reference; wave w then holds
-  // registers 4 w .. 4 w + 3.  Register i of oacc[0..3]: dims 4 mm .. 4 mm + 3 with
+  // merge of the waves, each relative to its own reference; wave w then holds
+  // registers NR w .. NR w + NR - 1.  Register i of oacc[0..3]: dims 4 mm .. 4 mm + 3 with
   // mm = 8 (i / 4) + 4 half + i % 4
   __syncthreads();  // every wave is done with the query
 #pragma unroll
@@ -925,32 +924,33 @@ __global__ __launch_bounds__(EX_W32 * 64, 2) void k_exact_f32(ExactArgs a) {
   s_part[wave][64][lane] = mrun;
   s_part[wave][65][lane] = lrun;
   __syncthreads();
-  float M = EX_NONE, L = 0.f, wgt[EX_W32];
+  float M = EX_NONE, L = 0.f, wgt[W];
 #pragma unroll
-  for (int w = 0; w < EX_W32; ++w) M = fmaxf(M, s_part[w][64][lane]);
+  for (int w = 0; w < W; ++w) M = fmaxf(M, s_part[w][64][lane]);
 #pragma unroll
-  for (int w = 0; w < EX_W32; ++w) {
+  for (int w = 0; w < W; ++w) {
     wgt[w] = __builtin_amdgcn_exp2f(s_part[w][64][lane] - M);
     L += wgt[w] * s_part[w][65][lane];
   }
   const float inv = nsp > 1 ? 1.0f : L > 0.f || L != L ? 1.0f / L : 0.f;
   const size_t pr = (((size_t)kvh * a.blocks + blk) * a.splits + split) * EX_ROWS_F32 + m;
-  auto dim = [&](int e) { return 4 * (8 * wave + 4 * half + e); };
+  constexpr int NR = 16 / W;  // registers of O that a wave merges
+  auto dim = [&](int e) { const int i = NR * wave + e; return 4 * (8 * (i >> 2) + 4 * half + (i & 3)); };
   auto merged = [&](int e) {
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < EX_W32; ++w)
+    for (int w = 0; w < W; ++w)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) o[b] += wgt[w] * s_part[w][b * 16 + 4 * wave + e][lane];
+      for (int b = 0; b < 4; ++b) o[b] += wgt[w] * s_part[w][b * 16 + NR * wave + e][lane];
     return o * inv;
   };
   float lse = 0.f;
   if (rvalid) {
     if (nsp > 1) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<f32x4*>(a.part_o + pr * D + dim(e)) = merged(e);
+      for (int e = 0; e < NR; ++e) *reinterpret_cast<f32x4*>(a.part_o + pr * D + dim(e)) = merged(e);
     } else {
-      lse = write_row<1, 4>(a, orow, L == 0.f ? -INFINITY : M + log2f(L), merged, dim);
+      lse = write_row<1, NR>(a, orow, L == 0.f ? -INFINITY : M + log2f(L), merged, dim);
     }
   }
   __syncthreads();  // every wave has read the prior's lse, which may be lse itself
@@ -1394,8 +1394,9 @@ hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t s
   const unsigned items = (unsigned)a.Hkv * a.blocks * a.splits;
   if (items == 0) return hipGetLastError();
   if (fp32) {
-    if (paged) hipLaunchKernelGGL((k_exact_f32<1>), dim3(items), dim3(EX_W32 * 64), 0, st, a);
-    else hipLaunchKernelGGL((k_exact_f32<0>), dim3(items), dim3(EX_W32 * 64), 0, st, a);
+    if (paged) hipLaunchKernelGGL((k_exact_f32<1, 4>), dim3(items), dim3(4 * 64), 0, st, a);
+    else if (a.waves == 4) hipLaunchKernelGGL((k_exact_f32<0, 4>), dim3(items), dim3(4 * 64), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_f32<0, 2>), dim3(items), dim3(2 * 64), 0, st, a);
   } else {
     const bool half = a.rows == EX_ROWS / 2;
     if (paged && half) hipLaunchKernelGGL((k_exact_bf16<1, 2>), dim3(items), dim3(512), 0, st, a);

@@ -175,3 +175,13 @@ def test_launches_that_would_be_too_large_are_refused():
 def test_rotate_of_no_tokens_needs_no_addresses():
     """Empty tensors may have none."""
     assert _status("rotate", rotate(num_tokens=0, q=None, k=None, v=None, q_out=None, positions=None, slots=None)) == 0
+
+
+def test_page_attend_refuses_places_that_would_pass_32_bits():
+    for stride, size in (((1 << 27) - 1, 16), ((1 << 27) - 127, 16), ((1 << 21) - 1, 1024)):
+        a = page(table_stride=stride)
+        a.pages.page_size = size
+        assert _status("page_attend", a) == 1
+        assert b"2^31" in pk.lib().protokv_last_error(None)
+    a = page(table_stride=(1 << 27) - 128, max_add=1, workspace=None)
+    assert _status("page_attend", a) == 3   # its sizes are fine
