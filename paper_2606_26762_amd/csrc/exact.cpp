@@ -125,7 +125,7 @@ void plan_blocks_f32(ExactArgs& a, bool paged) {
   a.rows = EX_ROWS_F32;
   a.blocks = (int)((int64_t)a.total * a.grp / EX_ROWS_F32) + a.n;
   a.splits = 1;
-  a.min_tiles = EX_MIN_TILES_F32;
+  a.min_tiles = EX_MIN_TILES;
   a.waves = 4;
   const int64_t items = (int64_t)a.blocks * a.Hkv;
   const int64_t keys = paged ? (int64_t)a.stride << a.shift : ((int64_t)a.total + a.n - 1) / std::max(a.n, 1);
@@ -135,7 +135,7 @@ void plan_blocks_f32(ExactArgs& a, bool paged) {
     return;
   }
   int64_t best = INT64_MAX;
-  for (int s = 1; s <= EX_MAX_SPLITS_F32 && (s == 1 || s <= tiles / EX_MIN_TILES_F32); ++s) {
+  for (int s = 1; s <= EX_MAX_SPLITS_F32 && (s == 1 || s <= tiles / EX_MIN_TILES); ++s) {
     const int64_t turns = ((tiles + s - 1) / s + 3) / 4;  // tiles of a wave
     const int64_t cost = (items * s + 255) / 256 * turns * 20 + (items * s + 511) / 512 * (s > 1 ? 80 : 40) + (s > 1 ? 25 + s / 2 : 0);
     if (cost < best) {
@@ -200,10 +200,17 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   a.shift = log2i(p->pages.page_size);
   a.num_pages = p->pages.num_pages;
   const bool fp32 = h.dtype == PROTOKV_KV_FP32;
-  // requests of few rows go to a kernel of their own, the others to row blocks (a
-  // single request that may have more rows is left to them)
+  // requests of few rows go to a kernel of their own, the others to row blocks.  Its two
+  // launches take 9 us even if no request has few rows; where some may have more, row
+  // blocks take them all if that costs little: blocks that fill a quarter of the GPU at
+  // most (8 x 16 tokens over 2000, 28 / 4 heads: 39 us with them, 31 without; 7 single
+  // tokens over 30 000, 32 / 8 heads, that might have been more: 177 and 156), or 256
+  // rows to a request on average (4 x 512 over 4096: 149 and 140; 4000 and six single
+  // ones over 16 k: 814 and 785).
   const bool many = (int64_t)a.max_add * a.grp > EX_FEW;
-  if (!fp32 && !(many && a.n == 1)) {
+  const int64_t rows = (int64_t)a.total * a.grp;
+  const bool alone = many && ((rows / EX_ROWS + a.n) * a.Hkv <= 64 || rows >= (int64_t)256 * a.n);
+  if (!fp32 && !alone) {
     const int64_t tiles = (((int64_t)a.stride << a.shift) + 31) / 32;
     const int64_t waves = std::max<int64_t>(1, ((int64_t)a.Hkv * a.n * tiles + 1) / 2);
     a.few = a.n ? (int)std::min<int64_t>(EX_FEW_WAVES, (waves + 3) / 4 * 4) : 0;

@@ -16,8 +16,8 @@ std::string& call_error();
 
 constexpr int EX_ROWS = 256;      // query rows per workgroup of the bf16 kernel (8 waves of 32), or half as many
 constexpr int EX_ROWS_F32 = 32;   // query rows per workgroup of the float32 kernel
-constexpr int EX_MAX_SPLITS = 16, EX_MAX_SPLITS_F32 = 64;
-constexpr int EX_MIN_TILES = 8, EX_MIN_TILES_F32 = 4;  // 64-key (bf16) or 32-key (float32) tiles that a context split has at least
+constexpr int EX_MAX_SPLITS = 32, EX_MAX_SPLITS_F32 = 64;
+constexpr int EX_MIN_TILES = 4;  // 64-key (bf16) or 32-key (float32) tiles that a context split has at least
 constexpr int EX_FEW = 32;        // rows per kv head of a request that the few-rows kernel takes
 constexpr int EX_FEW_WAVES = 2048;  // waves of the few-rows kernel, at most (two to a SIMD)
 constexpr int MAX_REQUESTS = 8192;

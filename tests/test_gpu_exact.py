@@ -965,3 +965,18 @@ def test_plan_and_rotation_on_a_stream_of_their_own():
     for f in pk.PagePlan.__slots__:
         assert torch.equal(getattr(a, f), getattr(b, f)), f
     assert torch.equal(ra, rb) and all(torch.equal(x, y) for x, y in zip(args[0], args[1]))
+
+
+def test_pages_few_rows_beside_many():
+    """So many requests that those of few rows go to runs of tiles and the others to
+    row blocks, which split their context."""
+    log("case: few rows beside many")
+    reqs = [(53 * i % 700, 1 + i % 2) for i in range(38)] + [(900, 50), (4000, 20)]
+    _paged(reqs, 6, 2, 16, "bf16", 61, prior=True)
+
+
+@pytest.mark.parametrize("reqs", [[(3000, 1), (10, 1)], [(1, 1), (700, 2), (0, 0), (64, 30)]])
+def test_few_rows_where_there_might_have_been_many(reqs):
+    """max_add above what any request has: row blocks with few rows in them."""
+    log(f"case: few rows, many allowed {reqs}")
+    _paged(reqs, 14, 2, 16, "bf16", 62, prior=True, max_add=300)
