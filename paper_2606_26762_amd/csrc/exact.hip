@@ -1015,7 +1015,7 @@ struct Sum {
 
 // Joins the splits of a row block.  Workgroup = EJ_ROWS rows of one (kv head, row
 // block), 32 threads per row.  A latency chain: block, references, partials (3 x 20
-// rows over 2500 tokens 4.9 us).
+// rows over 2500 tokens in float32 5.3 us).
 constexpr int EJ_ROWS = 16;
 template <int FP32, int R>
 __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
