@@ -980,3 +980,34 @@ def test_few_rows_where_there_might_have_been_many(reqs):
     """max_add above what any request has: row blocks with few rows in them."""
     log(f"case: few rows, many allowed {reqs}")
     _paged(reqs, 14, 2, 16, "bf16", 62, prior=True, max_add=300)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("add,n", [(1, 5), (3, 40), (70, 2)])
+def test_pages_shared_by_requests_strided_queries_no_lse(add, n, dtype):
+    """Requests over the same pages get the same rows, whichever of them asks; queries
+    inside a projection's rows; lse not wanted; k and v one tensor."""
+    import torch
+    log(f"case: shared pages {n} x {add} {dtype}")
+    pk, g = PK(), _g(71)
+    dt, hq, hk, P, ctx = _dt(dtype), 6, 2, 16, 500
+    kv = _randn(g, 40, hk, P, D, dtype=dt)
+    row = torch.randperm(40, generator=g, device="cuda").int()[:(ctx + add + P - 1) // P]
+    table = row.repeat(n, 1).contiguous()
+    cu = _i32([add * i for i in range(n + 1)])
+    lens = _i32([ctx + add] * n)
+    one = _randn(g, add, (hq + 2 * hk) * D, dtype=dt)
+    q = one.repeat(n, 1)[:, :hq * D].unflatten(1, (-1, D))   # rows at the projection's stride
+    assert not q.is_contiguous()
+    o, lse = pk.page_attend(q, (kv, kv), table, cu, lens, add)
+    o2, none = pk.page_attend(q.contiguous(), (kv, kv), table, cu, lens, add, lse=False)
+    torch.cuda.synchronize()
+    assert none is False and torch.equal(o, o2)
+    key = torch.arange(ctx + add, device="cuda")
+    flat = kv[row.long()].permute(1, 0, 2, 3).flatten(1, 2)[:, :ctx + add]
+    seen = key[None] <= (ctx + torch.arange(add, device="cuda"))[:, None]
+    for i in range(n):
+        sl = slice(i * add, (i + 1) * add)
+        for h in range(hq):
+            ref = attend64(q[sl, h], flat[h // 3], flat[h // 3], seen)
+            check(o[sl, h], lse[sl, h], ref, ctx + add, dt, None, f"request {i}, head {h}")
