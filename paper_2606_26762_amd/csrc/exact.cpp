@@ -94,7 +94,6 @@ void plan_blocks(ExactArgs& a, bool paged) {
   const int64_t keys = paged ? (int64_t)a.stride << a.shift : ((int64_t)a.total + a.n - 1) / std::max(a.n, 1);
   const int64_t tiles = (keys + 63) / 64;
   int64_t best = INT64_MAX;
-  a.min_tiles = EX_MIN_TILES;
   for (int half = 0; half <= 1; ++half) {
     const int R = EX_ROWS >> half;
     const int blocks = (int)((int64_t)a.total * a.grp / R) + a.n;
@@ -125,7 +124,6 @@ void plan_blocks_f32(ExactArgs& a, bool paged) {
   a.rows = EX_ROWS_F32;
   a.blocks = (int)((int64_t)a.total * a.grp / EX_ROWS_F32) + a.n;
   a.splits = 1;
-  a.min_tiles = EX_MIN_TILES;
   a.waves = 4;
   const int64_t items = (int64_t)a.blocks * a.Hkv;
   const int64_t keys = paged ? (int64_t)a.stride << a.shift : ((int64_t)a.total + a.n - 1) / std::max(a.n, 1);

@@ -129,13 +129,6 @@ __device__ __forceinline__ bool find_dearest(const ExactArgs& a, int d, Item& it
   return set_item<R>(a, i, __builtin_amdgcn_readlane(c0, i), __builtin_amdgcn_readlane(c1, i), k, it);
 }
 
-// Context splits of a block with `tiles` key tiles, and tiles of each.
-__device__ __forceinline__ int splits_of(const ExactArgs& a, int tiles, int& per) {
-  const int want = min(a.splits, max(1, tiles / a.min_tiles));
-  per = max(1, (tiles + want - 1) / want);
-  return max(1, (tiles + per - 1) / per);
-}
-
 // Weights of a row's own result (log2 of its sum: own2) and of the prior's (its
 // log-sum-exp p), and the log-sum-exp of both.
 struct Join {
@@ -239,10 +232,8 @@ __device__ __forceinline__ void ex_barrier() {
   asm volatile("s_barrier" ::: "memory");
 }
 
-constexpr int EX_KEYS = 64;             // keys per tile
 constexpr int EX_TILE = EX_KEYS * D * 2;  // one K or V tile, 16 KB
 constexpr int EX_NBUF = 4;              // tiles t - 1 and t in use, t + 1 and t + 2 loading
-constexpr int EX_IDS = 1024;            // page ids staged at a time
 
 // Workgroup = eight waves of 32 query rows each.  Tiles of 64 keys go straight from
 // global memory into LDS (global_load_lds_dwordx4), two tiles ahead, four whole rows
@@ -277,7 +268,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     return;  // uniform in the workgroup
   int per;
   const int tiles = (it.kend + EX_KEYS - 1) / EX_KEYS;
-  const int nsp = splits_of(a, tiles, per);
+  const int nsp = ex_splits(a.splits, tiles, per);
   if (split >= nsp) return;
   const int t0 = split * per, t1 = min(tiles, t0 + per);
 
@@ -302,7 +293,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 
   const uint8_t* kb = (const uint8_t*)a.k + (PAGED ? 0 : (size_t)it.s0 * a.ks + kvh * (D * 2));
   const uint8_t* vb = (const uint8_t*)a.v + (PAGED ? 0 : (size_t)it.s0 * a.vs + kvh * (D * 2));
-  const int tpc = PAGED ? (EX_IDS << a.shift) / EX_KEYS : 1;  // tiles per staged run of page ids
+  const int tpc = PAGED ? ex_run_tiles(a.shift) : 1;  // tiles per staged run of page ids
   auto load_ids = [&](int t) {  // the run that tile t is in
     const int e0 = (t / tpc) * EX_IDS, n = min(EX_IDS, ((it.kend - 1) >> a.shift) + 1 - e0);
     const int32_t* row = a.table + (size_t)it.seq * a.stride + e0;
@@ -536,9 +527,11 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 #pragma unroll
   for (int i = 0; i < EX_TILE / 8192; ++i) reinterpret_cast<uint4*>(s_zero)[tid + i * 512] = make_uint4(0, 0, 0, 0);
   if constexpr (PAGED) {
-    // the runs of tiles t0 .. t0 + 3
-    if (t0 < t1) load_ids(t0);
-    if ((t0 + 3) / tpc != t0 / tpc && t0 + 3 < t1) load_ids(t0 + 3);
+    if (t0 < t1) {
+      const int last = ex_ids_last(t0, t1);
+      load_ids(t0);
+      if (last / tpc != t0 / tpc) load_ids(last);
+    }
   }
   ex_barrier();
   // the first tile and the query together, the second tile once they are there: what
@@ -572,9 +565,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     else wait_vm<0>();
     ex_barrier();
     if constexpr (PAGED) {
-      // page ids from tile t + 4 on, located in period t + 1 at the earliest, in the
-      // place of those of tiles up to t + 3 - tpc (tpc >= 16)
-      if (t + 4 < t1 && (t + 4) % tpc == 0) load_ids(t + 4);  // uniform
+      // in the place of the ids of tiles up to t + 3 - tpc
+      if (ex_ids_due(t, t1, tpc)) load_ids(t + 4);  // uniform
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -740,7 +732,7 @@ __global__ __launch_bounds__(W * 64, 2) void k_exact_f32(ExactArgs a) {
     return;  // uniform in the workgroup
   int per;
   const int tiles = (it.kend + EX_KEYS32 - 1) / EX_KEYS32;
-  const int nsp = splits_of(a, tiles, per);
+  const int nsp = ex_splits(a.splits, tiles, per);
   if (split >= nsp) return;
   const int t0 = split * per + wave, t1 = min(tiles, split * per + per);
   const int m = lane & 31, half = lane >> 5;
@@ -1025,7 +1017,7 @@ __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
   if (!find_item<R>(a, blk, it)) return;
   int per;
   const int tiles = (it.kend + (FP32 ? EX_KEYS32 : EX_KEYS) - 1) / (FP32 ? EX_KEYS32 : EX_KEYS);
-  const int nsp = splits_of(a, tiles, per);
+  const int nsp = ex_splits(a.splits, tiles, per);
   if (nsp == 1) return;  // written by the attention itself
   const size_t base = ((size_t)kvh * a.blocks + blk) * a.splits;
   const int lr = part * EJ_ROWS + (threadIdx.x >> 5), r = it.row0 + lr, d4 = threadIdx.x & 31;

@@ -1011,3 +1011,45 @@ def test_pages_shared_by_requests_strided_queries_no_lse(add, n, dtype):
         for h in range(hq):
             ref = attend64(q[sl, h], flat[h // 3], flat[h // 3], seen)
             check(o[sl, h], lse[sl, h], ref, ctx + add, dt, None, f"request {i}, head {h}")
+
+
+# The last context split of these has two or three tiles, and the run of page ids that
+# the second or the third is in begins inside it (tests/test_exact_splits.py replays
+# the staging for all lengths).
+SHORT_LAST = [
+    ([(1024, 16)], 28, 4, 1, None), ([(1050, 128)], 28, 4, 1, None), ([(1072, 16), (1072, 16), (300, 16)], 28, 4, 1, None),
+    ([(1024, 300)], 8, 8, 1, None), ([(2048, 16)], 28, 4, 2, None), ([(6144, 16)], 28, 4, 2, None),
+    ([(8128, 128)], 28, 4, 8, None), ([(16320, 128)], 28, 4, 16, None), ([(16320, 128)], 28, 4, 16, 2048),
+    ([(16320, 100)], 32, 8, 16, None)]
+
+
+@pytest.mark.parametrize("reqs,hq,hk,P,width", SHORT_LAST)
+def test_pages_whose_ids_begin_anew_in_a_short_last_split(reqs, hq, hk, P, width):
+    log(f"case: short last split {reqs} heads {hq}/{hk} page {P} width {width}")
+    _paged(reqs, hq, hk, P, "bf16", 31, width=width)
+
+
+@pytest.mark.parametrize("reqs,hq,hk,P,width", SHORT_LAST)
+def test_page_size_does_not_change_the_result(reqs, hq, hk, P, width):
+    """The same tokens in small pages and in pages of 256, in tables of as many tokens:
+    the same keys in the same order, so the same bits."""
+    import torch
+    log(f"case: small pages and large {reqs} heads {hq}/{hk} page {P} width {width}")
+    pk, g = PK(), _g(32)
+    kv, add = [c + a for c, a in reqs], [a for _, a in reqs]
+    span = ((width * P if width else max(kv)) + 255) // 256 * 256
+    q = _randn(g, sum(add), hq, D, dtype=torch.bfloat16, scale=2.0)
+    k, v = (_randn(g, len(reqs), span, hk, D, dtype=torch.bfloat16) for _ in range(2))
+    got = []
+    for size in (P, 256):
+        n = span // size
+        order = torch.randperm(len(reqs) * n, generator=g, device="cuda")
+        pages = []
+        for x in (k, v):
+            y = torch.empty(len(reqs) * n, hk, size, D, dtype=x.dtype, device="cuda")
+            y[order] = x.view(len(reqs) * n, size, hk, D).transpose(1, 2)
+            pages.append(y)
+        table = order.view(len(reqs), n).int().contiguous()
+        got.append(pk.page_attend(q, pages, table, _i32(np.cumsum([0] + add).tolist()), _i32(kv), max(add)))
+    torch.cuda.synchronize()
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
