@@ -325,7 +325,7 @@ protokv_status protokv_rotate(const protokv_rotate_args* a, void* stream) PKV_GU
   // a wave per token and eight heads (a wave per token, 40 000 tokens of 32 + 8 heads:
   // 156 us against 139)
   r.parts = (r.Hq + (r.nslots ? 2 : 1) * r.Hkv + 7) / 8;
-  if ((int64_t)r.N * r.parts >= (1ll << 32) / 64)  // a launch has fewer than 2^32 threads
+  if (((int64_t)r.N * r.parts + 3) / 4 >= (1ll << 32) / 256)  // a launch has fewer than 2^32 threads, 256 to a workgroup
     return fail(PROTOKV_E_UNSUPPORTED, who, "num_tokens times heads above 2^29");
   std::memcpy(r.axis, a->axes, D / 2);
   for (int i = 0; i < D / 2; ++i) r.inv[i] = std::pow(a->theta, -2.0 * i / D);

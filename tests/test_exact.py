@@ -185,3 +185,11 @@ def test_page_attend_refuses_places_that_would_pass_32_bits():
         assert b"2^31" in pk.lib().protokv_last_error(None)
     a = page(table_stride=(1 << 27) - 128, max_add=1, workspace=None)
     assert _status("page_attend", a) == 3   # its sizes are fine
+
+
+@pytest.mark.parametrize("tokens", [(1 << 26) - 1, (1 << 26) - 3, 1 << 26])
+def test_rotate_refuses_waves_that_make_2_to_32_threads_in_whole_workgroups(tokens):
+    """A wave to a token; workgroups are of four."""
+    a = rotate(num_tokens=tokens, k=None, v=None, slots=None, no_pages=True)
+    assert _status("rotate", a) == 2
+    assert b"2^29" in pk.lib().protokv_last_error(None)
