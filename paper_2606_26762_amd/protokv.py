@@ -468,7 +468,8 @@ class ProtoKV:
 
 # -- exact attention around the readout (no handle) ---------------------------
 # One token's call takes a few microseconds on the GPU, so what these do in Python
-# counts: each tensor is looked at once.
+# counts: each tensor is looked at once.  Results carry no gradient: tensors that ask
+# for one are refused while gradients are on.
 
 
 def _device(t, stream) -> int:
@@ -496,6 +497,13 @@ def _kv(dtype) -> int:
     raise ValueError(f"expected bfloat16 or float32, got {dtype}")
 
 
+def _no_gradient(name):
+    import torch
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name}: requires a gradient, which these calls do not give (detach it, or call under "
+                         "torch.no_grad())")
+
+
 def _rows(t, name, dtype=None, dev=None):
     """-> (pointer, row stride in elements) of token rows [N][heads][D]."""
     shape = t.shape
@@ -503,6 +511,8 @@ def _rows(t, name, dtype=None, dev=None):
             dev is not None and t.get_device() != dev):
         raise ValueError(f"{name}: expected rows [N, heads, 128] in {dtype} on the current device, got "
                          f"{t.dtype} {tuple(shape)} on {t.device}")
+    if t.requires_grad:
+        _no_gradient(name)
     s0, s1, s2 = t.stride()
     if shape[0] > 0 and (s2 != 1 or (shape[1] > 1 and s1 != 128)):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
@@ -514,6 +524,8 @@ def _flat(t, name, dtype, dev, *shape) -> int:
     if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor {shape} on the current device, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.requires_grad:
+        _no_gradient(name)
     return t.data_ptr()
 
 

@@ -193,3 +193,45 @@ def test_rotate_refuses_waves_that_make_2_to_32_threads_in_whole_workgroups(toke
     a = rotate(num_tokens=tokens, k=None, v=None, slots=None, no_pages=True)
     assert _status("rotate", a) == 2
     assert b"2^29" in pk.lib().protokv_last_error(None)
+
+
+def _calls_with(**leaf):
+    """Each call that takes floating-point tensors, with those named in `leaf` in place of its own."""
+    t = dict(q=torch.zeros(4, 8, 128), k=torch.zeros(4, 2, 128), v=torch.zeros(4, 2, 128), k_pages=torch.zeros(3, 2, 16, 128),
+             v_pages=torch.zeros(3, 2, 16, 128), out=torch.zeros(4, 8, 128), prior_o=torch.zeros(4, 8, 128))
+    t.update(leaf)
+    i32 = dict(dtype=torch.int32)
+    cu, one, pages = torch.tensor([0, 4], **i32), torch.tensor([20], **i32), (t["k_pages"], t["v_pages"])
+    prior = (t["prior_o"], torch.zeros(4, 8))
+    uses = {
+        "rotate": ("q k v k_pages v_pages out", lambda: pk.rotate(
+            t["q"], t["k"], torch.zeros(4, **i32), pk.pair_axes((64,)), 1e4, q_out=t["out"], v=t["v"], pages=pages,
+            slots=torch.zeros(4, **i32))),
+        "prompt_attend": ("q k v out prior_o", lambda: pk.prompt_attend(t["q"], t["k"], t["v"], cu, out=t["out"], prior=prior)),
+        "page_attend": ("q k_pages v_pages out prior_o", lambda: pk.page_attend(
+            t["q"], pages, torch.zeros(1, 3, **i32), cu, one, 4, out=t["out"], prior=prior))}
+    return [f for names, f in uses.values() if set(leaf) <= set(names.split())]
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "k_pages", "v_pages", "out", "prior_o"])
+def test_binding_refuses_what_a_gradient_is_asked_of(name, monkeypatch):
+    """The results would carry none; with gradients off, the same tensors are only values."""
+    monkeypatch.setattr(pk, "_device", lambda t, stream: -1)   # host tensors pass as those of the current device
+    monkeypatch.setattr(pk, "_raw_stream", lambda stream, dev: None)
+    done = []
+    monkeypatch.setattr(pk, "_check", lambda status: done.append(status))
+    class Library:   # launches nothing
+        def __getattr__(self, call):
+            return lambda *a: 0
+    monkeypatch.setattr(pk, "lib", Library)
+    shape = dict(q=(4, 8, 128), out=(4, 8, 128), prior_o=(4, 8, 128), k=(4, 2, 128), v=(4, 2, 128)).get(name, (3, 2, 16, 128))
+    calls = _calls_with(**{name: torch.zeros(*shape, requires_grad=True)})
+    assert calls
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    assert not done
+    with torch.no_grad():
+        for call in calls:
+            call()
+    assert len(done) >= len(calls)
