@@ -54,9 +54,13 @@ protokv_status check_rows(const void* p, int64_t stride, int heads, const Heads&
   return PROTOKV_OK;
 }
 
-protokv_status check_pages(const protokv_pages& p, const char* who) {
+protokv_status check_page_rows(const protokv_pages& p, const char* who) {
   if (!p.k || !p.v || off16(p.k) || off16(p.v))
     return fail(PROTOKV_E_INVALID, who, "pages: k and v must be non-NULL and aligned to 16 bytes");
+  return PROTOKV_OK;
+}
+
+protokv_status check_page_sizes(const protokv_pages& p, const char* who) {
   if (p.num_pages < 1) return fail(PROTOKV_E_INVALID, who, "num_pages must be >= 1");
   if (!pow2(p.page_size) || p.page_size > 1024)
     return fail(PROTOKV_E_UNSUPPORTED, who, "page_size must be a power of two in [1, 1024]");
@@ -151,7 +155,7 @@ protokv_status check_grid(const ExactArgs& a, const char* who) {
 }
 
 // The workspace's parts, from `base` on (may be null); its size.
-size_t lay_out(ExactArgs& a, bool fp32, uint8_t* base) {
+size_t lay_out(ExactArgs& a, uint8_t* base) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
     uint8_t* p = base ? base + off : nullptr;
@@ -180,11 +184,8 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   if ((int64_t)p->total * h.q >= (1ll << 31) || p->num_requests >= (1 << 24))
     return fail(PROTOKV_E_UNSUPPORTED, who, "total * num_q_heads must be below 2^31, the number of sequences below 2^24");
   if (p->max_add < 1) return fail(PROTOKV_E_INVALID, who, "max_add must be >= 1");
-  if (p->pages.num_pages < 1) return fail(PROTOKV_E_INVALID, who, "num_pages must be >= 1");
-  if (!pow2(p->pages.page_size) || p->pages.page_size > 1024)
-    return fail(PROTOKV_E_UNSUPPORTED, who, "page_size must be a power of two in [1, 1024]");
-  if ((int64_t)p->pages.num_pages * p->pages.page_size >= (1ll << 31))
-    return fail(PROTOKV_E_UNSUPPORTED, who, "num_pages * page_size must be below 2^31");
+  s = check_page_sizes(p->pages, who);
+  if (s != PROTOKV_OK) return s;
   // (the places of a few tiles behind the last token are formed in 32 bits)
   if (p->table_stride < 1 || (int64_t)p->table_stride * p->pages.page_size > (1ll << 31) - 2048)
     return fail(PROTOKV_E_INVALID, who, "table_stride must be >= 1 and table_stride * page_size at most 2^31 - 2048");
@@ -281,7 +282,8 @@ protokv_status protokv_rotate(const protokv_rotate_args* a, void* stream) PKV_GU
   RotateArgs r;
   std::memset(&r, 0, sizeof(r));
   if (a->pages) {
-    s = check_pages(*a->pages, who);
+    s = check_page_rows(*a->pages, who);
+    if (s == PROTOKV_OK) s = check_page_sizes(*a->pages, who);
     if (s != PROTOKV_OK) return s;
     r.kp = (uint8_t*)a->pages->k;
     r.vp = (uint8_t*)a->pages->v;
@@ -374,7 +376,7 @@ protokv_status protokv_page_attend_workspace(const protokv_page_attend_args* p, 
   if (!p || !bytes) return fail(PROTOKV_E_INVALID, who, "args and bytes must be non-NULL");
   ExactArgs a{};
   protokv_status s = page_attend_shape(p, a, who);
-  if (s == PROTOKV_OK) *bytes = lay_out(a, p->kv_dtype == PROTOKV_KV_FP32, nullptr);
+  if (s == PROTOKV_OK) *bytes = lay_out(a, nullptr);
   return s;
 })
 
@@ -387,19 +389,19 @@ protokv_status protokv_page_attend(const protokv_page_attend_args* p, void* stre
   const Heads h{p->num_q_heads, p->num_kv_heads, p->head_dim, p->kv_dtype};
   s = check_result(h, p->num_requests, p->total, p->cu, p->o, p->lse, p->prior_o, p->prior_lse, who);
   if (s != PROTOKV_OK || p->num_requests == 0 || p->total == 0) return s;
-  s = check_pages(p->pages, who);
+  s = check_page_rows(p->pages, who);
   if (s == PROTOKV_OK) s = check_rows(p->q, p->q_stride, h.q, h, who, "q");
   if (s != PROTOKV_OK) return s;
   if (!p->kv_len || !p->table || off4(p->kv_len) || off4(p->table))
     return fail(PROTOKV_E_INVALID, who, "kv_len and table must be non-NULL and aligned to 4 bytes");
   const bool fp32 = h.dtype == PROTOKV_KV_FP32;
-  const size_t need = lay_out(a, fp32, nullptr);
+  const size_t need = lay_out(a, nullptr);
   if (need) {
     if (!p->workspace) return fail(PROTOKV_E_WORKSPACE, who, "workspace is NULL");
     if ((uintptr_t)p->workspace % 256) return fail(PROTOKV_E_WORKSPACE, who, "workspace must be 256-byte aligned");
     if (p->workspace_bytes < need)
       return fail(PROTOKV_E_WORKSPACE, who, ("workspace too small: need " + std::to_string(need) + " bytes").c_str());
-    lay_out(a, fp32, (uint8_t*)p->workspace);
+    lay_out(a, (uint8_t*)p->workspace);
   }
   a.q = p->q;
   a.k = p->pages.k;
