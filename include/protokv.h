@@ -572,7 +572,8 @@ typedef struct {
   int32_t num_requests;   /* n, 0..2^24 - 1 */
   int32_t total;          /* rows of q and o; total * Hq < 2^31 */
   int32_t max_add;        /* no request has more rows (rows beyond are left as they were), >= 1 */
-  int32_t table_stride;   /* table_stride * page_size at most 2^31 - 2048 */
+  int32_t table_stride;   /* table_stride * page_size at most 2^31 - 2048; launches and workspace are
+                           * planned for contexts that fill a row of the table */
   const int32_t* cu;      /* device [n + 1] */
   const int32_t* kv_len;  /* device [n]: tokens in the pages, the new ones among them */
   const int32_t* table;   /* device [n][table_stride] */

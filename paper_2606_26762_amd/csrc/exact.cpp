@@ -90,7 +90,12 @@ protokv_status check_result(const Heads& h, int n, int total, const int32_t* cu,
 // tenths of a 64-key tile's time in the form of 256 rows (about 2 us): a tile takes
 // 10 (128 rows, two waves to a row's keys: 6), a workgroup 40 to start and to end (50
 // with the waves' merge), a split 60 more for its partial; `slots` workgroups run at a time.  Prompts see half their keys on
-// average and take at least as long as their last rows.  Measured, 28 / 4 heads: one
+// average and take at least as long as the last rows of a sequence of mean length.  The
+// lengths are on the device: the host knows the mean of a prompt's, not the longest,
+// and of contexts the table's width, so that unequal prompts' last rows are counted
+// short, and contexts that leave most of the table empty are split for keys that are not
+// there (8 x 64 tokens over 2000, 28 / 4 heads: 52 us in a table of 2064 tokens, unsplit,
+// 62 in one of 32 768).  Measured, 28 / 4 heads, tables as wide as the contexts: one
 // prompt of 1500 tokens 43 us by 256 rows, 34 by 128; eight of 200 17 and 25; one of
 // 4000 115 and 146; 4 x 512 tokens over 16 k in 3 splits 540, unsplit 484.
 void plan_blocks(ExactArgs& a, bool paged) {
@@ -122,7 +127,7 @@ void plan_blocks(ExactArgs& a, bool paged) {
 // 20 tokens over 2500, 6 / 2 heads: nine tiles and more to a split 31 us, four 22; 8 single
 // tokens over 2000, 28 / 4 heads: 252 workgroups 31 us, 288 37).  Prompts: four waves, or
 // two, which leave less of a short row idle and merge less, where the launch lasts
-// several times as long as its longest rows (32 of 200 tokens, 28 / 4 heads: four waves 205
+// several times as long as the last rows of a sequence of mean length (32 of 200 tokens, 28 / 4 heads: four waves 205
 // us, two 154; 4 of 800 223 and 214; but one of 1500 188 and 215, one of 200 20 and 27).
 void plan_blocks_f32(ExactArgs& a, bool paged) {
   a.rows = EX_ROWS_F32;

@@ -245,8 +245,9 @@ constexpr int EX_NBUF = 4;              // tiles t - 1 and t in use, t + 1 and t
 // V^T through ds_read_b64_tr_b16: each lane holds one query column, so the
 // softmax is lane-local plus one exchange with the partner lane.
 // Bound by the matrix cores at the clock that their power leaves: 8192 tokens of
-// 32 / 8 heads 511 us, 1.08 PFLOP/s of what is seen (a plain product of 8192^3
-// reaches 1.12), 4 x 512 tokens over 16 384 of 28 / 4 heads 490 us, 1.0.  KH = 2:
+// 32 / 8 heads 503 - 516 us, 1.08 PFLOP/s of what is seen (a plain product of 8192^3
+// reaches 1.12), 4 x 512 tokens over 16 384 of 28 / 4 heads 477 - 502 us, 1.0, in one
+// round of 224 workgroups: an eighth of the compute units has none.  KH = 2:
 // two waves take a row's keys, half of every tile each; 128 rows to a workgroup, for
 // launches that 256 would leave in few rounds (the rule and its figures stand
 // with the host's block counts).
@@ -354,7 +355,11 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   f32x16 s[2];     // scores, then weights (KH = 2: of even and odd 16-dim steps, then all in the first)
   bf16x8 p_next;   // the first step's weights
   bf16x8 v_next[4];  // and its V operands
-  // P operand of 16-key step st: the weights in bfloat16
+  // P operand of 16-key step st: the weights in bfloat16, the type in which the matrix
+  // core takes the values at 16 times float32's rate; each is within 2^-8 of itself.  Sums,
+  // references and O stay float32, and the sum is of the unrounded weights: outputs are
+  // within 2.3e-3 of float64's (relative, in the mean square), 1.7e-3 with the output's own
+  // rounding alone.
   auto weight_operand = [&](int st) {
     bf16x8 p;
 #pragma unroll
@@ -1037,7 +1042,8 @@ __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
 // tile's loads in flight.  An item within one run is written out; of one
 // that runs on, each wave leaves a partial (at most two per wave: the item it ends
 // in, slot 1, and the one it continues, slot 0), and the wave that the item begins
-// in notes it for k_exact_few_join.  64 requests over 1.07 GB of pages: 198 us, 5.4
+// in notes it for k_exact_few_join.  Every wave sums the tiles of all requests, n / 64
+// steps, which is made for thousands of them.  64 requests over 1.07 GB of pages: 198 us, 5.4
 // TB/s; one over 1500 tokens 9.6 us, the chain of its two or three tiles.
 constexpr int FW_W = 4;              // waves per workgroup
 constexpr int FW_VB = 32 * 64 + 64;  // bytes of one 32-dim block of a V tile (64 of padding: bank spread)
