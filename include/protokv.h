@@ -604,6 +604,185 @@ protokv_status protokv_page_attend(const protokv_page_attend_args* a, void* stre
  * pointers of `a` are not looked at; 0: none is needed).  Host only. */
 protokv_status protokv_page_attend_workspace(const protokv_page_attend_args* a, size_t* bytes);
 
+/* ---------------------------------------------------------------------------
+ * A serving step's other calls around the paged dialogue, under the same
+ * conventions: heads that are normalised before they turn, a cache in 4 bits,
+ * and dialogues that several answers share.
+ * --------------------------------------------------------------------------- */
+
+typedef struct {
+  const void* q_weight;   /* device, kv_dtype [D], or NULL: ones */
+  const void* k_weight;   /* likewise */
+  double eps;             /* finite, >= 0 */
+} protokv_head_norm;
+
+/* protokv_rotate of normalised heads: every head x of q and of k is first
+ * replaced by x / sqrt(mean(x^2) + eps) * weight.  The mean is taken in
+ * float64, the quotient, the weight and the rotation in float32, and the
+ * result is rounded once.  v is stored as it is.  (A head of zeros with eps = 0
+ * gives NaN.) */
+protokv_status protokv_norm_rotate(const protokv_rotate_args* a, const protokv_head_norm* norm, void* stream);
+
+/* A cache of keys and values in 4 bits, in pages as protokv_pages.  A row of
+ * 128 dims is four blocks of 32.  A block has a scale 2^(s - 127) of one byte s
+ * and a code for each value: bits 0..2 choose one of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and bit 3 is the sign; dim 2 i has the low half of byte i of its row.  The
+ * value is the product of the two in float32, which bfloat16 holds exactly
+ * (s = 255: NaN, whatever the codes).
+ * Of a block, protokv_page4_store writes the least scale 2^e, e in -125..125,
+ * with max |x| <= 7 * 2^e (125 if there is none, -125 for zeros), and to each
+ * value the nearest code: between two the one with bit 0 clear, beyond 6 the
+ * last.  No value is then off by more than half a step of its code, but where
+ * e is at an end of its range.  A block that holds an infinity or NaN gets s = 255
+ * and codes of 0. */
+typedef struct {
+  uint8_t* k;             /* device [num_pages][num_kv_heads][page_size][D / 2] */
+  uint8_t* v;             /* likewise; both aligned to 16 bytes */
+  uint8_t* k_scale;       /* device [num_pages][num_kv_heads][page_size][D / 32] */
+  uint8_t* v_scale;       /* likewise; both aligned to 4 bytes */
+  int32_t num_pages;      /* num_pages * page_size < 2^31 */
+  int32_t page_size;      /* a power of two, 1..1024 */
+} protokv_pages4;
+
+typedef struct {
+  int32_t num_tokens;     /* N, >= 0 (0: nothing is done); 2 N num_kv_heads < 2^29 */
+  int32_t num_kv_heads, head_dim, kv_dtype;
+  void* k;                /* device rows of num_kv_heads heads: read by store, written by read */
+  void* v;
+  int64_t k_stride, v_stride;
+  const int32_t* slots;   /* device [N]: slot of each token */
+  protokv_pages4 pages;
+} protokv_page4_rows_args;
+
+/* Rows of k and v into their slots; a slot outside the pages: not stored.  The
+ * slots of one call that name a place in the pages are distinct (of two rows
+ * with one slot, parts of either may stay). */
+protokv_status protokv_page4_store(const protokv_page4_rows_args* a, void* stream);
+
+/* Rows of k and v from their slots (which may repeat), as the values that the
+ * cache holds; a slot outside the pages: zeros. */
+protokv_status protokv_page4_read(const protokv_page4_rows_args* a, void* stream);
+
+typedef struct {
+  int32_t num_q_heads, num_kv_heads, head_dim;
+  int32_t kv_dtype;       /* of q, o and the prior */
+  int32_t num_requests, total, max_add, table_stride;  /* these and the rest as in protokv_page_attend_args */
+  const int32_t* cu;
+  const int32_t* kv_len;
+  const int32_t* table;
+  const void* q;
+  int64_t q_stride;
+  protokv_pages4 pages;
+  void* o;
+  float* lse;
+  const void* prior_o;
+  const float* prior_lse;
+  void* workspace;        /* device, protokv_page4_attend_workspace bytes, 256-byte aligned */
+  size_t workspace_bytes;
+} protokv_page4_attend_args;
+
+/* protokv_page_attend over a cache in 4 bits: every rule of that call, with the
+ * values that the cache holds, which enter the products exactly. */
+protokv_status protokv_page4_attend(const protokv_page4_attend_args* a, void* stream);
+
+/* Bytes of workspace for these sizes, as protokv_page_attend_workspace.  Host only. */
+protokv_status protokv_page4_attend_workspace(const protokv_page4_attend_args* a, size_t* bytes);
+
+/* Pages that several requests hold.  shares (device int32 [num_pages]) counts
+ * the owners of each page beyond its first: 0 for a page that one request holds
+ * (as protokv_page_plan grants them) and for a free one; entries are >= 0.
+ * protokv_page_fork adds owners, protokv_page_release takes them away.  Only
+ * full pages are shared, so that protokv_page_plan's new tokens, which go
+ * behind a request's last one, never meet another request's.  A request some of
+ * whose pages may be shared is ended by protokv_page_release, not by
+ * protokv_page_plan's add < 0, which gives its pages back whoever else holds
+ * them. */
+
+typedef struct {
+  int32_t num_forks;      /* n, 1..8192 */
+  int32_t num_requests;   /* rows of the table, 1..8192 */
+  int32_t num_pages, page_size;  /* as in protokv_page_plan_args */
+  int32_t table_stride;
+  const int32_t* ctx;     /* device [num_requests]: tokens held (taken within [0, table_stride * page_size]) */
+  const int32_t* src;     /* device [n]: request that is forked */
+  const int32_t* dst;     /* device [n]: request that it becomes, which holds no tokens */
+  const int32_t* at;      /* device [n] or NULL: tokens to take (within [0, ctx]; NULL: all of them) */
+  int32_t* table;         /* device [num_requests][table_stride], in and out */
+  int32_t* shares;        /* device [num_pages], in and out */
+  const int32_t* free_pages;  /* device [num_pages]: the stack */
+  const int32_t* free_count;  /* device [1] (taken within [0, num_pages]) */
+  int32_t* free_count_out;    /* device [1] */
+  int32_t* ctx_out;       /* device [num_requests]: after the call */
+  int32_t* lens;          /* device [n] out: tokens of each fork, -1: refused */
+  int32_t* copy_src;      /* device [n] out: page that holds the fork's last rows, -1: none is to be copied */
+  int32_t* copy_dst;      /* device [n] out: its own page for them, or -1 */
+  int32_t* copy_rows;     /* device [n] out: how many, 0 .. page_size - 1 */
+  int32_t* refused;       /* device [1] out or NULL: forks that were refused */
+} protokv_page_fork_args;
+
+/* Requests that begin as copies of others.  Fork i takes the first L tokens of
+ * request src[i]: its floor(L / page_size) full pages enter dst[i]'s table row
+ * and get one owner more each; if tokens are left, a page from the stack enters
+ * behind them, and the three copy arrays say which rows protokv_page_copy has
+ * to bring there, in every layer.  Pages are taken in fork order.  A fork is refused if src or
+ * dst is no request or they are the same, if dst holds tokens, is the src of a
+ * fork of this call or the dst of an earlier one (forks whose src or dst is no
+ * request, or the same, do not count for that), or if it needs a page and those
+ * asked for up to and including it (by forks not refused for other reasons) are
+ * more than the stack holds.
+ * Outputs must not overlap the inputs nor each other. */
+protokv_status protokv_page_fork(const protokv_page_fork_args* a, void* stream);
+
+typedef struct {
+  void* base;             /* device, aligned to 16 bytes: [layers][num_pages][num_kv_heads][page_size] rows */
+  int32_t row_bytes;      /* a multiple of 4, up to 4096 */
+  int32_t layers;         /* >= 1 */
+  int64_t layer_stride;   /* bytes between layers, a multiple of 16 (one layer: any) */
+} protokv_page_array;
+
+typedef struct {
+  int32_t num_copies;     /* n, >= 0 */
+  int32_t num_kv_heads, num_pages, page_size;
+  int32_t num_arrays;     /* 1..128, with at most 65535 layers in all */
+  const protokv_page_array* arrays;  /* host */
+  const int32_t* src;     /* device [n]: pages */
+  const int32_t* dst;     /* device [n] */
+  const int32_t* rows;    /* device [n] or NULL: first rows of each head to copy (within [0, page_size]; NULL: all) */
+} protokv_page_copy_args;
+
+/* Rows 0 .. rows[i] - 1 of every head of page src[i] to page dst[i], in every
+ * layer of every array (keys and values, and the scales of a cache in 4 bits).
+ * Nothing is copied where src or dst is outside [0, num_pages) or they are the same.  The
+ * dst that name a page are distinct and no src of the call (else parts of either
+ * may be there). */
+protokv_status protokv_page_copy(const protokv_page_copy_args* a, void* stream);
+
+typedef struct {
+  int32_t num_requests;   /* n, 1..8192 */
+  int32_t num_pages, page_size;  /* as in protokv_page_plan_args */
+  int32_t table_stride;
+  const int32_t* ctx;     /* device [n]: tokens held (taken within [0, table_stride * page_size]) */
+  const int32_t* keep;    /* device [n]: tokens that stay (<= 0: none; ctx or more: all) */
+  const int32_t* table;   /* device [n][table_stride] */
+  int32_t* shares;        /* device [num_pages], in and out */
+  int32_t* free_pages;    /* device [num_pages], in and out: the stack */
+  const int32_t* free_count;  /* device [1] (taken within [0, num_pages]) */
+  int32_t* free_count_out;    /* device [1] */
+  int32_t* ctx_out;       /* device [n]: after the call */
+  int32_t* refused;       /* device [1] out */
+  int32_t* scratch;       /* device [ceil(num_pages / 4096)] */
+} protokv_page_release_args;
+
+/* Requests give up what is behind their first `keep` tokens.  Each page that a
+ * request drops loses one owner; those that have none left go onto the stack in
+ * the order of their numbers.  Table rows are left as they are (ctx_out says how
+ * much of them counts).  A request that would keep a part of a page that another one
+ * holds (as shares says before the call) is refused and left as it was: tokens that it then adds
+ * would be written over the other's; protokv_page_fork at that token and a
+ * release of the whole request do the same.  Entries outside [0, num_pages) are
+ * passed over.  Outputs must not overlap the inputs nor each other. */
+protokv_status protokv_page_release(const protokv_page_release_args* a, void* stream);
+
 /* Message for the last failure on h (or, when h is NULL, of protokv_init and
  * of the calls that take no handle, on this thread).
  * Valid until the next call on h. */

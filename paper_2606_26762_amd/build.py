@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libprotokv.so")
-SOURCES = ["protokv.cpp", "fold.hip", "query.hip", "warmup.hip", "exact.cpp", "exact.hip", "tokens.hip"]
+SOURCES = ["protokv.cpp", "fold.hip", "query.hip", "warmup.hip", "exact.cpp", "exact.hip", "tokens.hip",
+           "pages.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

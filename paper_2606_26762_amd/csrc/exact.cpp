@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "exact.h"
 #include "pkv_internal.h"
@@ -60,12 +61,51 @@ protokv_status check_page_rows(const protokv_pages& p, const char* who) {
   return PROTOKV_OK;
 }
 
-protokv_status check_page_sizes(const protokv_pages& p, const char* who) {
-  if (p.num_pages < 1) return fail(PROTOKV_E_INVALID, who, "num_pages must be >= 1");
-  if (!pow2(p.page_size) || p.page_size > 1024)
+protokv_status check_page_sizes(int num_pages, int page_size, const char* who) {
+  if (num_pages < 1) return fail(PROTOKV_E_INVALID, who, "num_pages must be >= 1");
+  if (!pow2(page_size) || page_size > 1024)
     return fail(PROTOKV_E_UNSUPPORTED, who, "page_size must be a power of two in [1, 1024]");
-  if ((int64_t)p.num_pages * p.page_size >= (1ll << 31))
+  if ((int64_t)num_pages * page_size >= (1ll << 31))
     return fail(PROTOKV_E_UNSUPPORTED, who, "num_pages * page_size must be below 2^31");
+  return PROTOKV_OK;
+}
+
+protokv_status check_pages4(const protokv_pages4& p, int heads, const char* who) {
+  // (a page's row is found in 32 bits)
+  if ((int64_t)p.num_pages * p.page_size * heads >= (1ll << 32))
+    return fail(PROTOKV_E_UNSUPPORTED, who, "num_pages * page_size * num_kv_heads must be below 2^32");
+  if (!p.k || !p.v || off16(p.k) || off16(p.v))
+    return fail(PROTOKV_E_INVALID, who, "pages: k and v must be non-NULL and aligned to 16 bytes");
+  if (!p.k_scale || !p.v_scale || off4(p.k_scale) || off4(p.v_scale))
+    return fail(PROTOKV_E_INVALID, who, "pages: k_scale and v_scale must be non-NULL and aligned to 4 bytes");
+  return PROTOKV_OK;
+}
+
+// Requests' block tables, as protokv_page_plan takes them.
+protokv_status check_table(int requests, int num_pages, int page_size, int stride, const char* who) {
+  if (requests < 1) return fail(PROTOKV_E_INVALID, who, "num_requests must be >= 1");
+  if (requests > MAX_REQUESTS) return fail(PROTOKV_E_UNSUPPORTED, who, "num_requests above 8192");
+  protokv_status s = check_page_sizes(num_pages, page_size, who);
+  if (s != PROTOKV_OK) return s;
+  if (num_pages > (1 << 29)) return fail(PROTOKV_E_UNSUPPORTED, who, "num_pages above 2^29");
+  if (stride < 1 || (int64_t)stride * page_size >= (1ll << 31))
+    return fail(PROTOKV_E_INVALID, who, "table_stride must be >= 1 and table_stride * page_size below 2^31");
+  return PROTOKV_OK;
+}
+
+// Arrays of int32: what a call needs, and outputs that are none of its inputs nor each other.
+protokv_status check_arrays(std::initializer_list<const void*> need, std::initializer_list<const void*> maybe,
+                            std::initializer_list<const void*> in, std::initializer_list<const void*> out, const char* who) {
+  for (const void* p : need)
+    if (!p || off4(p)) return fail(PROTOKV_E_INVALID, who, "arrays must be non-NULL and aligned to 4 bytes");
+  for (const void* p : maybe)
+    if (off4(p)) return fail(PROTOKV_E_INVALID, who, "arrays must be aligned to 4 bytes");
+  for (auto q = out.begin(); q != out.end(); ++q) {
+    for (const void* p : in)
+      if (p && p == *q) return fail(PROTOKV_E_INVALID, who, "an output must not be one of the inputs");
+    for (auto p = out.begin(); p != q; ++p)
+      if (*p && *p == *q) return fail(PROTOKV_E_INVALID, who, "two outputs are the same array");
+  }
   return PROTOKV_OK;
 }
 
@@ -189,7 +229,7 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   if ((int64_t)p->total * h.q >= (1ll << 31) || p->num_requests >= (1 << 24))
     return fail(PROTOKV_E_UNSUPPORTED, who, "total * num_q_heads must be below 2^31, the number of sequences below 2^24");
   if (p->max_add < 1) return fail(PROTOKV_E_INVALID, who, "max_add must be >= 1");
-  s = check_page_sizes(p->pages, who);
+  s = check_page_sizes(p->pages.num_pages, p->pages.page_size, who);
   if (s != PROTOKV_OK) return s;
   // (the places of a few tiles behind the last token are formed in 32 bits)
   if (p->table_stride < 1 || (int64_t)p->table_stride * p->pages.page_size > (1ll << 31) - 2048)
@@ -226,47 +266,7 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   return check_grid(a, who);
 }
 
-}  // namespace
-
-// What a check or a message allocates may fail; nothing may leave a C entry.
-#define PKV_GUARD(who, ...)                                      \
-  try __VA_ARGS__ catch (...) {                                  \
-    try { call_error() = who ": out of memory"; } catch (...) {} \
-    return PROTOKV_E_DEVICE;                                     \
-  }
-
-extern "C" {
-
-protokv_status protokv_page_plan(const protokv_page_plan_args* a, void* stream) PKV_GUARD("page_plan", {
-  const char* who = "page_plan";
-  if (!a) return fail(PROTOKV_E_INVALID, who, "args is NULL");
-  if (a->num_requests < 1) return fail(PROTOKV_E_INVALID, who, "num_requests must be >= 1");
-  if (a->num_requests > MAX_REQUESTS) return fail(PROTOKV_E_UNSUPPORTED, who, "num_requests above 8192");
-  if (a->num_pages < 1) return fail(PROTOKV_E_INVALID, who, "num_pages must be >= 1");
-  if (!pow2(a->page_size) || a->page_size > 1024)
-    return fail(PROTOKV_E_UNSUPPORTED, who, "page_size must be a power of two in [1, 1024]");
-  if ((int64_t)a->num_pages * a->page_size >= (1ll << 31))
-    return fail(PROTOKV_E_UNSUPPORTED, who, "num_pages * page_size must be below 2^31");
-  if (a->table_stride < 1 || (int64_t)a->table_stride * a->page_size >= (1ll << 31))
-    return fail(PROTOKV_E_INVALID, who, "table_stride must be >= 1 and table_stride * page_size below 2^31");
-  if (a->num_pages > (1 << 29)) return fail(PROTOKV_E_UNSUPPORTED, who, "num_pages above 2^29");
-  if (a->max_tokens < 1 || a->max_tokens > (1 << 29)) return fail(PROTOKV_E_INVALID, who, "max_tokens must be in [1, 2^29]");
-  const void* need[] = {a->ctx, a->add, a->table, a->free_pages, a->free_count, a->free_count_out, a->cu, a->kv_len, a->slots};
-  for (const void* p : need)
-    if (!p || off4(p)) return fail(PROTOKV_E_INVALID, who, "arrays must be non-NULL and aligned to 4 bytes");
-  if (off4(a->base) || off4(a->positions) || off4(a->refused))
-    return fail(PROTOKV_E_INVALID, who, "arrays must be aligned to 4 bytes");
-  // every workgroup reads the inputs while the first writes the outputs
-  const void* in[] = {a->ctx, a->add, a->base, a->free_count};
-  const void* out[] = {a->free_count_out, a->cu, a->kv_len, a->slots, a->positions, a->refused};
-  for (const void* p : in)
-    for (const void* q : out)
-      if (p && p == q) return fail(PROTOKV_E_INVALID, who, "an output must not be one of ctx, add, base and free_count");
-  return device(launch_page_plan(*a, (hipStream_t)stream), who);
-})
-
-protokv_status protokv_rotate(const protokv_rotate_args* a, void* stream) PKV_GUARD("rotate", {
-  const char* who = "rotate";
+protokv_status rotate(const protokv_rotate_args* a, const protokv_head_norm* norm, void* stream, const char* who) {
   if (!a) return fail(PROTOKV_E_INVALID, who, "args is NULL");
   const Heads h{a->num_q_heads, a->num_kv_heads, a->head_dim, a->kv_dtype};
   protokv_status s = check_heads(h, who);
@@ -288,7 +288,7 @@ protokv_status protokv_rotate(const protokv_rotate_args* a, void* stream) PKV_GU
   std::memset(&r, 0, sizeof(r));
   if (a->pages) {
     s = check_page_rows(*a->pages, who);
-    if (s == PROTOKV_OK) s = check_page_sizes(*a->pages, who);
+    if (s == PROTOKV_OK) s = check_page_sizes(a->pages->num_pages, a->pages->page_size, who);
     if (s != PROTOKV_OK) return s;
     r.kp = (uint8_t*)a->pages->k;
     r.vp = (uint8_t*)a->pages->v;
@@ -336,7 +336,163 @@ protokv_status protokv_rotate(const protokv_rotate_args* a, void* stream) PKV_GU
     return fail(PROTOKV_E_UNSUPPORTED, who, "num_tokens times heads above 2^29");
   std::memcpy(r.axis, a->axes, D / 2);
   for (int i = 0; i < D / 2; ++i) r.inv[i] = std::pow(a->theta, -2.0 * i / D);
-  return device(launch_rotate(r, h.dtype == PROTOKV_KV_FP32, (hipStream_t)stream), who);
+  NormArgs n{};
+  if (norm) n = NormArgs{(const uint8_t*)norm->q_weight, (const uint8_t*)norm->k_weight, norm->eps};
+  return device(launch_rotate(r, norm ? &n : nullptr, h.dtype == PROTOKV_KV_FP32, (hipStream_t)stream), who);
+}
+
+protokv_status page_attend(const protokv_page_attend_args* p, const protokv_pages4* four, void* stream, const char* who) {
+  ExactArgs a{};
+  protokv_status s = page_attend_shape(p, a, who);
+  if (s != PROTOKV_OK) return s;
+  const Heads h{p->num_q_heads, p->num_kv_heads, p->head_dim, p->kv_dtype};
+  s = check_result(h, p->num_requests, p->total, p->cu, p->o, p->lse, p->prior_o, p->prior_lse, who);
+  if (s != PROTOKV_OK || p->num_requests == 0 || p->total == 0) return s;
+  s = four ? check_pages4(*four, h.kv, who) : check_page_rows(p->pages, who);
+  if (s == PROTOKV_OK) s = check_rows(p->q, p->q_stride, h.q, h, who, "q");
+  if (s != PROTOKV_OK) return s;
+  if (!p->kv_len || !p->table || off4(p->kv_len) || off4(p->table))
+    return fail(PROTOKV_E_INVALID, who, "kv_len and table must be non-NULL and aligned to 4 bytes");
+  const bool fp32 = h.dtype == PROTOKV_KV_FP32;
+  const size_t need = lay_out(a, nullptr);
+  if (need) {
+    if (!p->workspace) return fail(PROTOKV_E_WORKSPACE, who, "workspace is NULL");
+    if ((uintptr_t)p->workspace % 256) return fail(PROTOKV_E_WORKSPACE, who, "workspace must be 256-byte aligned");
+    if (p->workspace_bytes < need)
+      return fail(PROTOKV_E_WORKSPACE, who, ("workspace too small: need " + std::to_string(need) + " bytes").c_str());
+    lay_out(a, (uint8_t*)p->workspace);
+  }
+  a.q = p->q;
+  a.k = p->pages.k;
+  a.v = p->pages.v;
+  a.o = p->o;
+  a.lse = p->lse;
+  a.po = p->prior_o;
+  a.pl = p->prior_lse;
+  a.cu = p->cu;
+  a.kv_len = p->kv_len;
+  a.table = p->table;
+  a.qs = p->q_stride * h.es();
+  if (four) {
+    a.ksc = four->k_scale;
+    a.vsc = four->v_scale;
+  }
+  return device(launch_exact(a, fp32, four ? Keys::PAGES4 : Keys::PAGES, (hipStream_t)stream), who);
+}
+
+// The same call over exact pages: sizes and addresses of everything but the pages' own.
+protokv_page_attend_args as_page_attend(const protokv_page4_attend_args& p) {
+  protokv_page_attend_args a;
+  a.num_q_heads = p.num_q_heads;
+  a.num_kv_heads = p.num_kv_heads;
+  a.head_dim = p.head_dim;
+  a.kv_dtype = p.kv_dtype;
+  a.num_requests = p.num_requests;
+  a.total = p.total;
+  a.max_add = p.max_add;
+  a.table_stride = p.table_stride;
+  a.cu = p.cu;
+  a.kv_len = p.kv_len;
+  a.table = p.table;
+  a.q = p.q;
+  a.q_stride = p.q_stride;
+  a.pages = protokv_pages{p.pages.k, p.pages.v, p.pages.num_pages, p.pages.page_size};
+  a.o = p.o;
+  a.lse = p.lse;
+  a.prior_o = p.prior_o;
+  a.prior_lse = p.prior_lse;
+  a.workspace = p.workspace;
+  a.workspace_bytes = p.workspace_bytes;
+  return a;
+}
+
+protokv_status attend_workspace(const protokv_page_attend_args& p, size_t* bytes, const char* who) {
+  ExactArgs a{};
+  protokv_status s = page_attend_shape(&p, a, who);
+  if (s == PROTOKV_OK) *bytes = lay_out(a, nullptr);
+  return s;
+}
+
+protokv_status page4_rows(const protokv_page4_rows_args* a, bool store, void* stream, const char* who) {
+  if (!a) return fail(PROTOKV_E_INVALID, who, "args is NULL");
+  const Heads h{a->num_kv_heads, a->num_kv_heads, a->head_dim, a->kv_dtype};
+  protokv_status s = check_heads(h, who);
+  if (s != PROTOKV_OK) return s;
+  if (a->num_tokens < 0) return fail(PROTOKV_E_INVALID, who, "num_tokens must be >= 0");
+  s = check_page_sizes(a->pages.num_pages, a->pages.page_size, who);
+  if (s != PROTOKV_OK) return s;
+  const int64_t rows = 2 * (int64_t)a->num_tokens * h.kv;
+  if (rows >= (1ll << 29))  // eight threads to a row, fewer than 2^32 to a launch
+    return fail(PROTOKV_E_UNSUPPORTED, who, "2 * num_tokens * num_kv_heads must be below 2^29");
+  if (rows == 0) return PROTOKV_OK;  // (empty arrays may have no address)
+  s = check_pages4(a->pages, h.kv, who);
+  if (s == PROTOKV_OK) s = check_rows(a->k, a->k_stride, h.kv, h, who, "k");
+  if (s == PROTOKV_OK) s = check_rows(a->v, a->v_stride, h.kv, h, who, "v");
+  if (s != PROTOKV_OK) return s;
+  if (!a->slots || off4(a->slots)) return fail(PROTOKV_E_INVALID, who, "slots must be non-NULL and aligned to 4 bytes");
+  if (!store && a->k == a->v) return fail(PROTOKV_E_INVALID, who, "k and v are the same rows");
+  if (store && (a->pages.k == a->pages.v || a->pages.k_scale == a->pages.v_scale))
+    return fail(PROTOKV_E_INVALID, who, "pages: k and v are the same array");
+  Page4Rows r{};
+  r.k = (uint8_t*)a->k;
+  r.v = (uint8_t*)a->v;
+  r.slots = a->slots;
+  r.pk = a->pages.k;
+  r.pv = a->pages.v;
+  r.ksc = a->pages.k_scale;
+  r.vsc = a->pages.v_scale;
+  r.ks = a->k_stride * h.es();
+  r.vs = a->v_stride * h.es();
+  r.rows = rows;
+  r.Hkv = h.kv;
+  r.shift = log2i(a->pages.page_size);
+  r.nslots = a->pages.num_pages * a->pages.page_size;
+  return device(launch_page4_rows(r, h.dtype == PROTOKV_KV_FP32, store, (hipStream_t)stream), who);
+}
+
+}  // namespace
+
+// What a check or a message allocates may fail; nothing may leave a C entry.
+#define PKV_GUARD(who, ...)                                      \
+  try __VA_ARGS__ catch (...) {                                  \
+    try { call_error() = who ": out of memory"; } catch (...) {} \
+    return PROTOKV_E_DEVICE;                                     \
+  }
+
+extern "C" {
+
+protokv_status protokv_page_plan(const protokv_page_plan_args* a, void* stream) PKV_GUARD("page_plan", {
+  const char* who = "page_plan";
+  if (!a) return fail(PROTOKV_E_INVALID, who, "args is NULL");
+  const protokv_status s = check_table(a->num_requests, a->num_pages, a->page_size, a->table_stride, who);
+  if (s != PROTOKV_OK) return s;
+  if (a->max_tokens < 1 || a->max_tokens > (1 << 29)) return fail(PROTOKV_E_INVALID, who, "max_tokens must be in [1, 2^29]");
+  const void* need[] = {a->ctx, a->add, a->table, a->free_pages, a->free_count, a->free_count_out, a->cu, a->kv_len, a->slots};
+  for (const void* p : need)
+    if (!p || off4(p)) return fail(PROTOKV_E_INVALID, who, "arrays must be non-NULL and aligned to 4 bytes");
+  if (off4(a->base) || off4(a->positions) || off4(a->refused))
+    return fail(PROTOKV_E_INVALID, who, "arrays must be aligned to 4 bytes");
+  // every workgroup reads the inputs while the first writes the outputs
+  const void* in[] = {a->ctx, a->add, a->base, a->free_count};
+  const void* out[] = {a->free_count_out, a->cu, a->kv_len, a->slots, a->positions, a->refused};
+  for (const void* p : in)
+    for (const void* q : out)
+      if (p && p == q) return fail(PROTOKV_E_INVALID, who, "an output must not be one of ctx, add, base and free_count");
+  return device(launch_page_plan(*a, (hipStream_t)stream), who);
+})
+
+protokv_status protokv_rotate(const protokv_rotate_args* a, void* stream) PKV_GUARD("rotate", {
+  return rotate(a, nullptr, stream, "rotate");
+})
+
+protokv_status protokv_norm_rotate(const protokv_rotate_args* a, const protokv_head_norm* norm,
+                                   void* stream) PKV_GUARD("norm_rotate", {
+  const char* who = "norm_rotate";
+  if (!norm) return fail(PROTOKV_E_INVALID, who, "norm is NULL");
+  if (!(norm->eps >= 0.0) || !std::isfinite(norm->eps)) return fail(PROTOKV_E_INVALID, who, "eps must be finite and >= 0");
+  if (off16(norm->q_weight) || off16(norm->k_weight))
+    return fail(PROTOKV_E_INVALID, who, "q_weight and k_weight must be aligned to 16 bytes");
+  return rotate(a, norm, stream, who);
 })
 
 protokv_status protokv_prompt_attend(const protokv_prompt_args* p, void* stream) PKV_GUARD("prompt_attend", {
@@ -373,53 +529,116 @@ protokv_status protokv_prompt_attend(const protokv_prompt_args* p, void* stream)
   else plan_blocks(a, false);
   s = check_grid(a, who);
   if (s != PROTOKV_OK) return s;
-  return device(launch_exact(a, fp32, false, (hipStream_t)stream), who);
+  return device(launch_exact(a, fp32, Keys::ROWS, (hipStream_t)stream), who);
 })
 
 protokv_status protokv_page_attend_workspace(const protokv_page_attend_args* p, size_t* bytes) PKV_GUARD("page_attend_workspace", {
   const char* who = "page_attend_workspace";
   if (!p || !bytes) return fail(PROTOKV_E_INVALID, who, "args and bytes must be non-NULL");
-  ExactArgs a{};
-  protokv_status s = page_attend_shape(p, a, who);
-  if (s == PROTOKV_OK) *bytes = lay_out(a, nullptr);
-  return s;
+  return attend_workspace(*p, bytes, who);
 })
 
 protokv_status protokv_page_attend(const protokv_page_attend_args* p, void* stream) PKV_GUARD("page_attend", {
   const char* who = "page_attend";
   if (!p) return fail(PROTOKV_E_INVALID, who, "args is NULL");
-  ExactArgs a{};
-  protokv_status s = page_attend_shape(p, a, who);
+  return page_attend(p, nullptr, stream, who);
+})
+
+protokv_status protokv_page4_attend_workspace(const protokv_page4_attend_args* p, size_t* bytes) PKV_GUARD("page4_attend_workspace", {
+  const char* who = "page4_attend_workspace";
+  if (!p || !bytes) return fail(PROTOKV_E_INVALID, who, "args and bytes must be non-NULL");
+  return attend_workspace(as_page_attend(*p), bytes, who);
+})
+
+protokv_status protokv_page4_attend(const protokv_page4_attend_args* p, void* stream) PKV_GUARD("page4_attend", {
+  const char* who = "page4_attend";
+  if (!p) return fail(PROTOKV_E_INVALID, who, "args is NULL");
+  const protokv_page_attend_args a = as_page_attend(*p);
+  return page_attend(&a, &p->pages, stream, who);
+})
+
+protokv_status protokv_page4_store(const protokv_page4_rows_args* a, void* stream) PKV_GUARD("page4_store", {
+  return page4_rows(a, true, stream, "page4_store");
+})
+
+protokv_status protokv_page4_read(const protokv_page4_rows_args* a, void* stream) PKV_GUARD("page4_read", {
+  return page4_rows(a, false, stream, "page4_read");
+})
+
+protokv_status protokv_page_fork(const protokv_page_fork_args* a, void* stream) PKV_GUARD("page_fork", {
+  const char* who = "page_fork";
+  if (!a) return fail(PROTOKV_E_INVALID, who, "args is NULL");
+  if (a->num_forks < 1) return fail(PROTOKV_E_INVALID, who, "num_forks must be >= 1");
+  if (a->num_forks > MAX_REQUESTS) return fail(PROTOKV_E_UNSUPPORTED, who, "num_forks above 8192");
+  protokv_status s = check_table(a->num_requests, a->num_pages, a->page_size, a->table_stride, who);
+  if (s == PROTOKV_OK)
+    s = check_arrays({a->ctx, a->src, a->dst, a->table, a->shares, a->free_pages, a->free_count, a->free_count_out, a->ctx_out,
+                      a->lens, a->copy_src, a->copy_dst, a->copy_rows},
+                     {a->at, a->refused}, {a->ctx, a->src, a->dst, a->at, a->free_pages, a->free_count},
+                     {a->table, a->shares, a->free_count_out, a->ctx_out, a->lens, a->copy_src, a->copy_dst, a->copy_rows, a->refused},
+                     who);
   if (s != PROTOKV_OK) return s;
-  const Heads h{p->num_q_heads, p->num_kv_heads, p->head_dim, p->kv_dtype};
-  s = check_result(h, p->num_requests, p->total, p->cu, p->o, p->lse, p->prior_o, p->prior_lse, who);
-  if (s != PROTOKV_OK || p->num_requests == 0 || p->total == 0) return s;
-  s = check_page_rows(p->pages, who);
-  if (s == PROTOKV_OK) s = check_rows(p->q, p->q_stride, h.q, h, who, "q");
+  return device(launch_page_fork(*a, (hipStream_t)stream), who);
+})
+
+protokv_status protokv_page_copy(const protokv_page_copy_args* a, void* stream) PKV_GUARD("page_copy", {
+  const char* who = "page_copy";
+  if (!a) return fail(PROTOKV_E_INVALID, who, "args is NULL");
+  if (a->num_copies < 0) return fail(PROTOKV_E_INVALID, who, "num_copies must be >= 0");
+  if (a->num_kv_heads < 1 || a->num_kv_heads > 65536) return fail(PROTOKV_E_INVALID, who, "num_kv_heads must be in [1, 65536]");
+  protokv_status s = check_page_sizes(a->num_pages, a->page_size, who);
   if (s != PROTOKV_OK) return s;
-  if (!p->kv_len || !p->table || off4(p->kv_len) || off4(p->table))
-    return fail(PROTOKV_E_INVALID, who, "kv_len and table must be non-NULL and aligned to 4 bytes");
-  const bool fp32 = h.dtype == PROTOKV_KV_FP32;
-  const size_t need = lay_out(a, nullptr);
-  if (need) {
-    if (!p->workspace) return fail(PROTOKV_E_WORKSPACE, who, "workspace is NULL");
-    if ((uintptr_t)p->workspace % 256) return fail(PROTOKV_E_WORKSPACE, who, "workspace must be 256-byte aligned");
-    if (p->workspace_bytes < need)
-      return fail(PROTOKV_E_WORKSPACE, who, ("workspace too small: need " + std::to_string(need) + " bytes").c_str());
-    lay_out(a, (uint8_t*)p->workspace);
+  if (a->num_arrays < 1 || a->num_arrays > MAX_ARRAYS || !a->arrays)
+    return fail(PROTOKV_E_INVALID, who, "num_arrays must be in [1, 128] and arrays non-NULL");
+  PageCopy c;
+  std::memset(&c, 0, sizeof(c));
+  int64_t layers = 0, most = 0;
+  for (int i = 0; i < a->num_arrays; ++i) {
+    const protokv_page_array& x = a->arrays[i];
+    if (a->num_copies && (!x.base || off16(x.base))) return fail(PROTOKV_E_INVALID, who, "arrays: base must be non-NULL and aligned to 16 bytes");
+    if (x.row_bytes < 4 || x.row_bytes > 4096 || x.row_bytes % 4)
+      return fail(PROTOKV_E_INVALID, who, "arrays: row_bytes must be a multiple of 4 in [4, 4096]");
+    if (x.layers < 1) return fail(PROTOKV_E_INVALID, who, "arrays: layers must be >= 1");
+    const int64_t page = (int64_t)x.row_bytes * a->num_kv_heads * a->page_size;
+    if (page >= (1ll << 31)) return fail(PROTOKV_E_UNSUPPORTED, who, "a page of 2^31 bytes or more");
+    if (x.layers > 1 && (x.layer_stride < page * a->num_pages || x.layer_stride % 16))
+      return fail(PROTOKV_E_INVALID, who, "arrays: layer_stride must hold the pages and be a multiple of 16");
+    c.base[i] = (uint8_t*)x.base;
+    c.layer_stride[i] = x.layers > 1 ? x.layer_stride : 0;
+    c.row_bytes[i] = x.row_bytes;
+    c.first[i] = (int)layers;
+    layers += x.layers;
+    if (layers > 65535) return fail(PROTOKV_E_UNSUPPORTED, who, "more than 65535 layers in all");
+    most = std::max(most, x.row_bytes % 16 ? page / 4 : page / 16);
   }
-  a.q = p->q;
-  a.k = p->pages.k;
-  a.v = p->pages.v;
-  a.o = p->o;
-  a.lse = p->lse;
-  a.po = p->prior_o;
-  a.pl = p->prior_lse;
-  a.cu = p->cu;
-  a.kv_len = p->kv_len;
-  a.table = p->table;
-  a.qs = p->q_stride * h.es();
-  return device(launch_exact(a, fp32, true, (hipStream_t)stream), who);
+  if (a->num_copies == 0) return PROTOKV_OK;
+  if (!a->src || !a->dst || off4(a->src) || off4(a->dst) || off4(a->rows))
+    return fail(PROTOKV_E_INVALID, who, "src and dst must be non-NULL, and they and rows aligned to 4 bytes");
+  // four units to a thread, up to 64 workgroups to a page
+  const int64_t parts = std::min<int64_t>((most + 1023) / 1024, 64);
+  if (parts * layers * a->num_copies >= (1ll << 32) / 256)
+    return fail(PROTOKV_E_UNSUPPORTED, who, "too many copies and layers for one launch");
+  c.num_arrays = a->num_arrays;
+  c.num_pages = a->num_pages;
+  c.Hkv = a->num_kv_heads;
+  c.shift = log2i(a->page_size);
+  c.src = a->src;
+  c.dst = a->dst;
+  c.rows = a->rows;
+  return device(launch_page_copy(c, a->num_copies, (int)layers, (unsigned)parts, (hipStream_t)stream), who);
+})
+
+protokv_status protokv_page_release(const protokv_page_release_args* a, void* stream) PKV_GUARD("page_release", {
+  const char* who = "page_release";
+  if (!a) return fail(PROTOKV_E_INVALID, who, "args is NULL");
+  protokv_status s = check_table(a->num_requests, a->num_pages, a->page_size, a->table_stride, who);
+  if (s == PROTOKV_OK)
+    s = check_arrays({a->ctx, a->keep, a->table, a->shares, a->free_pages, a->free_count, a->free_count_out, a->ctx_out,
+                      a->refused, a->scratch},
+                     {}, {a->ctx, a->keep, a->table, a->free_count},
+                     {a->shares, a->free_pages, a->free_count_out, a->ctx_out, a->refused, a->scratch}, who);
+  if (s != PROTOKV_OK) return s;
+  return device(launch_page_release(*a, (hipStream_t)stream), who);
 })
 
 }  // extern "C"

@@ -1,5 +1,6 @@
 // Internal declarations of the handle-free calls: exact attention (exact.hip),
-// rotary positions and block tables (tokens.hip), their host side (exact.cpp).
+// rotary positions and block tables (tokens.hip), pages of 4 bits and shared pages
+// (pages.hip), their host side (exact.cpp).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -65,6 +66,7 @@ struct ExactArgs {
   int blocks;  // row-block indices per kv head (0: no row blocks)
   int splits;  // most context splits of a row block
   int waves;   // waves of a float32 row block
+  const uint8_t *ksc, *vsc;  // scales of pages of 4 bits, whose codes are k and v (else null)
 };
 
 struct RotateArgs {
@@ -80,8 +82,51 @@ struct RotateArgs {
   double inv[64];                  // theta^(-2i/D)
 };
 
-hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t st);
-hipError_t launch_rotate(const RotateArgs& a, bool fp32, hipStream_t st);
+// Norms of the heads that turn: weights in the rows' type, or null.
+struct NormArgs {
+  const uint8_t *qw, *kw;
+  double eps;
+};
+
+// Rows into or out of pages of 4 bits.
+struct Page4Rows {
+  uint8_t *k, *v;    // rows
+  const int32_t* slots;
+  uint8_t *pk, *pv, *ksc, *vsc;
+  long long ks, vs;  // bytes between rows
+  long long rows;    // tokens times 2 Hkv
+  int Hkv, shift;
+  int nslots;        // slots of the pages
+};
+
+constexpr int MAX_ARRAYS = 128;
+struct PageCopy {
+  uint8_t* base[MAX_ARRAYS];
+  long long layer_stride[MAX_ARRAYS];
+  int row_bytes[MAX_ARRAYS];
+  int first[MAX_ARRAYS + 1];  // layers of the arrays before
+  int num_arrays, num_pages, Hkv, shift;
+  const int32_t *src, *dst, *rows;
+};
+
+constexpr int RL_PAGES = 4096;  // pages that a workgroup looks through for freed ones
+
+// Eight values of 4 bits as bfloat16, exactly: the codes of w, the scale's exponent.
+__device__ __forceinline__ uint4 values4(uint32_t w, float scale) {
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
+}
+
+// How the keys and values of an attention lie.
+enum class Keys { ROWS, PAGES, PAGES4 };
+hipError_t launch_exact(const ExactArgs& a, bool fp32, Keys keys, hipStream_t st);
+hipError_t launch_rotate(const RotateArgs& a, const NormArgs* norm, bool fp32, hipStream_t st);
+hipError_t launch_page4_rows(const Page4Rows& a, bool fp32, bool store, hipStream_t st);
+hipError_t launch_page_fork(const protokv_page_fork_args& a, hipStream_t st);
+hipError_t launch_page_copy(const PageCopy& a, int copies, int layers, unsigned parts, hipStream_t st);
+hipError_t launch_page_release(const protokv_page_release_args& a, hipStream_t st);
 hipError_t launch_page_plan(const protokv_page_plan_args& a, hipStream_t st);
 
 }  // namespace pkv

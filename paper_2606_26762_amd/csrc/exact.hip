@@ -18,6 +18,7 @@ namespace pkv {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef short v8i16 __attribute__((ext_vector_type(8)));
@@ -251,6 +252,9 @@ constexpr int EX_NBUF = 4;              // tiles t - 1 and t in use, t + 1 and t
 // two waves take a row's keys, half of every tile each; 128 rows to a workgroup, for
 // launches that 256 would leave in few rounds (the rule and its figures stand
 // with the host's block counts).
+// PAGED = 2: pages of 4 bits.  A thread takes 16 bytes of codes, the 32 dims of one block,
+// of a row of K or V of each tile, turns them to bfloat16 (exactly) between its products and puts
+// them where the DMA would have: 16 conversions and four LDS writes to a tile, beside 32 products.
 template <int PAGED, int KH>
 __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   __shared__ __attribute__((aligned(256))) uint8_t s_kv[EX_NBUF][2][EX_TILE];
@@ -307,6 +311,19 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     const size_t page = bad ? 0 : id;
     return ((((page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1)))) * (size_t)(D * 2);
   };
+  auto note_bad = [&](int t) {
+    if (wave == 0) {
+      bool bad;
+      paged_row(min(t * EX_KEYS + lane, it.kend - 1), bad);
+      const unsigned long long bm = __ballot(bad);
+      if (lane == 0) s_bad[t & 7] = bm;
+    }
+  };
+  // 4 bits: this thread's block c4 of row r4 of a tile, of K (waves 0 - 3) or V; its codes
+  // and scale of the tile to be put into LDS next
+  const int r4 = (tid & 255) >> 2, c4 = tid & 3;
+  uint4 codes = make_uint4(0, 0, 0, 0);
+  uint32_t scale = 0;
   // this lane's part of the rows 4 wave + lane / 16 and + 32 of a tile
   const int ckey = ((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)) * 16;
   const int cval = ((lane & 15) ^ ((lane >> 4) << 2)) * 16;
@@ -329,22 +346,33 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
       next_k[q] = rk + ckey;
       next_v[q] = rv + cval;
     }
-    if constexpr (PAGED) {
-      if (wave == 0) {
-        bool bad;
-        paged_row(min(t * EX_KEYS + lane, it.kend - 1), bad);
-        const unsigned long long bm = __ballot(bad);
-        if (lane == 0) s_bad[t & 7] = bm;
-      }
-    }
+    if constexpr (PAGED) note_bad(t);
+  };
+  auto fetch = [&](int t) {  // 4 bits: the codes and the scale of tile t
+    bool bad;
+    const size_t row = paged_row(min(t * EX_KEYS + r4, it.kend - 1), bad) / (D * 2);
+    codes = reinterpret_cast<const uint4*>(wave < 4 ? kb : vb)[row * 4 + c4];
+    scale = (wave < 4 ? a.ksc : a.vsc)[row * 4 + c4];
+    note_bad(t);
   };
   auto load = [&](int t, int part) {  // one of the four instructions that load tile t
+    if constexpr (PAGED == 2) {  // one of the four pieces of 8 dims
+      const uint32_t w = part == 0 ? codes.x : part == 1 ? codes.y : part == 2 ? codes.z : codes.w;
+      const int place = (4 * c4 + part) ^ (wave < 4 ? r4 & 15 : 4 * (r4 & 3));
+      *reinterpret_cast<uint4*>(s_kv[t % EX_NBUF][wave < 4 ? 0 : 1] + r4 * 256 + place * 16) =
+          values4(w, __uint_as_float(scale << 23));
+      return;
+    }
     const int q = part >> 1;
     if (part & 1) lds_dma16(next_v[q], s_kv[t % EX_NBUF][1] + (wave + 8 * q) * 1024);
     else lds_dma16(next_k[q], s_kv[t % EX_NBUF][0] + (wave + 8 * q) * 1024);
   };
+  auto next_of = [&](int t) {  // what is to be done of tile t before its loads
+    if constexpr (PAGED == 2) fetch(t);
+    else locate(t);
+  };
   auto issue = [&](int t) {
-    locate(t);
+    next_of(t);
 #pragma unroll
     for (int part = 0; part < 4; ++part) load(t, part);
   };
@@ -437,7 +465,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
         }
       }
     }
-    if (tk + 3 < t1) locate(tk + 3);
+    if (tk + 3 < t1) next_of(tk + 3);
     if (F == 0) lrun += (part[0] + part[1]) + (part[2] + part[3]);  // this half's keys; the halves meet at the end
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(0);
@@ -556,7 +584,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   wait_vm<0>();
   asm volatile("" ::"v"(near_o));
   if (t0 + 1 < t1) issue(t0 + 1);
-  if (t0 + 2 < t1) locate(t0 + 2);
+  if (t0 + 2 < t1) next_of(t0 + 2);
   // Waves w and w + 4 share a SIMD.  In period t waves 0 - 3 form the products of tile
   // t, then its weights, and waves 4 - 7 the weights of tile t - 1, then the products
   // of tile t, so that one wave of a SIMD has the matrix core while the other has the
@@ -566,8 +594,10 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   // t + 2 on; the rows of tile t + 3 are located behind them.
   auto even = [&](int t) {  // the barrier before period t
     __builtin_amdgcn_sched_barrier(0);
-    if (t + 1 < t1) wait_vm<4>();  // this wave's loads of tile t have landed, those of t + 1 may be in flight
-    else wait_vm<0>();
+    if constexpr (PAGED != 2) {
+      if (t + 1 < t1) wait_vm<4>();  // this wave's loads of tile t have landed, those of t + 1 may be in flight
+      else wait_vm<0>();
+    }
     ex_barrier();
     if constexpr (PAGED) {
       // in the place of the ids of tiles up to t + 3 - tpc
@@ -616,7 +646,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
     if (t + 2 < t1)
 #pragma unroll
       for (int part = 0; part < 4; ++part) load(t + 2, part);
-    if (t + 3 < t1) locate(t + 3);
+    if (t + 3 < t1) next_of(t + 3);
     second_barrier(t);
   }
   lrun += xor32(lrun);
@@ -722,6 +752,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
 //      m of accumulator b is dim 4 m + b.
 // A dot product is the sum of eight 16-dim chains: its rounding error is that of
 // a pairwise sum.
+// Pages of 4 bits (PAGED = 2): lane (m, h) takes dims 64 h .. 64 h + 63 of key m, 32 bytes,
+// and the query lies accordingly; of V two bytes of each key, its scale from the key's lane.
 constexpr int EX_KEYS32 = 32;
 
 template <int PAGED, int W>
@@ -751,13 +783,17 @@ __global__ __launch_bounds__(W * 64, 2) void k_exact_f32(ExactArgs a) {
   {
     const f32x4* qr = reinterpret_cast<const f32x4*>((const uint8_t*)a.q + (size_t)(it.s0 + tok) * a.qs) + head * (D / 4);
 #pragma unroll
-    for (int j = 0; j < 16 / W; ++j) s_q[16 / W * wave + j][lane] = qr[2 * (16 / W * wave + j) + half];
+    for (int j = 0; j < 16 / W; ++j) {
+      const int k = 16 / W * wave + j;
+      s_q[k][lane] = qr[PAGED == 2 ? 16 * half + k : 2 * k + half];
+    }
   }
   __syncthreads();
   const uint8_t* kb = (const uint8_t*)a.k + (PAGED ? 0 : (size_t)it.s0 * a.ks + kvh * (D * 4));
   const uint8_t* vb = (const uint8_t*)a.v + (PAGED ? 0 : (size_t)it.s0 * a.vs + kvh * (D * 4));
   auto key_of = [&](int t) { return min(t * EX_KEYS32 + m, it.kend - 1); };  // keys past the last repeat it
   auto id_of = [&](int t) { return PAGED ? a.table[(size_t)it.seq * a.stride + (key_of(t) >> a.shift)] : 0; };
+  uint32_t ksc = 0, vsc = 0;  // 4 bits: the scales of this lane's key
   // K and V rows of this lane's key of tile t, which is on page id
   auto resolve = [&](int t, int id, const float*& kp, const float*& vp, bool& bad) {
     const int key = key_of(t);
@@ -765,7 +801,15 @@ __global__ __launch_bounds__(W * 64, 2) void k_exact_f32(ExactArgs a) {
     if constexpr (PAGED) {
       bad = (unsigned)id >= (unsigned)a.num_pages;
       const size_t page = bad ? 0 : id;
-      const size_t e = ((((page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1)))) * (size_t)D;
+      const size_t row = (((page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1)));
+      if constexpr (PAGED == 2) {
+        kp = reinterpret_cast<const float*>(kb + row * (D / 2));
+        vp = reinterpret_cast<const float*>(vb + row * (D / 2));
+        ksc = reinterpret_cast<const uint32_t*>(a.ksc)[row];
+        vsc = reinterpret_cast<const uint32_t*>(a.vsc)[row];
+        return;
+      }
+      const size_t e = row * (size_t)D;
       kp = (const float*)kb + e;
       vp = (const float*)vb + e;
     } else {
@@ -775,6 +819,21 @@ __global__ __launch_bounds__(W * 64, 2) void k_exact_f32(ExactArgs a) {
   };
   // half h of a tile: dims 64 h .. 64 h + 63 of K; registers 8 h .. 8 h + 7 of V
   auto load_k = [&](const float* kp, int h, f32x4 (&kr)[8]) {
+    if constexpr (PAGED == 2) {
+      const uint4 w = reinterpret_cast<const uint4*>(kp)[2 * half + h];
+      const float sc = __uint_as_float(((ksc >> (16 * half + 8 * h)) & 255) << 23);
+      auto turn = [&](int j, uint32_t c) {
+        const f32x2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 1);
+        const f32x2 x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 3);
+        kr[2 * j] = (f32x4){x0[0], x0[1], x1[0], x1[1]};
+        kr[2 * j + 1] = (f32x4){x2[0], x2[1], x3[0], x3[1]};
+      };
+      turn(0, w.x);
+      turn(1, w.y);
+      turn(2, w.z);
+      turn(3, w.w);
+      return;
+    }
     gbl_f32x4* p = (gbl_f32x4*)(uintptr_t)kp + half + 16 * h;
 #pragma unroll
     for (int j = 0; j < 8; ++j) kr[j] = p[2 * j];
@@ -787,6 +846,13 @@ __global__ __launch_bounds__(W * 64, 2) void k_exact_f32(ExactArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t lo = of_key((int)(uint32_t)p, 8 * h + i), hi = of_key((int)(uint32_t)(p >> 32), 8 * h + i);
+      if constexpr (PAGED == 2) {
+        const uint32_t c = ((const uint16_t*)(uintptr_t)((uint64_t)hi << 32 | lo))[m];
+        const float sc = __uint_as_float((((uint32_t)of_key((int)vsc, 8 * h + i) >> (8 * (m >> 3))) & 255) << 23);
+        const f32x2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 1);
+        vr[i] = (f32x4){x0[0], x0[1], x1[0], x1[1]};
+        continue;
+      }
       vr[i] = ((gbl_f32x4*)(uintptr_t)((uint64_t)hi << 32 | lo))[m];
     }
   };
@@ -1076,6 +1142,10 @@ __device__ __forceinline__ long long wave_sum(long long x) {
   }
   return x;
 }
+// FP4: pages of 4 bits.  Lane (m, h) loads the blocks h and 2 + h of 32 dims of key m's row of K
+// and of V and turns them to bfloat16, K into the operand (the query's dims lie
+// accordingly), V into the wave's LDS, then the next tile's loads go out.
+template <int FP4>
 __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2][4 * FW_VB];  // the V tile in use and the next
   const int lane = threadIdx.x & 63;
@@ -1134,7 +1204,8 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
     {
       const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(s0 + tok) * a.qs + head * (D * 2));
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[2 * kk + half]);
+      for (int kk = 0; kk < 8; ++kk)
+        bq[kk] = __builtin_bit_cast(bf16x8, qr[FP4 ? 8 * (kk >> 2) + 4 * half + (kk & 3) : 2 * kk + half]);
     }
     f32x16 oacc[4] = {zero, zero, zero, zero};
     float mref = EX_NONE, lrun = 0.f;
@@ -1162,34 +1233,67 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
         for (int b = 0; b < 4; ++b) lds_dma16(p + b * 64, s_mem[wave][buf] + b * FW_VB + g * 1024);
       }
     };
+    uint4 kc[2], vc[2];  // 4 bits: codes and scales of this lane's blocks
+    uint32_t ks = 0, vs = 0;
+    auto load_codes = [&](int rw) {
+      const size_t r = (unsigned)rw;
+      const uint4 *k4 = reinterpret_cast<const uint4*>(kb) + r * 4 + half, *v4 = reinterpret_cast<const uint4*>(vb) + r * 4 + half;
+      ks = reinterpret_cast<const uint32_t*>(a.ksc)[r];
+      kc[0] = k4[0];
+      kc[1] = k4[2];
+      vs = reinterpret_cast<const uint32_t*>(a.vsc)[r];
+      vc[0] = v4[0];
+      vc[1] = v4[2];
+    };
+    auto scale_of = [&](uint32_t s, int i) { return __uint_as_float(((s >> (16 * i + 8 * half)) & 255) << 23); };
+    auto part_of = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
     if (ta < tend) {
       u16x8 kr[8];
       bool bad;
       int rw = row_of(ta, id_of(ta), bad);
       int id = id_of(min(ta + 1, tend - 1));
-      load_v(rw, ta & 1);
-      __builtin_amdgcn_sched_barrier(0);
-      load_k(rw, kr);
+      if constexpr (FP4) {
+        load_codes(rw);
+      } else {
+        load_v(rw, ta & 1);
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(rw, kr);
+      }
       for (int t = ta; t < tend; ++t) {
         const int tn = min(t + 1, tend - 1);  // past the last tile the loads repeat it
         const unsigned badm = (unsigned)__ballot(bad);
         rw = row_of(tn, id, bad);
         const bool masked = (t + 1) * 32 > wfull || badm != 0;  // uniform
         f32x16 s = zero;
+        if constexpr (FP4) {
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk)
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[kk]), bq[kk], s, 0, 0, 0);
-        // Loads return in the order of their issue: V's are issued before K's of the
-        // same tile, so with K in the registers of the products V is in LDS.
-        asm volatile("" : "+v"(s) : : "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        if (t + 1 < tend) {  // uniform
-          id = id_of(min(tn + 1, tend - 1));
-          load_v(rw, (t + 1) & 1);  // read last by the products of tile t - 1
+          for (int kk = 0; kk < 8; ++kk)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(bf16x8, values4(part_of(kc[kk >> 2], kk & 3), scale_of(ks, kk >> 2))), bq[kk], s, 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint4*>(s_mem[wave][t & 1] + (2 * (j >> 2) + half) * FW_VB + m * 64 + (j & 3) * 16) =
+                values4(part_of(vc[j >> 2], j & 3), scale_of(vs, j >> 2));
+          if (t + 1 < tend) {  // uniform
+            id = id_of(min(tn + 1, tend - 1));
+            load_codes(rw);
+          }
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[kk]), bq[kk], s, 0, 0, 0);
+          // Loads return in the order of their issue: V's are issued before K's of the
+          // same tile, so with K in the registers of the products V is in LDS.
+          asm volatile("" : "+v"(s) : : "memory");
           __builtin_amdgcn_sched_barrier(0);
-          load_k(rw, kr);
+          if (t + 1 < tend) {  // uniform
+            id = id_of(min(tn + 1, tend - 1));
+            load_v(rw, (t + 1) & 1);  // read last by the products of tile t - 1
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(rw, kr);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
         const uint8_t* vl = vl0 + (t & 1) * (4 * FW_VB);
         if (masked) {
           const int rel = klim - t * 32 - 4 * half;
@@ -1380,10 +1484,11 @@ __global__ __launch_bounds__(FJ_W * 64) void k_exact_few_join(ExactArgs a, int w
 
 }  // namespace
 
-hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t st) {
+hipError_t launch_exact(const ExactArgs& a, bool fp32, Keys keys, hipStream_t st) {
   if (a.few) {
     const int wgs = (a.few + FW_W - 1) / FW_W;
-    hipLaunchKernelGGL(k_exact_few, dim3(wgs), dim3(FW_W * 64), 0, st, a);
+    if (keys == Keys::PAGES4) hipLaunchKernelGGL((k_exact_few<1>), dim3(wgs), dim3(FW_W * 64), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_few<0>), dim3(wgs), dim3(FW_W * 64), 0, st, a);
     // a workgroup per row and 8 waves, up to 2048 of them, at least four to 8 waves
     const int parts = (wgs * FW_W + FJ_W - 1) / FJ_W;
     hipLaunchKernelGGL(k_exact_few_join, dim3(parts, std::min(a.few_rows, std::max(FJ_Y, 2048 / parts))), dim3(FJ_W * 64), 0,
@@ -1391,22 +1496,27 @@ hipError_t launch_exact(const ExactArgs& a, bool fp32, bool paged, hipStream_t s
   }
   const unsigned items = (unsigned)a.Hkv * a.blocks * a.splits;
   if (items == 0) return hipGetLastError();
+  const dim3 wgs(items);
   if (fp32) {
-    if (paged) hipLaunchKernelGGL((k_exact_f32<1, 4>), dim3(items), dim3(4 * 64), 0, st, a);
-    else if (a.waves == 4) hipLaunchKernelGGL((k_exact_f32<0, 4>), dim3(items), dim3(4 * 64), 0, st, a);
-    else hipLaunchKernelGGL((k_exact_f32<0, 2>), dim3(items), dim3(2 * 64), 0, st, a);
+    if (keys == Keys::PAGES4) hipLaunchKernelGGL((k_exact_f32<2, 4>), wgs, dim3(4 * 64), 0, st, a);
+    else if (keys == Keys::PAGES) hipLaunchKernelGGL((k_exact_f32<1, 4>), wgs, dim3(4 * 64), 0, st, a);
+    else if (a.waves == 4) hipLaunchKernelGGL((k_exact_f32<0, 4>), wgs, dim3(4 * 64), 0, st, a);
+    else hipLaunchKernelGGL((k_exact_f32<0, 2>), wgs, dim3(2 * 64), 0, st, a);
   } else {
     const bool half = a.rows == EX_ROWS / 2;
-    if (paged && half) hipLaunchKernelGGL((k_exact_bf16<1, 2>), dim3(items), dim3(512), 0, st, a);
-    else if (paged) hipLaunchKernelGGL((k_exact_bf16<1, 1>), dim3(items), dim3(512), 0, st, a);
-    else if (half) hipLaunchKernelGGL((k_exact_bf16<0, 2>), dim3(items), dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((k_exact_bf16<0, 1>), dim3(items), dim3(512), 0, st, a);
+    const dim3 threads(512);
+    if (keys == Keys::PAGES4 && half) hipLaunchKernelGGL((k_exact_bf16<2, 2>), wgs, threads, 0, st, a);
+    else if (keys == Keys::PAGES4) hipLaunchKernelGGL((k_exact_bf16<2, 1>), wgs, threads, 0, st, a);
+    else if (keys == Keys::PAGES && half) hipLaunchKernelGGL((k_exact_bf16<1, 2>), wgs, threads, 0, st, a);
+    else if (keys == Keys::PAGES) hipLaunchKernelGGL((k_exact_bf16<1, 1>), wgs, threads, 0, st, a);
+    else if (half) hipLaunchKernelGGL((k_exact_bf16<0, 2>), wgs, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_exact_bf16<0, 1>), wgs, threads, 0, st, a);
   }
   if (a.splits > 1) {
-    const dim3 wgs(a.Hkv * a.blocks * (a.rows / EJ_ROWS)), threads(EJ_ROWS * 32);
-    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), wgs, threads, 0, st, a);
-    else if (a.rows == EX_ROWS) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), wgs, threads, 0, st, a);
-    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2>), wgs, threads, 0, st, a);
+    const dim3 joins(a.Hkv * a.blocks * (a.rows / EJ_ROWS)), threads(EJ_ROWS * 32);
+    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), joins, threads, 0, st, a);
+    else if (a.rows == EX_ROWS) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), joins, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2>), joins, threads, 0, st, a);
   }
   return hipGetLastError();
 }

@@ -1,0 +1,355 @@
+// Pages of 4 bits (protokv_page4_store, protokv_page4_read) and pages that several
+// requests hold (protokv_page_fork, protokv_page_copy, protokv_page_release) for gfx950.
+#include "exact.h"
+#include "pkv_internal.h"
+
+namespace pkv {
+
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// ---------------------------------------------------------------------------
+// Rows into and out of 4 bits.  A row (token, head, k or v) to eight lanes, 16
+// dims each; a block of 32 dims is two of them.  v_cvt_scalef32_pk_fp4_f32 divides by
+// the power of two, rounds to the nearest code, ties to the even one, and ends at 6,
+// which is the format's own rule (all bfloat16 values and the codes' borders checked
+// against it); the way back is exact.  Bound by the rows' bytes.
+// ---------------------------------------------------------------------------
+
+// Rows of a call: row r is k's or v's (r / Hkv odd) head r % Hkv of token r / (2 Hkv).
+struct Row4 {
+  long long at;  // bytes from the rows' start
+  int slot;      // -1: none
+  int head;
+  bool value;
+};
+__device__ __forceinline__ Row4 row4_of(const Page4Rows& a, long long r) {
+  const int t = (int)(r / (2 * a.Hkv)), j = (int)(r - (long long)t * (2 * a.Hkv));
+  Row4 x;
+  x.value = j >= a.Hkv;
+  x.head = x.value ? j - a.Hkv : j;
+  x.slot = a.slots[t];
+  if ((unsigned)x.slot >= (unsigned)a.nslots) x.slot = -1;
+  x.at = (long long)t * (x.value ? a.vs : a.ks);
+  return x;
+}
+// row of the pages that a slot's head is
+__device__ __forceinline__ long long place4(const Page4Rows& a, const Row4& x) {
+  return (((long long)(x.slot >> a.shift) * a.Hkv + x.head) << a.shift) + (x.slot & ((1 << a.shift) - 1));
+}
+
+template <int FP32>
+__global__ __launch_bounds__(256) void k_page4_store(Page4Rows a) {
+  const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) >> 3;
+  const int c = threadIdx.x & 7;
+  if (r >= a.rows) return;  // all eight lanes of a row together
+  const Row4 x = row4_of(a, r);
+  if (x.slot < 0) return;
+  const uint8_t* src = (x.value ? a.v : a.k) + x.at + (size_t)x.head * (D * (FP32 ? 4 : 2));
+  float v[16];
+  if constexpr (FP32) {
+    const float4* p = reinterpret_cast<const float4*>(src) + 4 * c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 w = p[i];
+      v[4 * i] = w.x;
+      v[4 * i + 1] = w.y;
+      v[4 * i + 2] = w.z;
+      v[4 * i + 3] = w.w;
+    }
+  } else {
+    const uint4* p = reinterpret_cast<const uint4*>(src) + 2 * c;
+    const uint4 w[2] = {p[0], p[1]};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint4 q = w[i >> 2];
+      const uint32_t u = (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w;
+      v[2 * i] = __uint_as_float(u << 16);
+      v[2 * i + 1] = __uint_as_float(u & 0xFFFF0000u);
+    }
+  }
+  // the largest |x| by its bits, where infinities and NaN lie above every number
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));  // the pair's other lane
+  // least e with top <= 7 * 2^e: two below top's exponent, one more past 1.75
+  const bool odd = top >= 0x7F800000u;
+  const int s = odd ? 255 : min(max((int)((top + 0x1FFFFFu) >> 23) - 2, 2), 252);
+  const float scale = __uint_as_float((uint32_t)s << 23);
+  uint32_t lo = 0, hi = 0;
+  lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, v[0], v[1], scale, 0);
+  lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, v[2], v[3], scale, 1);
+  lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, v[4], v[5], scale, 2);
+  lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, v[6], v[7], scale, 3);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(hi, v[8], v[9], scale, 0);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(hi, v[10], v[11], scale, 1);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(hi, v[12], v[13], scale, 2);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(hi, v[14], v[15], scale, 3);
+  const long long at = place4(a, x);
+  reinterpret_cast<uint2*>((x.value ? a.pv : a.pk) + at * (D / 2))[c] = odd ? make_uint2(0, 0) : make_uint2(lo, hi);
+  if (!(c & 1)) (x.value ? a.vsc : a.ksc)[at * (D / 32) + (c >> 1)] = (uint8_t)s;
+}
+
+template <int FP32>
+__global__ __launch_bounds__(256) void k_page4_read(Page4Rows a) {
+  const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) >> 3;
+  const int c = threadIdx.x & 7;
+  if (r >= a.rows) return;
+  const Row4 x = row4_of(a, r);
+  uint2 w = make_uint2(0, 0);
+  float scale = 1.f;
+  if (x.slot >= 0) {
+    const long long at = place4(a, x);
+    w = reinterpret_cast<const uint2*>((x.value ? a.pv : a.pk) + at * (D / 2))[c];
+    scale = __uint_as_float((uint32_t)(x.value ? a.vsc : a.ksc)[at * (D / 32) + (c >> 1)] << 23);
+  }
+  uint8_t* dst = (x.value ? a.v : a.k) + x.at + (size_t)x.head * (D * (FP32 ? 4 : 2));
+  if constexpr (FP32) {
+    float4* p = reinterpret_cast<float4*>(dst) + 4 * c;
+    auto put = [&](int i, f32x2 l, f32x2 h) { p[i] = make_float4(l[0], l[1], h[0], h[1]); };
+    put(0, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 1));
+    put(1, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 3));
+    put(2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.y, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.y, scale, 1));
+    put(3, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.y, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.y, scale, 3));
+  } else {
+    uint4* p = reinterpret_cast<uint4*>(dst) + 2 * c;
+    p[0] = values4(w.x, scale);
+    p[1] = values4(w.y, scale);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Forks.  One workgroup decides: who is refused, who gets which page; then a
+// wave to a fork copies its table row and counts the owners.  Latency chains both.
+// ---------------------------------------------------------------------------
+constexpr int FK_NT = 1024;
+
+// Inclusive running sum over the workgroup's threads; total: of all.  s: FK_NT / 64
+// words, free again after the next barrier.
+__device__ __forceinline__ int block_sum(int x, int* s, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  if (lane == 63) s[wave] = x;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < FK_NT / 64; ++w) {
+    const int y = s[w];
+    if (w < wave) before += y;
+    total += y;
+  }
+  return before + x;
+}
+
+__global__ __launch_bounds__(FK_NT) void k_page_fork(protokv_page_fork_args a, int shift) {
+  __shared__ uint32_t s_src[MAX_REQUESTS / 32];  // requests that are forked
+  __shared__ int s_dst[MAX_REQUESTS];            // first fork that becomes request r; once granted -1 - its tokens
+  __shared__ int s_sum[2][FK_NT / 64];
+  __shared__ int s_refused;
+  const int tid = threadIdx.x, n = a.num_forks, R = a.num_requests, P1 = (1 << shift) - 1;
+  const int span = a.table_stride << shift;
+  const int held = min(max(a.free_count[0], 0), a.num_pages);
+  for (int r = tid; r < R; r += FK_NT) s_dst[r] = 0x7FFFFFFF;
+  for (int w = tid; w < (R + 31) / 32; w += FK_NT) s_src[w] = 0;
+  if (tid == 0) s_refused = 0;
+  __syncthreads();
+  for (int i = tid; i < n; i += FK_NT) {
+    const int s = a.src[i], d = a.dst[i];
+    if ((unsigned)s < (unsigned)R && (unsigned)d < (unsigned)R && s != d) {
+      atomicOr(&s_src[s >> 5], 1u << (s & 31));
+      atomicMin(&s_dst[d], i);
+    }
+  }
+  __syncthreads();
+  int asked = 0, refused = 0;
+  for (int i0 = 0, turn = 0; i0 < n; i0 += FK_NT, turn ^= 1) {
+    const int i = i0 + tid;
+    int s = 0, d = 0, len = 0;
+    bool ok = false;
+    if (i < n) {
+      s = a.src[i];
+      d = a.dst[i];
+      ok = (unsigned)s < (unsigned)R && (unsigned)d < (unsigned)R && s != d && !((s_src[d >> 5] >> (d & 31)) & 1) &&
+           s_dst[d] == i && a.ctx[d] <= 0;
+      if (ok) {
+        len = min(max(a.ctx[s], 0), span);
+        if (a.at) len = min(max(a.at[i], 0), len);
+      }
+    }
+    const int part = len & P1, full = len >> shift;
+    int total;
+    const int upto = asked + block_sum(ok && part, s_sum[turn], total);
+    asked += total;
+    if (i < n) {
+      const bool take = ok && part;
+      if (take && upto > held) ok = false;
+      int from = -1, to = -1;
+      if (ok && part) {
+        from = a.table[(size_t)s * a.table_stride + full];
+        to = a.free_pages[held - upto];
+        a.table[(size_t)d * a.table_stride + full] = to;
+      }
+      a.lens[i] = ok ? len : -1;
+      a.copy_src[i] = from;
+      a.copy_dst[i] = to;
+      a.copy_rows[i] = ok ? part : 0;
+      if (ok) s_dst[d] = -1 - len;  // no other thread's fork is i
+      refused += !ok;
+    }
+  }
+  if (refused) atomicAdd(&s_refused, refused);
+  __syncthreads();
+  for (int r = tid; r < R; r += FK_NT) a.ctx_out[r] = s_dst[r] < 0 ? -1 - s_dst[r] : a.ctx[r];
+  if (tid == 0) {
+    a.free_count_out[0] = held - min(asked, held);
+    if (a.refused) a.refused[0] = s_refused;
+  }
+}
+
+__global__ __launch_bounds__(256) void k_page_fork_rows(protokv_page_fork_args a, int shift) {
+  const int i = blockIdx.y, full = a.lens[i] >> shift;  // refused: -1
+  const size_t from = (size_t)(full > 0 ? a.src[i] : 0) * a.table_stride, to = (size_t)(full > 0 ? a.dst[i] : 0) * a.table_stride;
+  for (int j = blockIdx.x * 256 + threadIdx.x; j < full; j += gridDim.x * 256) {
+    const int page = a.table[from + j];
+    a.table[to + j] = page;
+    if ((unsigned)page < (unsigned)a.num_pages) atomicAdd(&a.shares[page], 1);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rows of pages to other pages: bound by their bytes.  A head's rows of a page lie
+// together; a workgroup takes a part of one copy in one layer of one array.
+// ---------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ void copy_rows_of(const uint8_t* from, uint8_t* to, int heads, size_t head_bytes, unsigned per) {
+  const unsigned all = heads * per;  // units of T: below 2^31, as a page's bytes are
+  for (unsigned u = blockIdx.y * 256 + threadIdx.x; u < all; u += gridDim.y * 256) {
+    const unsigned h = u / per;
+    const size_t at = h * head_bytes + (size_t)(u - h * per) * sizeof(T);
+    *reinterpret_cast<T*>(to + at) = *reinterpret_cast<const T*>(from + at);
+  }
+}
+__global__ __launch_bounds__(256) void k_page_copy(PageCopy a) {
+  const int layer = blockIdx.z;
+  int e = 0;
+  while (e + 1 < a.num_arrays && layer >= a.first[e + 1]) ++e;  // uniform
+  const int i = blockIdx.x, src = a.src[i], dst = a.dst[i], P = 1 << a.shift;
+  if ((unsigned)src >= (unsigned)a.num_pages || (unsigned)dst >= (unsigned)a.num_pages || src == dst) return;
+  const int rows = a.rows ? min(max(a.rows[i], 0), P) : P;
+  const size_t rb = a.row_bytes[e], head = rb << a.shift, page = head * a.Hkv;
+  uint8_t* base = a.base[e] + (size_t)(layer - a.first[e]) * a.layer_stride[e];
+  const unsigned bytes = (unsigned)(rows * rb);
+  if (bytes == 0) return;
+  if (rb % 16 == 0) copy_rows_of<uint4>(base + src * page, base + dst * page, a.Hkv, head, bytes / 16);
+  else copy_rows_of<uint32_t>(base + src * page, base + dst * page, a.Hkv, head, bytes / 4);
+}
+
+// ---------------------------------------------------------------------------
+// Releases, in three steps: what each request keeps, from the owners as they are;
+// an owner less for every page dropped, whose count then is -1 exactly if none is
+// left; those pages onto the stack in their order.  scratch[b]: pages freed
+// of the 4096 from 4096 b on.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(1024) void k_release_keep(protokv_page_release_args a, int shift) {
+  __shared__ int s_refused;
+  const int span = a.table_stride << shift, P1 = (1 << shift) - 1;
+  if (threadIdx.x == 0) s_refused = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.num_requests; i += 1024) {
+    const int ctx = min(max(a.ctx[i], 0), span);
+    int keep = min(max(a.keep[i], 0), ctx);
+    if (keep < ctx && (keep & P1)) {
+      const int page = a.table[(size_t)i * a.table_stride + (keep >> shift)];
+      if ((unsigned)page < (unsigned)a.num_pages && a.shares[page] > 0) {
+        keep = ctx;
+        atomicAdd(&s_refused, 1);
+      }
+    }
+    a.ctx_out[i] = keep;
+  }
+  for (int b = threadIdx.x; b < (a.num_pages + RL_PAGES - 1) / RL_PAGES; b += 1024) a.scratch[b] = 0;
+  __syncthreads();
+  if (threadIdx.x == 0) a.refused[0] = s_refused;
+}
+
+__global__ __launch_bounds__(256) void k_release_drop(protokv_page_release_args a, int shift) {
+  const int i = blockIdx.y, P1 = (1 << shift) - 1, span = a.table_stride << shift;
+  const int ctx = min(max(a.ctx[i], 0), span);
+  const int first = (int)(((long long)a.ctx_out[i] + P1) >> shift), end = (int)(((long long)ctx + P1) >> shift);
+  for (int j = first + blockIdx.x * 256 + threadIdx.x; j < end; j += gridDim.x * 256) {
+    const int page = a.table[(size_t)i * a.table_stride + j];
+    // of a page's drops the one that finds no owner beyond itself is one alone
+    if ((unsigned)page < (unsigned)a.num_pages && atomicSub(&a.shares[page], 1) == 0)
+      atomicAdd(&a.scratch[page / RL_PAGES], 1);
+  }
+}
+
+__global__ __launch_bounds__(1024) void k_release_collect(protokv_page_release_args a) {
+  __shared__ int s_sum[2][16];
+  const int tid = threadIdx.x, b = blockIdx.x;
+  int before = 0, all;
+  for (int w = tid; w < b; w += 1024) before += a.scratch[w];
+  block_sum(before, s_sum[0], all);
+  const int held = min(max(a.free_count[0], 0), a.num_pages);
+  const int p0 = b * RL_PAGES + tid * 4;
+  int sh[4], mine = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    sh[k] = p0 + k < a.num_pages ? a.shares[p0 + k] : 0;
+    mine += sh[k] < 0;
+  }
+  int total;
+  int at = held + all + block_sum(mine, s_sum[1], total) - mine;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (sh[k] < 0) {
+      a.shares[p0 + k] = 0;
+      if (at < a.num_pages) a.free_pages[at] = p0 + k;
+      ++at;
+    }
+  }
+  if (b == (int)gridDim.x - 1 && tid == 0) a.free_count_out[0] = min(held + all + total, a.num_pages);
+}
+
+}  // namespace
+
+hipError_t launch_page4_rows(const Page4Rows& a, bool fp32, bool store, hipStream_t st) {
+  const dim3 wgs((unsigned)((a.rows * 8 + 255) / 256)), threads(256);
+  if (store && fp32) hipLaunchKernelGGL((k_page4_store<1>), wgs, threads, 0, st, a);
+  else if (store) hipLaunchKernelGGL((k_page4_store<0>), wgs, threads, 0, st, a);
+  else if (fp32) hipLaunchKernelGGL((k_page4_read<1>), wgs, threads, 0, st, a);
+  else hipLaunchKernelGGL((k_page4_read<0>), wgs, threads, 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_fork(const protokv_page_fork_args& a, hipStream_t st) {
+  const int shift = 31 - __builtin_clz((unsigned)a.page_size);
+  hipLaunchKernelGGL(k_page_fork, dim3(1), dim3(FK_NT), 0, st, a, shift);
+  const unsigned parts = std::min((a.table_stride + 255u) / 256u, 64u);
+  hipLaunchKernelGGL(k_page_fork_rows, dim3(parts, a.num_forks), dim3(256), 0, st, a, shift);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_copy(const PageCopy& a, int copies, int layers, unsigned parts, hipStream_t st) {
+  hipLaunchKernelGGL(k_page_copy, dim3(copies, parts, layers), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_release(const protokv_page_release_args& a, hipStream_t st) {
+  const int shift = 31 - __builtin_clz((unsigned)a.page_size);
+  hipLaunchKernelGGL(k_release_keep, dim3(1), dim3(1024), 0, st, a, shift);
+  const unsigned parts = std::min((a.table_stride + 255u) / 256u, 64u);
+  hipLaunchKernelGGL(k_release_drop, dim3(parts, a.num_requests), dim3(256), 0, st, a, shift);
+  hipLaunchKernelGGL(k_release_collect, dim3((a.num_pages + RL_PAGES - 1) / RL_PAGES), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace pkv

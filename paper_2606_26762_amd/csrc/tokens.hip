@@ -1,5 +1,7 @@
 // Rotary positions of several axes and block tables (protokv_rotate,
 // protokv_page_plan) for gfx950.
+#include <type_traits>
+
 #include "exact.h"
 #include "pkv_internal.h"
 #include "rope.h"
@@ -47,8 +49,25 @@ struct Vec8<1> {
   }
 };
 
-template <int FP32>
-__global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
+// x + the same of the other lanes of eight
+__device__ __forceinline__ double sum8(double x) {
+  auto add = [&](auto ctrl) {
+    const long long u = __builtin_bit_cast(long long, x);
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)u, decltype(ctrl)::value, 0xf, 0xf, false);
+    const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), decltype(ctrl)::value, 0xf, 0xf, false);
+    x += __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | lo));
+  };
+  add(std::integral_constant<int, 0xB1>{});   // quad_perm: lane ^ 1
+  add(std::integral_constant<int, 0x4E>{});   // quad_perm: lane ^ 2
+  add(std::integral_constant<int, 0x141>{});  // row_half_mirror: the other four
+  return x;
+}
+
+// NORM: the heads that turn are normalised first, x / sqrt(mean(x^2) + eps) * w.  A
+// head's eight lanes sum its squares in float64, in which no float32's square overflows or
+// vanishes; it costs nothing beside the rows' bytes.
+template <int FP32, int NORM>
+__device__ __forceinline__ void rotate_rows(const RotateArgs& a, const NormArgs& nm) {
   constexpr int ES = FP32 ? 4 : 2;
   typedef Vec8<FP32> V;
   __shared__ __attribute__((aligned(16))) float s_cs[4][D];  // (cos, sin) of every pair
@@ -81,7 +100,35 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
                          : vh < 0 ? a.k + t * a.ks + (size_t)kh * (D * ES)
                                   : a.v + t * a.vs + (size_t)vh * (D * ES);
     V lo = reinterpret_cast<const V*>(src)[c8], hi = reinterpret_cast<const V*>(src + D / 2 * ES)[c8];
-    if (vh < 0) {
+    if (NORM && vh < 0) {
+      double ss = 0.0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double x = lo.get(i), y = hi.get(i);
+        ss = fma(x, x, fma(y, y, ss));
+      }
+      const float inv = (float)(1.0 / sqrt(sum8(ss) * (1.0 / D) + nm.eps));
+      const uint8_t* w = h < a.Hq ? nm.qw : nm.kw;
+      float x[8], y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = lo.get(i) * inv;
+        y[i] = hi.get(i) * inv;
+      }
+      if (w) {
+        const V wl = reinterpret_cast<const V*>(w)[c8], wh = reinterpret_cast<const V*>(w + D / 2 * ES)[c8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] *= wl.get(i);
+          y[i] *= wh.get(i);
+        }
+      }
+      float tx[8], ty[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rope_pair(x[i], y[i], cs[2 * i], cs[2 * i + 1], tx[i], ty[i]);
+      lo.set(tx);
+      hi.set(ty);
+    } else if (vh < 0) {
       float x[8], y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) rope_pair(lo.get(i), hi.get(i), cs[2 * i], cs[2 * i + 1], x[i], y[i]);
@@ -101,6 +148,15 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
         put((vh < 0 ? a.kp : a.vp) + ((((page * a.Hkv + hk) << a.shift) + off)) * (size_t)(D * ES));
     }
   }
+}
+
+template <int FP32>
+__global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
+  rotate_rows<FP32, 0>(a, NormArgs{});
+}
+template <int FP32>
+__global__ __launch_bounds__(256) void k_norm_rotate(RotateArgs a, NormArgs nm) {
+  rotate_rows<FP32, 1>(a, nm);
 }
 
 // ---------------------------------------------------------------------------
@@ -295,9 +351,11 @@ __global__ __launch_bounds__(NT) void k_page_plan(protokv_page_plan_args a, int 
 
 }  // namespace
 
-hipError_t launch_rotate(const RotateArgs& a, bool fp32, hipStream_t st) {
+hipError_t launch_rotate(const RotateArgs& a, const NormArgs* norm, bool fp32, hipStream_t st) {
   const unsigned blocks = (unsigned)(((long long)a.N * a.parts + 3) / 4);
-  if (fp32) hipLaunchKernelGGL((k_rotate<1>), dim3(blocks), dim3(256), 0, st, a);
+  if (norm && fp32) hipLaunchKernelGGL((k_norm_rotate<1>), dim3(blocks), dim3(256), 0, st, a, *norm);
+  else if (norm) hipLaunchKernelGGL((k_norm_rotate<0>), dim3(blocks), dim3(256), 0, st, a, *norm);
+  else if (fp32) hipLaunchKernelGGL((k_rotate<1>), dim3(blocks), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_rotate<0>), dim3(blocks), dim3(256), 0, st, a);
   return hipGetLastError();
 }

@@ -31,6 +31,8 @@ EXPORTED = [
     "protokv_read_pseudo_counts",
     "protokv_page_plan", "protokv_rotate", "protokv_prompt_attend", "protokv_page_attend",
     "protokv_page_attend_workspace",
+    "protokv_norm_rotate", "protokv_page4_store", "protokv_page4_read", "protokv_page4_attend",
+    "protokv_page4_attend_workspace", "protokv_page_fork", "protokv_page_copy", "protokv_page_release",
     "protokv_last_error",
 ]
 
@@ -139,6 +141,52 @@ class PageAttendArgs(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class HeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_double)]
+
+
+class Pages4(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class Page4RowsArgs(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("kv_dtype", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("slots", ctypes.c_void_p), ("pages", Pages4)]
+
+
+class Page4AttendArgs(ctypes.Structure):
+    _fields_ = [(f, Pages4 if f == "pages" else t) for f, t in PageAttendArgs._fields_]
+
+
+class PageForkArgs(ctypes.Structure):
+    _fields_ = [("num_forks", ctypes.c_int32), ("num_requests", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("table_stride", ctypes.c_int32)] + [
+        (f, ctypes.c_void_p) for f in ("ctx", "src", "dst", "at", "table", "shares", "free_pages", "free_count",
+                                       "free_count_out", "ctx_out", "lens", "copy_src", "copy_dst", "copy_rows", "refused")]
+
+
+class PageArray(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("row_bytes", ctypes.c_int32), ("layers", ctypes.c_int32),
+                ("layer_stride", ctypes.c_int64)]
+
+
+class PageCopyArgs(ctypes.Structure):
+    _fields_ = [("num_copies", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_arrays", ctypes.c_int32), ("arrays", ctypes.POINTER(PageArray)),
+                ("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("rows", ctypes.c_void_p)]
+
+
+class PageReleaseArgs(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("table_stride", ctypes.c_int32)] + [
+        (f, ctypes.c_void_p) for f in ("ctx", "keep", "table", "shares", "free_pages", "free_count", "free_count_out",
+                                       "ctx_out", "refused", "scratch")]
+
+
+RELEASE_PAGES = 4096   # pages to an entry of page_release's scratch
+
 _lib = None
 
 
@@ -177,6 +225,14 @@ def lib() -> ctypes.CDLL:
         L.protokv_prompt_attend.argtypes = [P(PromptArgs), vp]
         L.protokv_page_attend.argtypes = [P(PageAttendArgs), vp]
         L.protokv_page_attend_workspace.argtypes = [P(PageAttendArgs), P(sz)]
+        L.protokv_norm_rotate.argtypes = [P(RotateArgs), P(HeadNorm), vp]
+        L.protokv_page4_store.argtypes = [P(Page4RowsArgs), vp]
+        L.protokv_page4_read.argtypes = [P(Page4RowsArgs), vp]
+        L.protokv_page4_attend.argtypes = [P(Page4AttendArgs), vp]
+        L.protokv_page4_attend_workspace.argtypes = [P(Page4AttendArgs), P(sz)]
+        L.protokv_page_fork.argtypes = [P(PageForkArgs), vp]
+        L.protokv_page_copy.argtypes = [P(PageCopyArgs), vp]
+        L.protokv_page_release.argtypes = [P(PageReleaseArgs), vp]
         L.protokv_last_error.argtypes = [vp]
         L.protokv_last_error.restype = ctypes.c_char_p
         for name in EXPORTED:
@@ -587,31 +643,26 @@ def pair_axes(sections: Sequence[int], interleaved: bool = False) -> bytes:
     return out
 
 
-def rotate(q, k, positions, axes: bytes, theta: float, *, q_out=None, k_out=None, v=None, pages=None, slots=None,
-           stream=None):
-    """protokv_rotate on token rows q [N][Hq][D] and k [N][Hkv][D] (either may be
-    None; rows may be strided): positions int32 [num_axes][N] (or [N]: every axis
-    the same), axes from ``pair_axes``.  With pages=(k, v) tensors [num_pages][Hkv]
-    [page_size][D] and slots int32 [N] the turned keys and v's rows are stored, and
-    k_out is written only if given.  -> (q_out, k_out)"""
+def _rotate_args(who, q, k, positions, axes, theta, q_out, k_out, v, pages, slots, stream):
+    """-> the arguments of a rotation, its device, q_out, k_out"""
     import torch
     some = q if q is not None else k
     if some is None:
-        raise ValueError("rotate: neither q nor k")
+        raise ValueError(f"{who}: neither q nor k")
     dev, dtype, n = _device(some, stream), some.dtype, some.shape[0]
     a = RotateArgs()
     a.num_tokens, a.head_dim, a.kv_dtype = n, 128, _kv(dtype)
     hk = a.num_kv_heads = k.shape[1] if k is not None else 1
     a.num_q_heads = q.shape[1] if q is not None else hk
     if not isinstance(axes, bytes) or len(axes) != 64:
-        raise ValueError("rotate: axes are 64 bytes (pair_axes)")
+        raise ValueError(f"{who}: axes are 64 bytes (pair_axes)")
     num_axes = a.num_axes = max(axes) + 1
     a.axes, a.theta = axes, theta
     if positions.dim() == 1:
         a.positions = _flat(positions, "positions", torch.int32, dev, n)
     else:
         if positions.shape[0] < num_axes:
-            raise ValueError("rotate: positions has fewer axes than axes names")
+            raise ValueError(f"{who}: positions has fewer axes than axes names")
         a.positions, a.position_stride = _flat(positions, "positions", torch.int32, dev, positions.shape[0], n), n
     if q is not None:
         a.q, a.q_stride = _rows(q, "q", dtype, dev)
@@ -620,32 +671,55 @@ def rotate(q, k, positions, axes: bytes, theta: float, *, q_out=None, k_out=None
             a.q_out, a.q_out_stride = q_out.data_ptr(), a.num_q_heads * 128
         else:
             if q_out.shape != q.shape:
-                raise ValueError("rotate: q_out must have q's shape")
+                raise ValueError(f"{who}: q_out must have q's shape")
             a.q_out, a.q_out_stride = _rows(q_out, "q_out", dtype, dev)
     elif q_out is not None:
-        raise ValueError("rotate: q_out without q")
+        raise ValueError(f"{who}: q_out without q")
     if k is not None:
         if k.shape[0] != n:
-            raise ValueError("rotate: q and k must have the same rows")
+            raise ValueError(f"{who}: q and k must have the same rows")
         a.k, a.k_stride = _rows(k, "k", dtype, dev)
         if k_out is None and pages is None:
             k_out = _new((n, hk, 128), dtype, k, stream)
         if k_out is not None:
             if k_out.shape != k.shape:
-                raise ValueError("rotate: k_out must have k's shape")
+                raise ValueError(f"{who}: k_out must have k's shape")
             a.k_out, a.k_out_stride = _rows(k_out, "k_out", dtype, dev)
     elif k_out is not None:
-        raise ValueError("rotate: k_out without k")
+        raise ValueError(f"{who}: k_out without k")
     if pages is not None:
         if k is None or v is None or slots is None or v.shape != k.shape:
-            raise ValueError("rotate: pages take k, v of its shape, and slots")
+            raise ValueError(f"{who}: pages take k, v of its shape, and slots")
         a.v, a.v_stride = _rows(v, "v", dtype, dev)
         p = _pages(pages, dtype, dev, hk)
         a.pages = ctypes.pointer(p)
         a.slots = _flat(slots, "slots", torch.int32, dev, n)
     elif v is not None or slots is not None:
-        raise ValueError("rotate: v and slots need pages")
+        raise ValueError(f"{who}: v and slots need pages")
+    return a, dev, q_out, k_out
+
+
+def rotate(q, k, positions, axes: bytes, theta: float, *, q_out=None, k_out=None, v=None, pages=None, slots=None,
+           stream=None):
+    """protokv_rotate on token rows q [N][Hq][D] and k [N][Hkv][D] (either may be
+    None; rows may be strided): positions int32 [num_axes][N] (or [N]: every axis
+    the same), axes from ``pair_axes``.  With pages=(k, v) tensors [num_pages][Hkv]
+    [page_size][D] and slots int32 [N] the turned keys and v's rows are stored, and
+    k_out is written only if given.  -> (q_out, k_out)"""
+    a, dev, q_out, k_out = _rotate_args("rotate", q, k, positions, axes, theta, q_out, k_out, v, pages, slots, stream)
     _check(lib().protokv_rotate(ctypes.byref(a), _raw_stream(stream, dev)))
+    return q_out, k_out
+
+
+def norm_rotate(q, k, positions, axes: bytes, theta: float, q_norm, k_norm, eps: float, *, q_out=None, k_out=None, v=None,
+                pages=None, slots=None, stream=None):
+    """protokv_norm_rotate: ``rotate`` of heads that are normalised first, x / sqrt(mean(x^2) + eps)
+    times q_norm or k_norm [128] of the rows' type (None: ones).  -> (q_out, k_out)"""
+    a, dev, q_out, k_out = _rotate_args("norm_rotate", q, k, positions, axes, theta, q_out, k_out, v, pages, slots, stream)
+    dtype = (q if q is not None else k).dtype
+    n = HeadNorm(None if q_norm is None else _flat(q_norm, "q_norm", dtype, dev, 128),
+                 None if k_norm is None else _flat(k_norm, "k_norm", dtype, dev, 128), eps)
+    _check(lib().protokv_norm_rotate(ctypes.byref(a), ctypes.byref(n), _raw_stream(stream, dev)))
     return q_out, k_out
 
 
@@ -733,3 +807,161 @@ def page_attend(q, pages, table, cu, kv_len, max_add: int, *, out=None, lse=None
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(lib().protokv_page_attend(ctypes.byref(a), _raw_stream(stream, dev)))
     return out, lse
+
+
+# -- a cache in 4 bits, and pages that several requests hold ------------------
+
+
+def _pages4(pages, dev, kv_heads) -> Pages4:
+    """Pages of 4 bits: uint8 tensors (k, v) [num_pages][kv heads][page size][64] and their
+    scales (k_scale, v_scale) [num_pages][kv heads][page size][4]."""
+    import torch
+    k, v, ks, vs = pages
+    shape = k.shape
+    if len(shape) != 4 or shape[1] != kv_heads or shape[3] != 64:
+        raise ValueError(f"pages: expected k and v [num_pages, {kv_heads}, page_size, 64]")
+    n, _, size, _ = shape
+    u8 = torch.uint8
+    return Pages4(_flat(k, "pages", u8, dev, *shape), _flat(v, "pages", u8, dev, *shape),
+                  _flat(ks, "pages' scales", u8, dev, n, kv_heads, size, 4),
+                  _flat(vs, "pages' scales", u8, dev, n, kv_heads, size, 4), n, size)
+
+
+def page4_store(k, v, pages, slots, *, stream=None):
+    """protokv_page4_store: token rows k, v [N][Hkv][D] (rows may be strided) into their slots int32 [N]
+    of pages=(k, v, k_scale, v_scale), uint8 [num_pages][Hkv][page_size][64] and [..][4]."""
+    import torch
+    dev, dtype = _device(k, stream), k.dtype
+    n, hk = k.shape[:2]
+    if v.shape != k.shape:
+        raise ValueError("page4_store: k and v must have the same shape")
+    (kp, ks), (vp, vs) = _rows(k, "k", dtype, dev), _rows(v, "v", dtype, dev)
+    a = Page4RowsArgs(n, hk, 128, _kv(dtype), kp, vp, ks, vs, _flat(slots, "slots", torch.int32, dev, n),
+                      _pages4(pages, dev, hk))
+    _check(lib().protokv_page4_store(ctypes.byref(a), _raw_stream(stream, dev)))
+
+
+def page4_read(pages, slots, dtype, *, k_out=None, v_out=None, stream=None):
+    """protokv_page4_read: the rows of k and v that the slots int32 [N] of pages (as in ``page4_store``)
+    hold, as bfloat16 or float32.  -> (k_out, v_out) [N][Hkv][D]"""
+    import torch
+    dev, n, hk = _device(slots, stream), slots.shape[0], pages[0].shape[1]
+    if k_out is None:
+        k_out = _new((n, hk, 128), dtype, pages[0], stream)
+    if v_out is None:
+        v_out = _new((n, hk, 128), dtype, pages[0], stream)
+    if k_out.shape != (n, hk, 128) or v_out.shape != (n, hk, 128):
+        raise ValueError(f"page4_read: k_out and v_out must be [{n}, {hk}, 128]")
+    (kp, ks), (vp, vs) = _rows(k_out, "k_out", dtype, dev), _rows(v_out, "v_out", dtype, dev)
+    a = Page4RowsArgs(n, hk, 128, _kv(dtype), kp, vp, ks, vs, _flat(slots, "slots", torch.int32, dev, n),
+                      _pages4(pages, dev, hk))
+    _check(lib().protokv_page4_read(ctypes.byref(a), _raw_stream(stream, dev)))
+    return k_out, v_out
+
+
+def page4_attend(q, pages, table, cu, kv_len, max_add: int, *, out=None, lse=None, prior=None, workspace=None, stream=None):
+    """protokv_page4_attend: ``page_attend`` over pages of 4 bits (as in ``page4_store``).
+    -> (o, lse); lse=False: none."""
+    import torch
+    dev, dtype, i32 = _device(q, stream), q.dtype, torch.int32
+    a = Page4AttendArgs()
+    a.q, a.q_stride = _rows(q, "q", dtype, dev)
+    a.total, a.num_q_heads, _ = q.shape
+    a.num_kv_heads, a.head_dim, a.kv_dtype = pages[0].shape[1], 128, _kv(dtype)
+    a.pages = _pages4(pages, dev, a.num_kv_heads)
+    n, width = cu.shape[0] - 1, table.shape[1]
+    a.num_requests, a.max_add, a.table_stride = n, max_add, width
+    a.cu, a.kv_len = _flat(cu, "cu", i32, dev, n + 1), _flat(kv_len, "kv_len", i32, dev, n)
+    a.table = _flat(table, "table", i32, dev, n, width)
+    out, lse = _result(a, q, out, lse, prior, dev, stream)
+    if workspace is None:
+        need = ctypes.c_size_t()
+        _check(lib().protokv_page4_attend_workspace(ctypes.byref(a), ctypes.byref(need)))
+        if need.value:
+            workspace = _new((need.value,), torch.uint8, q, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor on the current device")
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib().protokv_page4_attend(ctypes.byref(a), _raw_stream(stream, dev)))
+    return out, lse
+
+
+class PageFork:
+    """What protokv_page_fork returned: ctx [requests], lens, copy_src, copy_dst and
+    copy_rows [forks], count [1] (pages left on the stack), refused [1]."""
+    __slots__ = ("ctx", "lens", "copy_src", "copy_dst", "copy_rows", "count", "refused")
+
+
+def page_fork(ctx, src, dst, table, shares, free_pages, count, page_size: int, *, at=None, stream=None) -> PageFork:
+    """protokv_page_fork: requests dst begin as copies of requests src (int32 [forks]), of their first `at`
+    tokens (None: all that ctx [requests] says); table [requests][width] and shares [num_pages] are
+    updated in place, the stack free_pages [num_pages] and count [1] are not.  ``page_copy`` then
+    brings the rows of the last pages.  The results are parts of one new tensor."""
+    import torch
+    dev, i32, r, n = _device(ctx, stream), torch.int32, ctx.shape[0], src.shape[0]
+    out = PageFork()
+    out.ctx, out.lens, out.copy_src, out.copy_dst, out.copy_rows, out.count, out.refused = torch.unsafe_split_with_sizes(
+        _new((r + 4 * n + 2,), i32, ctx, stream), (r, n, n, n, n, 1, 1))
+    width, pages, p = table.shape[1], free_pages.shape[0], out.ctx.data_ptr()
+    lens = p + 4 * r
+    a = PageForkArgs(n, r, pages, page_size, width, _flat(ctx, "ctx", i32, dev, r), _flat(src, "src", i32, dev, n),
+                     _flat(dst, "dst", i32, dev, n), None if at is None else _flat(at, "at", i32, dev, n),
+                     _flat(table, "table", i32, dev, r, width), _flat(shares, "shares", i32, dev, pages),
+                     _flat(free_pages, "free_pages", i32, dev, pages), _flat(count, "count", i32, dev, 1),
+                     lens + 16 * n, p, lens, lens + 4 * n, lens + 8 * n, lens + 12 * n, lens + 16 * n + 4)
+    _check(lib().protokv_page_fork(ctypes.byref(a), _raw_stream(stream, dev)))
+    return out
+
+
+def page_copy(arrays, src, dst, rows=None, *, stream=None):
+    """protokv_page_copy: the first rows [n] (None: all) of every head of pages src [n] to pages dst [n], in
+    each of the arrays: contiguous tensors [num_pages][Hkv][page_size][row] of one layer, or
+    [layers][num_pages][Hkv][page_size][row] of several, of any type."""
+    import torch
+    arrays = list(arrays)
+    if not 1 <= len(arrays) <= 128:
+        raise ValueError("page_copy: 1 to 128 arrays")
+    dev, i32, n = _device(arrays[0], stream), torch.int32, src.shape[0]
+    shape = arrays[0].shape[-4:-1]
+    if len(shape) != 3:
+        raise ValueError("page_copy: expected arrays [num_pages, heads, page_size, row], or of several layers")
+    pages, heads, size = shape
+    each = (PageArray * len(arrays))()
+    for x, t in zip(each, arrays):
+        if t.dim() not in (4, 5) or t.shape[-4:-1] != shape or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError(f"page_copy: expected contiguous arrays of pages {tuple(shape)} on the current device, got "
+                             f"{tuple(t.shape)} on {t.device}")
+        if t.requires_grad:
+            _no_gradient("page_copy's arrays")
+        row = t.shape[-1] * t.element_size()
+        x.base, x.row_bytes, x.layers = t.data_ptr(), row, 1 if t.dim() == 4 else t.shape[0]
+        x.layer_stride = row * size * heads * pages
+    a = PageCopyArgs(n, heads, pages, size, len(arrays), each, _flat(src, "src", i32, dev, n),
+                     _flat(dst, "dst", i32, dev, n), None if rows is None else _flat(rows, "rows", i32, dev, n))
+    _check(lib().protokv_page_copy(ctypes.byref(a), _raw_stream(stream, dev)))
+
+
+class PageRelease:
+    """What protokv_page_release returned: ctx [requests], count [1] (pages on the stack), refused [1]."""
+    __slots__ = ("ctx", "count", "refused")
+
+
+def page_release(ctx, keep, table, shares, free_pages, count, page_size: int, *, stream=None) -> PageRelease:
+    """protokv_page_release: requests of ctx tokens keep the first `keep` (int32 [requests]); pages
+    [num_pages] that nobody holds any more go onto the stack free_pages, which is updated in place
+    as shares is; count [1] is not.  The results are parts of one new tensor."""
+    import torch
+    dev, i32, n = _device(ctx, stream), torch.int32, ctx.shape[0]
+    width, pages = table.shape[1], free_pages.shape[0]
+    blocks = (pages + RELEASE_PAGES - 1) // RELEASE_PAGES
+    out = PageRelease()
+    out.ctx, out.count, out.refused, scratch = torch.unsafe_split_with_sizes(
+        _new((n + 2 + blocks,), i32, ctx, stream), (n, 1, 1, blocks))
+    p = out.ctx.data_ptr()
+    a = PageReleaseArgs(n, pages, page_size, width, _flat(ctx, "ctx", i32, dev, n), _flat(keep, "keep", i32, dev, n),
+                        _flat(table, "table", i32, dev, n, width), _flat(shares, "shares", i32, dev, pages),
+                        _flat(free_pages, "free_pages", i32, dev, pages), _flat(count, "count", i32, dev, 1),
+                        p + 4 * n, p, p + 4 * n + 4, p + 4 * n + 8)
+    _check(lib().protokv_page_release(ctypes.byref(a), _raw_stream(stream, dev)))
+    return out
