@@ -111,14 +111,6 @@ struct PageCopy {
 
 constexpr int RL_PAGES = 4096;  // pages that a workgroup looks through for freed ones
 
-// Eight values of 4 bits as bfloat16, exactly: the codes of w, the scale's exponent.
-__device__ __forceinline__ uint4 values4(uint32_t w, float scale) {
-  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
-}
-
 // How the keys and values of an attention lie.
 enum class Keys { ROWS, PAGES, PAGES4 };
 hipError_t launch_exact(const ExactArgs& a, bool fp32, Keys keys, hipStream_t st);

@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "exact.h"
+#include "page4.h"
 #include "pkv_internal.h"
 
 namespace pkv {

@@ -1,6 +1,7 @@
 // Pages of 4 bits (protokv_page4_store, protokv_page4_read) and pages that several
 // requests hold (protokv_page_fork, protokv_page_copy, protokv_page_release) for gfx950.
 #include "exact.h"
+#include "page4.h"
 #include "pkv_internal.h"
 
 namespace pkv {
