@@ -1145,10 +1145,10 @@ __device__ __forceinline__ long long wave_sum(long long x) {
 }
 // FP4: pages of 4 bits.  Lane (m, h) loads the blocks h and 2 + h of 32 dims of key m's row of K
 // and of V and turns them to bfloat16, K into the operand (the query's dims lie
-// accordingly), V into the wave's LDS, then the next tile's loads go out.
+// accordingly), V into the wave's LDS; the loads run two tiles ahead.
 template <int FP4>
 __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2][4 * FW_VB];  // the V tile in use and the next
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][(FP4 ? 1 : 2) * 4 * FW_VB];  // the V tile in use and the next
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int w = blockIdx.x * FW_W + wave;
@@ -1186,7 +1186,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   const uint8_t* vb = (const uint8_t*)a.v;
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const int grp16 = lane >> 4, s16 = lane & 15;
-  const uint8_t* vl0 = s_mem[wave][0] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
+  const uint8_t* vl0 = s_mem[wave] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
 
   // tiles [ta, tb) of request i's kv head kvh; whole: that is all of them
   auto item = [&](int i, int s0, int add, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
@@ -1231,70 +1231,150 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
         const unsigned r = __builtin_amdgcn_ds_bpermute(64 * g + (lane & ~3), rw);
         const uint8_t* p = vb + (size_t)r * (D * 2) + (lane & 3) * 16;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) lds_dma16(p + b * 64, s_mem[wave][buf] + b * FW_VB + g * 1024);
+        for (int b = 0; b < 4; ++b) lds_dma16(p + b * 64, s_mem[wave] + buf * (4 * FW_VB) + b * FW_VB + g * 1024);
       }
     };
-    uint4 kc[2], vc[2];  // 4 bits: codes and scales of this lane's blocks
-    uint32_t ks = 0, vs = 0;
-    auto load_codes = [&](int rw) {
-      const size_t r = (unsigned)rw;
-      const uint4 *k4 = reinterpret_cast<const uint4*>(kb) + r * 4 + half, *v4 = reinterpret_cast<const uint4*>(vb) + r * 4 + half;
-      ks = reinterpret_cast<const uint32_t*>(a.ksc)[r];
-      kc[0] = k4[0];
-      kc[1] = k4[2];
-      vs = reinterpret_cast<const uint32_t*>(a.vsc)[r];
-      vc[0] = v4[0];
-      vc[1] = v4[2];
+    struct Codes {  // a tile of 4 bits: this lane's blocks `half` and 2 + half of its key, and the key's scales
+      uint4 k[2], v[2];
+      uint32_t ks, vs;
+      bool bad;
     };
-    auto scale_of = [&](uint32_t s, int i) { return __uint_as_float(((s >> (16 * i + 8 * half)) & 255) << 23); };
+    auto load4 = [&](size_t r, Codes& c) {
+      const uint4 *k4 = reinterpret_cast<const uint4*>(kb) + r * 4 + half, *v4 = reinterpret_cast<const uint4*>(vb) + r * 4 + half;
+      c.ks = reinterpret_cast<const uint32_t*>(a.ksc)[r];
+      c.k[0] = k4[0];
+      c.k[1] = k4[2];
+      c.vs = reinterpret_cast<const uint32_t*>(a.vsc)[r];
+      c.v[0] = v4[0];
+      c.v[1] = v4[2];
+    };
     auto part_of = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
-    if (ta < tend) {
+    // 4 bits: tile t from c, whose registers then take tile t + 2; id: the page of tile t + 2, then of t + 3
+    auto step4 = [&](int t, Codes& c, int& id) {
+      const unsigned badm = (unsigned)__ballot(c.bad);
+      const bool masked = (t + 1) * 32 > wfull || badm != 0;  // uniform
+      // blocks of V that read as NaN: their codes go into the products as zeros, and NaN into the
+      // outputs of the rows that see them (a zero weight times NaN would be one)
+      const bool odd = __ballot((((c.vs & 0x7F7F7F7Fu) + 0x01010101u) & c.vs & 0x80808080u) != 0) != 0;  // uniform
+      unsigned nans[4] = {0, 0, 0, 0};  // keys of each block of 32 dims
+      if (odd) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) nans[b] = (unsigned)__ballot(((c.vs >> (8 * b)) & 255) == 255);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (((c.vs >> (16 * i + 8 * half)) & 255) == 255) {
+            c.vs &= ~(255u << (16 * i + 8 * half));
+            c.v[i] = make_uint4(0, 0, 0, 0);
+          }
+      }
+      auto scale_of = [&](uint32_t w, int i) { return __uint_as_float(((w >> (16 * i + 8 * half)) & 255) << 23); };
+      f32x16 s = zero;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, values4(part_of(c.k[kk >> 2], kk & 3), scale_of(c.ks, kk >> 2))), bq[kk], s, 0, 0, 0);
+      uint8_t* vw = s_mem[wave] + half * FW_VB + m * 64;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<uint4*>(vw + 2 * (j >> 2) * FW_VB + (j & 3) * 16) =
+            values4(part_of(c.v[j >> 2], j & 3), scale_of(c.vs, j >> 2));
+      if (t + 2 < tend) {  // uniform
+        const size_t r = (unsigned)row_of(t + 2, id, c.bad);
+        id = id_of(min(t + 3, tend - 1));
+        load4(r, c);
+      }
+      const int rel = klim - t * 32 - 4 * half;
+      const unsigned bm = badm >> (4 * half);
+      if (masked) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          s[j] = 8 * (j >> 2) + (j & 3) > rel || ((bm >> (8 * (j >> 2) + (j & 3))) & 1) ? -INFINITY : s[j];
+      }
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) tmax = fmaxf(tmax, s[j]);
+      tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
+      const bool grow = tmax > mref + 8.0f;
+      if (__ballot(grow)) {  // uniform
+        const float mnew = grow ? tmax : mref;
+        const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
+        lrun *= alpha;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
+        mref = mnew;
+      }
+      v8i16 vo[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint8_t* p = vl0 + (i >> 1) * FW_VB + (i & 1) * 1024;
+        const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)p);
+        const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(p + 512));
+        vo[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+      bf16x8 pb[2];
+      float part[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[j], EX_SCALE, -mref));
+        part[j & 1] += p;
+        pb[j >> 3][j & 7] = (__bf16)p;
+      }
+      lrun += part[0] + part[1];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        oacc[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vo[i]), pb[i & 1], oacc[i >> 1], 0, 0, 0);
+      if (odd) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          bool hit = false;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int key = 8 * (j >> 2) + (j & 3);
+            hit |= key <= rel && ((nans[b] & ~badm) >> (4 * half + key)) & 1;
+          }
+          oacc[b] += xor32(hit ? 1 : 0) | hit ? NAN : 0.f;
+        }
+      }
+    };
+    if constexpr (FP4) {
+      if (ta < tend) {
+        Codes c0, c1;
+        load4((unsigned)row_of(ta, id_of(ta), c0.bad), c0);
+        load4((unsigned)row_of(min(ta + 1, tend - 1), id_of(min(ta + 1, tend - 1)), c1.bad), c1);
+        int id = id_of(min(ta + 2, tend - 1));
+        for (int t = ta; t < tend; t += 2) {
+          step4(t, c0, id);
+          if (t + 1 < tend) step4(t + 1, c1, id);  // uniform
+        }
+      }
+    } else if (ta < tend) {
       u16x8 kr[8];
       bool bad;
       int rw = row_of(ta, id_of(ta), bad);
       int id = id_of(min(ta + 1, tend - 1));
-      if constexpr (FP4) {
-        load_codes(rw);
-      } else {
-        load_v(rw, ta & 1);
-        __builtin_amdgcn_sched_barrier(0);
-        load_k(rw, kr);
-      }
+      load_v(rw, ta & 1);
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(rw, kr);
       for (int t = ta; t < tend; ++t) {
         const int tn = min(t + 1, tend - 1);  // past the last tile the loads repeat it
         const unsigned badm = (unsigned)__ballot(bad);
         rw = row_of(tn, id, bad);
         const bool masked = (t + 1) * 32 > wfull || badm != 0;  // uniform
         f32x16 s = zero;
-        if constexpr (FP4) {
 #pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8, values4(part_of(kc[kk >> 2], kk & 3), scale_of(ks, kk >> 2))), bq[kk], s, 0, 0, 0);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<uint4*>(s_mem[wave][t & 1] + (2 * (j >> 2) + half) * FW_VB + m * 64 + (j & 3) * 16) =
-                values4(part_of(vc[j >> 2], j & 3), scale_of(vs, j >> 2));
-          if (t + 1 < tend) {  // uniform
-            id = id_of(min(tn + 1, tend - 1));
-            load_codes(rw);
-          }
-        } else {
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[kk]), bq[kk], s, 0, 0, 0);
-          // Loads return in the order of their issue: V's are issued before K's of the
-          // same tile, so with K in the registers of the products V is in LDS.
-          asm volatile("" : "+v"(s) : : "memory");
+        for (int kk = 0; kk < 8; ++kk)
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[kk]), bq[kk], s, 0, 0, 0);
+        // Loads return in the order of their issue: V's are issued before K's of the
+        // same tile, so with K in the registers of the products V is in LDS.
+        asm volatile("" : "+v"(s) : : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 1 < tend) {  // uniform
+          id = id_of(min(tn + 1, tend - 1));
+          load_v(rw, (t + 1) & 1);  // read last by the products of tile t - 1
           __builtin_amdgcn_sched_barrier(0);
-          if (t + 1 < tend) {  // uniform
-            id = id_of(min(tn + 1, tend - 1));
-            load_v(rw, (t + 1) & 1);  // read last by the products of tile t - 1
-            __builtin_amdgcn_sched_barrier(0);
-            load_k(rw, kr);
-          }
-          __builtin_amdgcn_sched_barrier(0);
+          load_k(rw, kr);
         }
+        __builtin_amdgcn_sched_barrier(0);
         const uint8_t* vl = vl0 + (t & 1) * (4 * FW_VB);
         if (masked) {
           const int rel = klim - t * 32 - 4 * half;

@@ -123,10 +123,13 @@ __global__ __launch_bounds__(256) void k_page4_read(Page4Rows a) {
 }
 
 // ---------------------------------------------------------------------------
-// Forks.  One workgroup decides: who is refused, who gets which page; then a
-// wave to a fork copies its table row and counts the owners.  Latency chains both.
+// Forks.  One workgroup decides who is refused and who gets which page.  Where the
+// forks' table rows are short together (PG_FEW entries) it copies them and counts the owners as well,
+// else a second launch does that, with workgroups to each fork.  Latency chains both.
 // ---------------------------------------------------------------------------
 constexpr int FK_NT = 1024;
+constexpr int PG_FEW = 16384;  // table entries, and pages, that one workgroup goes through by itself
+constexpr int PG_REQ = 2048;   // and requests
 
 // Inclusive running sum over the workgroup's threads; total: of all.  s: FK_NT / 64
 // words, free again after the next barrier.
@@ -150,7 +153,9 @@ __device__ __forceinline__ int block_sum(int x, int* s, int& total) {
   return before + x;
 }
 
+template <int ROWS>
 __global__ __launch_bounds__(FK_NT) void k_page_fork(protokv_page_fork_args a, int shift) {
+  __shared__ int4 s_fork[ROWS ? PG_REQ : 1];     // full pages, src, dst
   __shared__ uint32_t s_src[MAX_REQUESTS / 32];  // requests that are forked
   __shared__ int s_dst[MAX_REQUESTS];            // first fork that becomes request r; once granted -1 - its tokens
   __shared__ int s_sum[2][FK_NT / 64];
@@ -203,6 +208,7 @@ __global__ __launch_bounds__(FK_NT) void k_page_fork(protokv_page_fork_args a, i
       a.copy_dst[i] = to;
       a.copy_rows[i] = ok ? part : 0;
       if (ok) s_dst[d] = -1 - len;  // no other thread's fork is i
+      if constexpr (ROWS) s_fork[i] = make_int4(ok ? full : 0, s, d, 0);
       refused += !ok;
     }
   }
@@ -212,6 +218,26 @@ __global__ __launch_bounds__(FK_NT) void k_page_fork(protokv_page_fork_args a, i
   if (tid == 0) {
     a.free_count_out[0] = held - min(asked, held);
     if (a.refused) a.refused[0] = s_refused;
+  }
+  if constexpr (ROWS) {
+    // (no src is a dst, so that what is read here was not written above)
+    const int all = n * a.table_stride;
+    for (int x0 = tid; x0 < all; x0 += 4 * FK_NT) {
+      int page[4], to[4];  // four entries in flight
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int x = x0 + k * FK_NT, i = x / a.table_stride, j = x - i * a.table_stride;
+        const int4 f = x < all ? s_fork[i] : make_int4(0, 0, 0, 0);
+        to[k] = j < f.x ? f.z * a.table_stride + j : -1;  // (at most 8192 rows of PG_FEW)
+        if (to[k] >= 0) page[k] = a.table[f.y * a.table_stride + j];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (to[k] < 0) continue;
+        a.table[to[k]] = page[k];
+        if ((unsigned)page[k] < (unsigned)a.num_pages) atomicAdd(&a.shares[page[k]], 1);
+      }
+    }
   }
 }
 
@@ -255,24 +281,89 @@ __global__ __launch_bounds__(256) void k_page_copy(PageCopy a) {
 
 // ---------------------------------------------------------------------------
 // Releases, in three steps: what each request keeps, from the owners as they are;
-// an owner less for every page dropped, whose count then is -1 exactly if none is
-// left; those pages onto the stack in their order.  scratch[b]: pages freed
-// of the 4096 from 4096 b on.
+// an owner less for every page dropped, whose count then is below 0 exactly if none is
+// left; those pages onto the stack in their order.  Each step needs the whole of the
+// one before: one workgroup where entries and pages are few (PG_FEW), else a launch to each, with
+// a wave to a request.  Latency chains.
 // ---------------------------------------------------------------------------
+
+// Tokens that request i of ctx tokens keeps; -1 if that is refused.
+__device__ __forceinline__ int kept(const protokv_page_release_args& a, int i, int ctx, int shift) {
+  const int keep = min(max(a.keep[i], 0), ctx);
+  if (keep < ctx && (keep & ((1 << shift) - 1))) {
+    const int page = a.table[(size_t)i * a.table_stride + (keep >> shift)];
+    if ((unsigned)page < (unsigned)a.num_pages && a.shares[page] > 0) return -1;
+  }
+  return keep;
+}
+__device__ __forceinline__ int pages_of(int tokens, int shift) { return (int)(((long long)tokens + (1 << shift) - 1) >> shift); }
+
+__global__ __launch_bounds__(1024) void k_release_few(protokv_page_release_args a, int shift) {
+  __shared__ int2 s_drop[PG_REQ];  // pages first .. end - 1 of a request
+  __shared__ int s_sum[16];
+  __shared__ int s_refused;
+  const int tid = threadIdx.x, span = a.table_stride << shift;
+  if (tid == 0) s_refused = 0;
+  __syncthreads();
+  for (int i = tid; i < a.num_requests; i += 1024) {
+    const int ctx = min(max(a.ctx[i], 0), span);
+    int keep = kept(a, i, ctx, shift);
+    if (keep < 0) {
+      keep = ctx;
+      atomicAdd(&s_refused, 1);
+    }
+    a.ctx_out[i] = keep;
+    s_drop[i] = make_int2(pages_of(keep, shift), pages_of(ctx, shift));
+  }
+  __syncthreads();
+  const int all = a.num_requests * a.table_stride;
+  for (int x0 = tid; x0 < all; x0 += 4096) {
+    int page[4];  // four entries in flight
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int x = x0 + 1024 * k, i = x / a.table_stride, j = x - i * a.table_stride;
+      const int2 d = x < all ? s_drop[i] : make_int2(0, 0);
+      page[k] = j >= d.x && j < d.y ? a.table[x] : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if ((unsigned)page[k] < (unsigned)a.num_pages) atomicSub(&a.shares[page[k]], 1);
+  }
+  wait_vm<0>();  // this wave's are done
+  __syncthreads();
+  // a thread's pages lie together; read past the L1, which may hold them as they were
+  const int per = (a.num_pages + 1023) / 1024, p0 = tid * per;
+  uint32_t freed = 0;
+#pragma unroll
+  for (int k = 0; k < PG_FEW / 1024; ++k)
+    if (k < per && p0 + k < a.num_pages)
+      freed |= (__hip_atomic_load(&a.shares[p0 + k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0 ? 1u : 0u) << k;
+  int total;
+  const int held = min(max(a.free_count[0], 0), a.num_pages);
+  int at = held + block_sum(__popc(freed), s_sum, total) - __popc(freed);
+  for (; freed; freed &= freed - 1, ++at) {
+    const int page = p0 + __ffs(freed) - 1;
+    a.shares[page] = 0;
+    if (at < a.num_pages) a.free_pages[at] = page;
+  }
+  if (tid == 0) {
+    a.free_count_out[0] = min(held + total, a.num_pages);
+    a.refused[0] = s_refused;
+  }
+}
+
+// scratch[b]: pages freed of the RL_PAGES from RL_PAGES b on
 __global__ __launch_bounds__(1024) void k_release_keep(protokv_page_release_args a, int shift) {
   __shared__ int s_refused;
-  const int span = a.table_stride << shift, P1 = (1 << shift) - 1;
+  const int span = a.table_stride << shift;
   if (threadIdx.x == 0) s_refused = 0;
   __syncthreads();
   for (int i = threadIdx.x; i < a.num_requests; i += 1024) {
     const int ctx = min(max(a.ctx[i], 0), span);
-    int keep = min(max(a.keep[i], 0), ctx);
-    if (keep < ctx && (keep & P1)) {
-      const int page = a.table[(size_t)i * a.table_stride + (keep >> shift)];
-      if ((unsigned)page < (unsigned)a.num_pages && a.shares[page] > 0) {
-        keep = ctx;
-        atomicAdd(&s_refused, 1);
-      }
+    int keep = kept(a, i, ctx, shift);
+    if (keep < 0) {
+      keep = ctx;
+      atomicAdd(&s_refused, 1);
     }
     a.ctx_out[i] = keep;
   }
@@ -281,16 +372,33 @@ __global__ __launch_bounds__(1024) void k_release_keep(protokv_page_release_args
   if (threadIdx.x == 0) a.refused[0] = s_refused;
 }
 
+constexpr int RL_BINS = 256;  // entries of scratch that a workgroup counts in its LDS first
 __global__ __launch_bounds__(256) void k_release_drop(protokv_page_release_args a, int shift) {
-  const int i = blockIdx.y, P1 = (1 << shift) - 1, span = a.table_stride << shift;
-  const int ctx = min(max(a.ctx[i], 0), span);
-  const int first = (int)(((long long)a.ctx_out[i] + P1) >> shift), end = (int)(((long long)ctx + P1) >> shift);
-  for (int j = first + blockIdx.x * 256 + threadIdx.x; j < end; j += gridDim.x * 256) {
-    const int page = a.table[(size_t)i * a.table_stride + j];
-    // of a page's drops the one that finds no owner beyond itself is one alone
-    if ((unsigned)page < (unsigned)a.num_pages && atomicSub(&a.shares[page], 1) == 0)
-      atomicAdd(&a.scratch[page / RL_PAGES], 1);
+  __shared__ int s_freed[RL_BINS];
+  const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6), span = a.table_stride << shift;
+  const bool few = (a.num_pages + RL_PAGES - 1) / RL_PAGES <= RL_BINS;  // uniform
+  s_freed[threadIdx.x] = 0;
+  __syncthreads();
+  if (i < a.num_requests) {
+    const int ctx = min(max(a.ctx[i], 0), span);
+    const int first = pages_of(a.ctx_out[i], shift), end = pages_of(ctx, shift);
+    const int32_t* row = a.table + (size_t)i * a.table_stride;
+    for (int j0 = first + lane; j0 < end; j0 += 256) {
+      int page[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) page[k] = j0 + 64 * k < end ? row[j0 + 64 * k] : -1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // of a page's drops the one that finds no owner beyond itself is one alone
+        if ((unsigned)page[k] < (unsigned)a.num_pages && atomicSub(&a.shares[page[k]], 1) == 0) {
+          if (few) atomicAdd(&s_freed[page[k] / RL_PAGES], 1);
+          else atomicAdd(&a.scratch[page[k] / RL_PAGES], 1);
+        }
+      }
+    }
   }
+  __syncthreads();
+  if (few && s_freed[threadIdx.x]) atomicAdd(&a.scratch[threadIdx.x], s_freed[threadIdx.x]);
 }
 
 __global__ __launch_bounds__(1024) void k_release_collect(protokv_page_release_args a) {
@@ -333,7 +441,11 @@ hipError_t launch_page4_rows(const Page4Rows& a, bool fp32, bool store, hipStrea
 
 hipError_t launch_page_fork(const protokv_page_fork_args& a, hipStream_t st) {
   const int shift = 31 - __builtin_clz((unsigned)a.page_size);
-  hipLaunchKernelGGL(k_page_fork, dim3(1), dim3(FK_NT), 0, st, a, shift);
+  if (a.num_forks <= PG_REQ && (long long)a.num_forks * a.table_stride <= PG_FEW) {
+    hipLaunchKernelGGL((k_page_fork<1>), dim3(1), dim3(FK_NT), 0, st, a, shift);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((k_page_fork<0>), dim3(1), dim3(FK_NT), 0, st, a, shift);
   const unsigned parts = std::min((a.table_stride + 255u) / 256u, 64u);
   hipLaunchKernelGGL(k_page_fork_rows, dim3(parts, a.num_forks), dim3(256), 0, st, a, shift);
   return hipGetLastError();
@@ -346,9 +458,12 @@ hipError_t launch_page_copy(const PageCopy& a, int copies, int layers, unsigned 
 
 hipError_t launch_page_release(const protokv_page_release_args& a, hipStream_t st) {
   const int shift = 31 - __builtin_clz((unsigned)a.page_size);
+  if (a.num_requests <= PG_REQ && (long long)a.num_requests * a.table_stride <= PG_FEW && a.num_pages <= PG_FEW) {
+    hipLaunchKernelGGL(k_release_few, dim3(1), dim3(1024), 0, st, a, shift);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(k_release_keep, dim3(1), dim3(1024), 0, st, a, shift);
-  const unsigned parts = std::min((a.table_stride + 255u) / 256u, 64u);
-  hipLaunchKernelGGL(k_release_drop, dim3(parts, a.num_requests), dim3(256), 0, st, a, shift);
+  hipLaunchKernelGGL(k_release_drop, dim3((a.num_requests + 3) / 4), dim3(256), 0, st, a, shift);
   hipLaunchKernelGGL(k_release_collect, dim3((a.num_pages + RL_PAGES - 1) / RL_PAGES), dim3(1024), 0, st, a);
   return hipGetLastError();
 }

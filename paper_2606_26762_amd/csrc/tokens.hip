@@ -101,6 +101,12 @@ __device__ __forceinline__ void rotate_rows(const RotateArgs& a, const NormArgs&
                                   : a.v + t * a.vs + (size_t)vh * (D * ES);
     V lo = reinterpret_cast<const V*>(src)[c8], hi = reinterpret_cast<const V*>(src + D / 2 * ES)[c8];
     if (NORM && vh < 0) {
+      const uint8_t* w = h < a.Hq ? nm.qw : nm.kw;
+      V wl, wh;
+      if (w) {
+        wl = reinterpret_cast<const V*>(w)[c8];
+        wh = reinterpret_cast<const V*>(w + D / 2 * ES)[c8];
+      }
       double ss = 0.0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -108,7 +114,6 @@ __device__ __forceinline__ void rotate_rows(const RotateArgs& a, const NormArgs&
         ss = fma(x, x, fma(y, y, ss));
       }
       const float inv = (float)(1.0 / sqrt(sum8(ss) * (1.0 / D) + nm.eps));
-      const uint8_t* w = h < a.Hq ? nm.qw : nm.kw;
       float x[8], y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -116,7 +121,6 @@ __device__ __forceinline__ void rotate_rows(const RotateArgs& a, const NormArgs&
         y[i] = hi.get(i) * inv;
       }
       if (w) {
-        const V wl = reinterpret_cast<const V*>(w)[c8], wh = reinterpret_cast<const V*>(w + D / 2 * ES)[c8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           x[i] *= wl.get(i);

@@ -846,9 +846,11 @@ def page4_read(pages, slots, dtype, *, k_out=None, v_out=None, stream=None):
     hold, as bfloat16 or float32.  -> (k_out, v_out) [N][Hkv][D]"""
     import torch
     dev, n, hk = _device(slots, stream), slots.shape[0], pages[0].shape[1]
-    if k_out is None:
+    if k_out is None and v_out is None:
+        k_out, v_out = _new((2, n, hk, 128), dtype, pages[0], stream).unbind(0)
+    elif k_out is None:
         k_out = _new((n, hk, 128), dtype, pages[0], stream)
-    if v_out is None:
+    elif v_out is None:
         v_out = _new((n, hk, 128), dtype, pages[0], stream)
     if k_out.shape != (n, hk, 128) or v_out.shape != (n, hk, 128):
         raise ValueError(f"page4_read: k_out and v_out must be [{n}, {hk}, 128]")
@@ -863,27 +865,38 @@ def page4_attend(q, pages, table, cu, kv_len, max_add: int, *, out=None, lse=Non
     """protokv_page4_attend: ``page_attend`` over pages of 4 bits (as in ``page4_store``).
     -> (o, lse); lse=False: none."""
     import torch
-    dev, dtype, i32 = _device(q, stream), q.dtype, torch.int32
-    a = Page4AttendArgs()
-    a.q, a.q_stride = _rows(q, "q", dtype, dev)
-    a.total, a.num_q_heads, _ = q.shape
-    a.num_kv_heads, a.head_dim, a.kv_dtype = pages[0].shape[1], 128, _kv(dtype)
-    a.pages = _pages4(pages, dev, a.num_kv_heads)
-    n, width = cu.shape[0] - 1, table.shape[1]
-    a.num_requests, a.max_add, a.table_stride = n, max_add, width
-    a.cu, a.kv_len = _flat(cu, "cu", i32, dev, n + 1), _flat(kv_len, "kv_len", i32, dev, n)
-    a.table = _flat(table, "table", i32, dev, n, width)
-    out, lse = _result(a, q, out, lse, prior, dev, stream)
+    dev, dtype, i32, f32 = _device(q, stream), q.dtype, torch.int32, torch.float32
+    qp, qs = _rows(q, "q", dtype, dev)
+    total, hq, _ = q.shape
+    hk, n, width = pages[0].shape[1], cu.shape[0] - 1, table.shape[1]
+    paged, kv = _pages4(pages, dev, hk), _kv(dtype)
+    if out is None:
+        out = torch.empty_like(q) if stream is None and q.is_contiguous() else _new((total, hq, 128), dtype, q, stream)
+        o = out.data_ptr()
+    else:
+        o = _flat(out, "out", dtype, dev, total, hq, 128)
+    l = po = pl = None
+    if lse is None:
+        lse = _new((total, hq), f32, q, stream)
+        l = lse.data_ptr()
+    elif lse is not False:
+        l = _flat(lse, "lse", f32, dev, total, hq)
+    if prior is not None:
+        po, pl = _flat(prior[0], "prior", dtype, dev, total, hq, 128), _flat(prior[1], "prior lse", f32, dev, total, hq)
+    a = Page4AttendArgs(hq, hk, 128, kv, n, total, max_add, width, _flat(cu, "cu", i32, dev, n + 1),
+                        _flat(kv_len, "kv_len", i32, dev, n), _flat(table, "table", i32, dev, n, width), qp, qs, paged, o, l,
+                        po, pl, None, 0)
+    at = ctypes.byref(a)
     if workspace is None:
         need = ctypes.c_size_t()
-        _check(lib().protokv_page4_attend_workspace(ctypes.byref(a), ctypes.byref(need)))
+        _check(lib().protokv_page4_attend_workspace(at, ctypes.byref(need)))
         if need.value:
             workspace = _new((need.value,), torch.uint8, q, stream)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace: expected a contiguous tensor on the current device")
     if workspace is not None:
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(lib().protokv_page4_attend(ctypes.byref(a), _raw_stream(stream, dev)))
+    _check(lib().protokv_page4_attend(at, _raw_stream(stream, dev)))
     return out, lse
 
 
