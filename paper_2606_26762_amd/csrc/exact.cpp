@@ -138,7 +138,7 @@ protokv_status check_result(const Heads& h, int n, int total, const int32_t* cu,
 // 62 in one of 32 768).  Measured, 28 / 4 heads, tables as wide as the contexts: one
 // prompt of 1500 tokens 43 us by 256 rows, 34 by 128; eight of 200 17 and 25; one of
 // 4000 115 and 146; 4 x 512 tokens over 16 k in 3 splits 540, unsplit 484.
-void plan_blocks(ExactArgs& a, bool paged) {
+int64_t plan_blocks(ExactArgs& a, bool paged) {
   const int64_t slots = 256;
   const int64_t keys = paged ? (int64_t)a.stride << a.shift : ((int64_t)a.total + a.n - 1) / std::max(a.n, 1);
   const int64_t tiles = (keys + 63) / 64;
@@ -159,6 +159,7 @@ void plan_blocks(ExactArgs& a, bool paged) {
       }
     }
   }
+  return best;
 }
 
 // Row blocks of float32: 32 rows, whose waves take the 32-key tiles in turn, a tile
@@ -221,7 +222,7 @@ size_t lay_out(ExactArgs& a, uint8_t* base) {
   return off;
 }
 
-protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a, const char* who) {
+protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a, bool four, const char* who) {
   const Heads h{p->num_q_heads, p->num_kv_heads, p->head_dim, p->kv_dtype};
   protokv_status s = check_heads(h, who);
   if (s != PROTOKV_OK) return s;
@@ -254,16 +255,41 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
   const bool many = (int64_t)a.max_add * a.grp > EX_FEW;
   const int64_t rows = (int64_t)a.total * a.grp;
   const bool alone = many && ((rows / EX_ROWS + a.n) * a.Hkv <= 64 || rows >= (int64_t)256 * a.n);
-  if (!fp32 && !alone) {
-    const int64_t tiles = (((int64_t)a.stride << a.shift) + 31) / 32;
-    const int64_t waves = std::max<int64_t>(1, ((int64_t)a.Hkv * a.n * tiles + 1) / 2);
-    a.few = a.n ? (int)std::min<int64_t>(EX_FEW_WAVES, (waves + 3) / 4 * 4) : 0;
-    a.few_rows = (int)std::min<int64_t>(EX_FEW, (int64_t)a.max_add * a.grp);
-  }
+  const bool with_few = !fp32 && !alone;
+  a.few_limit = EX_FEW;
+  a.few_rows = (int)std::min<int64_t>(EX_FEW, (int64_t)a.max_add * a.grp);
+  const int64_t span = (int64_t)a.stride << a.shift;
+  auto few_waves = [&](int64_t runs) {
+    a.few = a.n ? (int)std::min<int64_t>(EX_FEW_WAVES, (std::max<int64_t>(1, runs) + 3) / 4 * 4) : 0;
+  };
   a.splits = 1;
   if (fp32) plan_blocks_f32(a, true);
-  else if (many) plan_blocks(a, true);
-  return check_grid(a, who);
+  const int64_t cost = !fp32 && many ? plan_blocks(a, true) + (with_few ? 45 : 0) : 0;
+  s = check_grid(a, who);
+  if (s != PROTOKV_OK) return s;
+  if (four && !fp32) {
+    // Pages of 4 bits: the few-rows kernel takes requests of more rows too, in groups of
+    // 32, if it takes all of them and that costs less: its waves go through equal runs of tiles
+    // whatever the lengths, where a row block of few rows leaves most of its compute unit
+    // idle and a long context among short ones holds one for its whole length.  A wave's tile of 64
+    // keys counts 16 of plan_blocks' tenths where the waves fill the GPU, else 10, launches and join
+    // 60, and a fifth on top, which the blocks' count is closer by.  28 / 4 heads: 64 x 16 tokens
+    // over 8000 327 us by blocks, 203; 8 x 40 over 250 to 16 000 93 and 55; but 8 x 512 over
+    // 16 000 895 and 1290, one chunk of 64 over 30 000 49 and 61.  Over 44 shapes of 1 to 64 requests the
+    // better of the two is 2.5 % below this choice on average, at most 38 %.
+    const int64_t groups = many ? rows / EX_FEW + a.n : a.n, tiles = a.Hkv * groups * ((span + 63) / 64);
+    const int64_t run = std::max<int64_t>({(tiles + EX_FEW_WAVES - 1) / EX_FEW_WAVES, std::min<int64_t>(EX_FEW_RUN4, (tiles + 511) / 512), 1});
+    const bool all = many && (run * (tiles > 1024 * run ? 16 : 10) + 60) * 6 / 5 <= cost;
+    if (all) {
+      a.few_limit = INT32_MAX;
+      a.blocks = 0;
+      a.splits = 1;
+    }
+    if (all || with_few) few_waves(tiles);
+  } else if (with_few) {
+    few_waves(((int64_t)a.Hkv * a.n * ((span + 31) / 32) + 1) / 2);
+  }
+  return PROTOKV_OK;
 }
 
 protokv_status rotate(const protokv_rotate_args* a, const protokv_head_norm* norm, void* stream, const char* who) {
@@ -343,7 +369,7 @@ protokv_status rotate(const protokv_rotate_args* a, const protokv_head_norm* nor
 
 protokv_status page_attend(const protokv_page_attend_args* p, const protokv_pages4* four, void* stream, const char* who) {
   ExactArgs a{};
-  protokv_status s = page_attend_shape(p, a, who);
+  protokv_status s = page_attend_shape(p, a, four != nullptr, who);
   if (s != PROTOKV_OK) return s;
   const Heads h{p->num_q_heads, p->num_kv_heads, p->head_dim, p->kv_dtype};
   s = check_result(h, p->num_requests, p->total, p->cu, p->o, p->lse, p->prior_o, p->prior_lse, who);
@@ -406,9 +432,9 @@ protokv_page_attend_args as_page_attend(const protokv_page4_attend_args& p) {
   return a;
 }
 
-protokv_status attend_workspace(const protokv_page_attend_args& p, size_t* bytes, const char* who) {
+protokv_status attend_workspace(const protokv_page_attend_args& p, bool four, size_t* bytes, const char* who) {
   ExactArgs a{};
-  protokv_status s = page_attend_shape(&p, a, who);
+  protokv_status s = page_attend_shape(&p, a, four, who);
   if (s == PROTOKV_OK) *bytes = lay_out(a, nullptr);
   return s;
 }
@@ -535,7 +561,7 @@ protokv_status protokv_prompt_attend(const protokv_prompt_args* p, void* stream)
 protokv_status protokv_page_attend_workspace(const protokv_page_attend_args* p, size_t* bytes) PKV_GUARD("page_attend_workspace", {
   const char* who = "page_attend_workspace";
   if (!p || !bytes) return fail(PROTOKV_E_INVALID, who, "args and bytes must be non-NULL");
-  return attend_workspace(*p, bytes, who);
+  return attend_workspace(*p, false, bytes, who);
 })
 
 protokv_status protokv_page_attend(const protokv_page_attend_args* p, void* stream) PKV_GUARD("page_attend", {
@@ -547,7 +573,7 @@ protokv_status protokv_page_attend(const protokv_page_attend_args* p, void* stre
 protokv_status protokv_page4_attend_workspace(const protokv_page4_attend_args* p, size_t* bytes) PKV_GUARD("page4_attend_workspace", {
   const char* who = "page4_attend_workspace";
   if (!p || !bytes) return fail(PROTOKV_E_INVALID, who, "args and bytes must be non-NULL");
-  return attend_workspace(as_page_attend(*p), bytes, who);
+  return attend_workspace(as_page_attend(*p), true, bytes, who);
 })
 
 protokv_status protokv_page4_attend(const protokv_page4_attend_args* p, void* stream) PKV_GUARD("page4_attend", {

@@ -21,6 +21,7 @@ constexpr int EX_MAX_SPLITS = 32, EX_MAX_SPLITS_F32 = 64;
 constexpr int EX_MIN_TILES = 4;  // a context of fewer than twice as many tiles (64 keys bf16, 32 float32) is not split
 constexpr int EX_FEW = 32;        // rows per kv head of a request that the few-rows kernel takes
 constexpr int EX_FEW_WAVES = 2048;  // waves of the few-rows kernel, at most (two to a SIMD)
+constexpr int EX_FEW_RUN4 = 8;    // its tiles of 64 keys of 4 bits to a wave that are not spread over more waves than 512
 constexpr int MAX_REQUESTS = 8192;
 constexpr int MAX_AXES = 8;
 
@@ -62,6 +63,7 @@ struct ExactArgs {
   float *few_o, *few_ml;
   int32_t* few_meta;
   int few, few_rows;  // its waves (0: not launched, the row blocks take every request), its rows at most
+  int few_limit;      // pages of 4 bits: rows per kv head of a request that it takes, in groups of 32
   int rows;    // query rows of a row block
   int blocks;  // row-block indices per kv head (0: no row blocks)
   int splits;  // most context splits of a row block

@@ -46,14 +46,15 @@ struct Item {
 };
 
 // Row block blk of sequence i, whose rows are c0 .. c1 - 1; false if there is none.
-template <int R>
+// FEW: a request of at most so many rows is not the row blocks' (0: few_limit).
+template <int R, int FEW = EX_FEW>
 __device__ __forceinline__ bool set_item(const ExactArgs& a, int i, int c0, int c1, int blk, Item& it) {
   it.seq = i;
   it.s0 = c0;
   it.add = c1 - c0;
   if (it.add <= 0 || blk < 0) return false;
   it.rows = min(it.add, a.max_add) * a.grp;
-  if (blk >= (it.rows + R - 1) / R || (a.few && it.rows <= EX_FEW)) return false;
+  if (blk >= (it.rows + R - 1) / R || (a.few && it.rows <= (FEW ? FEW : a.few_limit))) return false;
   it.row0 = blk * R;
   int kv = it.add;
   it.off = 0;
@@ -70,7 +71,7 @@ __device__ __forceinline__ bool set_item(const ExactArgs& a, int i, int c0, int 
 // f(i) = floor(cu[i] grp / R) + i, non-decreasing, so it is found by comparing 64
 // entries at a time; indices behind a sequence's rows are left empty.  Every
 // lane of the wave takes part; false (uniform) if the block is empty.
-template <int R>
+template <int R, int FEW = EX_FEW>
 __device__ __forceinline__ bool find_item(const ExactArgs& a, int b, Item& it) {
   const int lane = threadIdx.x & 63;
   auto entry = [&](int i) { return min(max(a.cu[i], 0), a.total); };
@@ -90,7 +91,7 @@ __device__ __forceinline__ bool find_item(const ExactArgs& a, int b, Item& it) {
     lo += l * step;
     hi = min(hi, lo + step);
   }
-  return set_item<R>(a, lo, c0, c1, b - first(c0, lo), it);
+  return set_item<R, FEW>(a, lo, c0, c1, b - first(c0, lo), it);
 }
 
 // The sum of x over the wave.
@@ -270,7 +271,8 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   const int split = rest % a.splits, blk = a.blocks - 1 - rest / a.splits;
   Item it;
   constexpr int ROWS = EX_ROWS / KH;
-  if (!PAGED && a.n <= 64 ? !find_dearest<ROWS>(a, a.blocks - 1 - blk, it) : !find_item<ROWS>(a, blk, it))
+  if (!PAGED && a.n <= 64 ? !find_dearest<ROWS>(a, a.blocks - 1 - blk, it)
+                          : !find_item<ROWS, PAGED == 2 ? 0 : EX_FEW>(a, blk, it))
     return;  // uniform in the workgroup
   int per;
   const int tiles = (it.kend + EX_KEYS - 1) / EX_KEYS;
@@ -1081,12 +1083,12 @@ struct Sum {
 // block), 32 threads per row.  A latency chain: block, references, partials (3 x 20
 // rows over 2500 tokens in float32 5.3 us).
 constexpr int EJ_ROWS = 16;
-template <int FP32, int R>
+template <int FP32, int R, int FEW>
 __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
   const int part = blockIdx.x % (R / EJ_ROWS), rest = blockIdx.x / (R / EJ_ROWS);
   const int kvh = rest % a.Hkv, blk = rest / a.Hkv;
   Item it;
-  if (!find_item<R>(a, blk, it)) return;
+  if (!find_item<R, FEW>(a, blk, it)) return;
   int per;
   const int tiles = (it.kend + (FP32 ? EX_KEYS32 : EX_KEYS) - 1) / (FP32 ? EX_KEYS32 : EX_KEYS);
   const int nsp = ex_splits(a.splits, tiles, per);
@@ -1113,22 +1115,29 @@ __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
 // steps, which is made for thousands of them.  64 requests over 1.07 GB of pages: 198 us, 5.4
 // TB/s; one over 1500 tokens 9.6 us, the chain of its two or three tiles.
 constexpr int FW_W = 4;              // waves per workgroup
+constexpr int FW_KEYS4 = 64;         // keys to a tile of pages of 4 bits
+constexpr int FW_START4 = 1;         // tiles that an item's start and end count as, before its first
 constexpr int FW_VB = 32 * 64 + 64;  // bytes of one 32-dim block of a V tile (64 of padding: bank spread)
 
 // What k_exact_few takes of request i.
 struct Few {
   int s0, add, rows, kv, tiles;  // tiles: one even if its rows see nothing, 0 if it is not that kernel's
 };
+template <int FP4>
 __device__ __forceinline__ Few few_of(const ExactArgs& a, int i) {
   Few r;
   const int c0 = min(max(a.cu[i], 0), a.total), c1 = min(max(a.cu[i + 1], 0), a.total);
   r.s0 = c0;
   r.add = max(c1 - c0, 0);
-  r.rows = (int)min((long long)min(r.add, a.max_add) * a.grp, (long long)EX_FEW + 1);
+  // (total * Hq, and with it a request's rows, are below 2^31)
+  r.rows = FP4 ? min(r.add, a.max_add) * a.grp : (int)min((long long)min(r.add, a.max_add) * a.grp, (long long)EX_FEW + 1);
   r.kv = min(max(a.kv_len[i], 0), a.stride << a.shift);
-  r.tiles = r.rows < 1 || r.rows > EX_FEW ? 0 : max(1, (r.kv + 31) / 32);
+  r.tiles = r.rows < 1 || r.rows > (FP4 ? a.few_limit : EX_FEW) ? 0 : max(1, (r.kv + (FP4 ? FW_KEYS4 : 32) - 1) / (FP4 ? FW_KEYS4 : 32)) + FP4 * FW_START4;
   return r;
 }
+// groups of 32 rows
+template <int FP4>
+__device__ __forceinline__ int groups_of(int rows) { return FP4 ? (rows + EX_FEW - 1) / EX_FEW : 1; }
 __device__ __forceinline__ long long lane_ll(long long x, int l) {
   const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)x, l), hi = __builtin_amdgcn_readlane((int)(x >> 32), l);
   return (long long)((unsigned long long)hi << 32 | lo);
@@ -1148,7 +1157,7 @@ __device__ __forceinline__ long long wave_sum(long long x) {
 // accordingly), V into the wave's LDS; the loads run two tiles ahead.
 template <int FP4>
 __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][(FP4 ? 1 : 2) * 4 * FW_VB];  // the V tile in use and the next
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2 * 4 * FW_VB];  // two V tiles of 32 keys: in use and the next; of one tile of 64
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int w = blockIdx.x * FW_W + wave;
@@ -1156,12 +1165,13 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   int32_t* meta = a.few_meta + w * 4;
   // total tiles and this wave's run: lane l sums the requests of the l-th of 64 blocks
   const int per64 = (a.n + 63) / 64;
-  long long mine = 0;
+  long long mine = 0, items = 0;
   Few q{};
   for (int j = 0; j < per64; ++j) {
     const int i = lane * per64 + j;
-    if (i < a.n) q = few_of(a, i);
-    mine += i < a.n ? q.tiles : 0;
+    if (i < a.n) q = few_of<FP4>(a, i);
+    mine += i < a.n ? (long long)q.tiles * groups_of<FP4>(q.rows) : 0;
+    if (FP4) items += i < a.n && q.tiles ? groups_of<FP4>(q.rows) : 0;
   }
   long long upto = wave_sum(mine);
   const long long N = lane_ll(upto, 63) * a.Hkv;
@@ -1170,7 +1180,11 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   // two waves to a compute unit, since more partials cost more than more loads in
   // flight give (30 000 tokens, 4 kv heads, 2048 waves 32 us, 470 24; 8 x 8000, 7 rows
   // 38 and 31, 32 rows 64 and 35; but 64 x 8000, 2048 waves 203, 512 231)
-  const long long per = max(max((N + waves - 1) / waves, min(16ll, (N + 511) / 512)), 2ll);
+  // Pages of 4 bits: 8 tiles of 64 keys instead, and not where items are of 8 or fewer on average,
+  // which leave few partials (see `alone` below)
+  long long share = min(FP4 ? EX_FEW_RUN4 : 16ll, (N + 511) / 512);
+  if (FP4 && N <= EX_FEW_RUN4 * lane_ll(wave_sum(items), 63) * a.Hkv) share = 1;
+  const long long per = max(max((N + waves - 1) / waves, share), FP4 ? 1ll : 2ll);
   const long long x1 = min(N, (w + 1) * per);
   long long x = w * per;
   if (lane == 0) meta[0] = 0;
@@ -1188,18 +1202,18 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   const int grp16 = lane >> 4, s16 = lane & 15;
   const uint8_t* vl0 = s_mem[wave] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
 
-  // tiles [ta, tb) of request i's kv head kvh; whole: that is all of them
-  auto item = [&](int i, int s0, int add, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
+  // tiles [ta, tb) of request i's kv head kvh, rows r0 .. r0 + rows - 1; whole: that is all of them
+  auto item = [&](int i, int s0, int add, int r0, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
     const int off = kv - add;
     const bool rvalid = m < rows;
-    const int tok = rvalid ? m / a.grp : 0;
-    const int head = kvh * a.grp + (rvalid ? m - tok * a.grp : 0);
+    const int tok = rvalid ? (r0 + m) / a.grp : 0;
+    const int head = kvh * a.grp + (rvalid ? r0 + m - tok * a.grp : 0);
     const size_t orow = (size_t)(s0 + tok) * a.Hq + head;
     const int klim = rvalid ? off + tok : -1;
-    const int ntok = (rows - 1) / a.grp + 1;
-    const int wfull = off + 1;                          // keys that every row sees
+    const int ntok = (r0 + rows - 1) / a.grp + 1;
+    const int wfull = off + r0 / a.grp + 1;             // keys that every row sees
     const int kend = min(max(off + ntok, 0), kv);       // keys that some row sees
-    const int tend = min(tb, (kend + 31) / 32);
+    const int tend = min(tb, (kend + (FP4 ? FW_KEYS4 : 32) - 1) / (FP4 ? FW_KEYS4 : 32));
     const int32_t* row = a.table + (size_t)i * a.stride;
     bf16x8 bq[8];
     {
@@ -1234,117 +1248,170 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
         for (int b = 0; b < 4; ++b) lds_dma16(p + b * 64, s_mem[wave] + buf * (4 * FW_VB) + b * FW_VB + g * 1024);
       }
     };
-    struct Codes {  // a tile of 4 bits: this lane's blocks `half` and 2 + half of its key, and the key's scales
+    auto part_of = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
+    // 4 bits: 32 keys u of a tile, this lane's blocks `half` and 2 + half of its key, and the key's scales
+    struct Codes {
       uint4 k[2], v[2];
       uint32_t ks, vs;
       bool bad;
     };
-    auto load4 = [&](size_t r, Codes& c) {
-      const uint4 *k4 = reinterpret_cast<const uint4*>(kb) + r * 4 + half, *v4 = reinterpret_cast<const uint4*>(vb) + r * 4 + half;
+    auto key4 = [&](int t, int u) { return min(t * FW_KEYS4 + 32 * u + m, kend - 1); };
+    auto id4 = [&](int t, int u) { return row[key4(t, u) >> a.shift]; };
+    auto row4 = [&](int t, int u, int id, Codes& c) {  // of the pages (below 2^32)
+      c.bad = (unsigned)id >= (unsigned)a.num_pages;
+      return (unsigned)((((unsigned)(c.bad ? 0 : id) * a.Hkv + kvh) << a.shift) + (key4(t, u) & ((1 << a.shift) - 1)));
+    };
+    auto load4k = [&](size_t r, Codes& c) {
+      const uint4* k4 = reinterpret_cast<const uint4*>(kb) + r * 4 + half;
       c.ks = reinterpret_cast<const uint32_t*>(a.ksc)[r];
       c.k[0] = k4[0];
       c.k[1] = k4[2];
+    };
+    auto load4v = [&](size_t r, Codes& c) {
+      const uint4* v4 = reinterpret_cast<const uint4*>(vb) + r * 4 + half;
       c.vs = reinterpret_cast<const uint32_t*>(a.vsc)[r];
       c.v[0] = v4[0];
       c.v[1] = v4[2];
     };
-    auto part_of = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
-    // 4 bits: tile t from c, whose registers then take tile t + 2; id: the page of tile t + 2, then of t + 3
-    auto step4 = [&](int t, Codes& c, int& id) {
-      const unsigned badm = (unsigned)__ballot(c.bad);
-      const bool masked = (t + 1) * 32 > wfull || badm != 0;  // uniform
-      // blocks of V that read as NaN: their codes go into the products as zeros, and NaN into the
-      // outputs of the rows that see them (a zero weight times NaN would be one)
-      const bool odd = __ballot((((c.vs & 0x7F7F7F7Fu) + 0x01010101u) & c.vs & 0x80808080u) != 0) != 0;  // uniform
-      unsigned nans[4] = {0, 0, 0, 0};  // keys of each block of 32 dims
-      if (odd) {
-#pragma unroll
-        for (int b = 0; b < 4; ++b) nans[b] = (unsigned)__ballot(((c.vs >> (8 * b)) & 255) == 255);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (((c.vs >> (16 * i + 8 * half)) & 255) == 255) {
-            c.vs &= ~(255u << (16 * i + 8 * half));
-            c.v[i] = make_uint4(0, 0, 0, 0);
-          }
-      }
-      auto scale_of = [&](uint32_t w, int i) { return __uint_as_float(((w >> (16 * i + 8 * half)) & 255) << 23); };
-      f32x16 s = zero;
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, values4(part_of(c.k[kk >> 2], kk & 3), scale_of(c.ks, kk >> 2))), bq[kk], s, 0, 0, 0);
-      uint8_t* vw = s_mem[wave] + half * FW_VB + m * 64;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<uint4*>(vw + 2 * (j >> 2) * FW_VB + (j & 3) * 16) =
-            values4(part_of(c.v[j >> 2], j & 3), scale_of(c.vs, j >> 2));
-      if (t + 2 < tend) {  // uniform
-        const size_t r = (unsigned)row_of(t + 2, id, c.bad);
-        id = id_of(min(t + 3, tend - 1));
-        load4(r, c);
-      }
-      const int rel = klim - t * 32 - 4 * half;
-      const unsigned bm = badm >> (4 * half);
-      if (masked) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          s[j] = 8 * (j >> 2) + (j & 3) > rel || ((bm >> (8 * (j >> 2) + (j & 3))) & 1) ? -INFINITY : s[j];
-      }
-      float tmax = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) tmax = fmaxf(tmax, s[j]);
-      tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
-      const bool grow = tmax > mref + 8.0f;
-      if (__ballot(grow)) {  // uniform
-        const float mnew = grow ? tmax : mref;
-        const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
-        lrun *= alpha;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
-        mref = mnew;
-      }
-      v8i16 vo[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint8_t* p = vl0 + (i >> 1) * FW_VB + (i & 1) * 1024;
-        const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)p);
-        const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(p + 512));
-        vo[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-      bf16x8 pb[2];
-      float part[2] = {0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[j], EX_SCALE, -mref));
-        part[j & 1] += p;
-        pb[j >> 3][j & 7] = (__bf16)p;
-      }
-      lrun += part[0] + part[1];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        oacc[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vo[i]), pb[i & 1], oacc[i >> 1], 0, 0, 0);
-      if (odd) {
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          bool hit = false;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int key = 8 * (j >> 2) + (j & 3);
-            hit |= key <= rel && ((nans[b] & ~badm) >> (4 * half + key)) & 1;
-          }
-          oacc[b] += xor32(hit ? 1 : 0) | hit ? NAN : 0.f;
-        }
-      }
-    };
+    auto scale_of = [&](uint32_t w, int i) { return __uint_as_float(((w >> (16 * i + 8 * half)) & 255) << 23); };
+    // V's place in the wave's LDS: key row m of 64 bytes in each 32-dim block, its four chunks of 16
+    // permuted, chunk j at j ^ (m / 4 % 4), so that 16 rows' writes fall on distinct banks
+    uint8_t* const vw = s_mem[wave] + half * FW_VB + m * 64;
+    const uint8_t* const vr = s_mem[wave] + (4 * half + (s16 >> 2)) * 64 + (s16 & 1) * 8;
+    const int vchunk = (grp16 & 1) * 2 + ((s16 & 3) >> 1);
+    const uint8_t *const vlo = vr + ((vchunk ^ half) * 16), *const vhi = vr + 512 + ((vchunk ^ half ^ 2) * 16);
     if constexpr (FP4) {
       if (ta < tend) {
-        Codes c0, c1;
-        load4((unsigned)row_of(ta, id_of(ta), c0.bad), c0);
-        load4((unsigned)row_of(min(ta + 1, tend - 1), id_of(min(ta + 1, tend - 1)), c1.bad), c1);
-        int id = id_of(min(ta + 2, tend - 1));
-        for (int t = ta; t < tend; t += 2) {
-          step4(t, c0, id);
-          if (t + 1 < tend) step4(t + 1, c1, id);  // uniform
+        Codes c[2];
+        int id[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) id[u] = id4(ta, u);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const unsigned r = row4(ta, u, id[u], c[u]);
+          load4k(r, c[u]);
+          load4v(r, c[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) id[u] = id4(min(ta + 1, tend - 1), u);
+        for (int t = ta; t < tend; ++t) {
+          unsigned badm[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) badm[u] = (unsigned)__ballot(c[u].bad);
+          const bool masked = (t + 1) * FW_KEYS4 > wfull || (badm[0] | badm[1]) != 0;  // uniform
+          // blocks of V that read as NaN: their codes go into the products as zeros, and NaN into the
+          // outputs of the rows that see them (a zero weight times NaN would be one)
+          auto has_nan = [](uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & w & 0x80808080u; };
+          const bool odd = __ballot((has_nan(c[0].vs) | has_nan(c[1].vs)) != 0) != 0;  // uniform
+          unsigned nans[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // keys of each block of 32 dims
+          if (odd) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+              for (int b = 0; b < 4; ++b) nans[u][b] = (unsigned)__ballot(((c[u].vs >> (8 * b)) & 255) == 255) & ~badm[u];
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                if (((c[u].vs >> (16 * i + 8 * half)) & 255) == 255) {
+                  c[u].vs &= ~(255u << (16 * i + 8 * half));
+                  c[u].v[i] = make_uint4(0, 0, 0, 0);
+                }
+            }
+          }
+          f32x16 s[2];
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                  __builtin_bit_cast(bf16x8, values4(part_of(c[u].k[kk >> 2], kk & 3), scale_of(c[u].ks, kk >> 2))), bq[kk],
+                  kk ? s[u] : zero, 0, 0, 0);
+          // the next tile's K goes out once this one's is used, its V likewise
+          const int tn = min(t + 1, tend - 1);  // past the last tile the loads repeat it
+          unsigned next[2];
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            next[u] = row4(tn, u, id[u], c[u]);
+            load4k(next[u], c[u]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              *reinterpret_cast<uint4*>(vw + u * (4 * FW_VB) + 2 * (j >> 2) * FW_VB + (((j & 3) ^ ((m >> 2) & 3)) * 16)) =
+                  values4(part_of(c[u].v[j >> 2], j & 3), scale_of(c[u].vs, j >> 2));
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) load4v(next[u], c[u]);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) id[u] = id4(min(t + 2, tend - 1), u);
+          __builtin_amdgcn_sched_barrier(0);
+          const int rel = klim - t * FW_KEYS4 - 4 * half;
+          if (masked) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const unsigned bm = badm[u] >> (4 * half);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const int key = 8 * (j >> 2) + (j & 3);
+                s[u][j] = 32 * u + key > rel || ((bm >> key) & 1) ? -INFINITY : s[u][j];
+              }
+            }
+          }
+          float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top[u] = fmaxf(top[u], s[u][j]);
+          float tmax = fmaxf(top[0], top[1]);
+          tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
+          const bool grow = tmax > mref + 8.0f;
+          if (__ballot(grow)) {  // uniform
+            const float mnew = grow ? tmax : mref;
+            const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
+            lrun *= alpha;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
+            mref = mnew;
+          }
+          float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            v8i16 vo[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int at = u * (4 * FW_VB) + (i >> 1) * FW_VB + (i & 1) * 1024;
+              const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vlo + at));
+              const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vhi + at));
+              vo[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+            bf16x8 pb[2];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float p = __builtin_amdgcn_exp2f(fmaf(s[u][j], EX_SCALE, -mref));
+              part[j & 3] += p;
+              pb[j >> 3][j & 7] = (__bf16)p;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              oacc[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vo[i]), pb[i & 1], oacc[i >> 1], 0, 0, 0);
+          }
+          lrun += (part[0] + part[1]) + (part[2] + part[3]);
+          if (odd) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              int hit = 0;
+#pragma unroll
+              for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                  const int key = 8 * (j >> 2) + (j & 3);
+                  hit |= 32 * u + key <= rel ? (int)(nans[u][b] >> (4 * half + key)) & 1 : 0;
+                }
+              oacc[b] += (xor32(hit) | hit) ? NAN : 0.f;
+            }
+          }
         }
       }
     } else if (ta < tend) {
@@ -1481,26 +1548,36 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   while (x < x1 && i0 < a.n) {
     if (per64 > 1) {  // else the lanes have them
       q = Few{};
-      if (i0 + lane < a.n) q = few_of(a, i0 + lane);
+      if (i0 + lane < a.n) q = few_of<FP4>(a, i0 + lane);
     }
-    const long long incl = wave_sum(q.tiles), excl = incl - q.tiles;
+    const long long span = (long long)q.tiles * groups_of<FP4>(q.rows), incl = wave_sum(span), excl = incl - span;
     const long long all = before + lane_ll(incl, 63);
     while (x < x1 && x < all * a.Hkv) {
       // the request that x is in: the last one that begins at or before it
       const int r = __builtin_amdgcn_readfirstlane(__popcll(__ballot((before + excl) * a.Hkv <= x)) - 1);
       const int T = __builtin_amdgcn_readlane(q.tiles, r);
       const long long first = (before + lane_ll(excl, r)) * a.Hkv;
-      const int kvh = __builtin_amdgcn_readfirstlane((int)((x - first) / T));
-      const int ta = __builtin_amdgcn_readfirstlane((int)(x - first - (long long)kvh * T));
-      const int tb = __builtin_amdgcn_readfirstlane((int)min((long long)T, ta + (x1 - x)));
-      item(i0 + r, __builtin_amdgcn_readlane(q.s0, r), __builtin_amdgcn_readlane(q.add, r),
-           __builtin_amdgcn_readlane(q.rows, r), __builtin_amdgcn_readlane(q.kv, r), kvh, ta, tb, ta == 0 && tb == T,
-           ta == 0);
+      // its kv heads one after the other, the groups of rows of each, their tiles
+      const int rows = __builtin_amdgcn_readlane(q.rows, r), groups = groups_of<FP4>(rows);
+      const long long at = (x - first) / T;
+      const int kvh = __builtin_amdgcn_readfirstlane((int)(FP4 ? at / groups : at));
+      const int r0 = FP4 ? __builtin_amdgcn_readfirstlane((int)(at - (long long)kvh * groups)) * EX_FEW : 0;
+      const int mine = FP4 ? min(rows - r0, EX_FEW) : rows;
+      const int ta = __builtin_amdgcn_readfirstlane((int)(x - first - at * T));
+      // FP4: an item of half a run or less, or of four tiles, is its first tile's wave's
+      // alone, so that many short items leave no partials
+      const bool alone = FP4 && (2 * T <= per || T <= 4 + FW_START4);  // uniform
+      const int tb = __builtin_amdgcn_readfirstlane(alone ? T : (int)min((long long)T, ta + (x1 - x)));
+      if (alone && ta > 0) {
+        x += T - ta;
+        continue;
+      }
+      item(i0 + r, __builtin_amdgcn_readlane(q.s0, r), __builtin_amdgcn_readlane(q.add, r), r0, mine,
+           __builtin_amdgcn_readlane(q.kv, r), kvh, max(ta - FP4 * FW_START4, 0), tb - FP4 * FW_START4, ta == 0 && tb == T, ta == 0);
       if (ta == 0 && tb < T && lane == 0) {
-        // its rows, kv head, the wave that it ends in, its first row of q
-        *reinterpret_cast<int4*>(meta) = make_int4(__builtin_amdgcn_readlane(q.rows, r), kvh,
-                                                   (int)((first + (long long)(kvh + 1) * T - 1) / per),
-                                                   __builtin_amdgcn_readlane(q.s0, r));
+        // its rows and their group, kv head, the wave that it ends in, its first row of q
+        *reinterpret_cast<int4*>(meta) = make_int4(mine | (int)((unsigned)(r0 / EX_FEW) << 6), kvh,
+                                                   (int)((first + (at + 1) * T - 1) / per), __builtin_amdgcn_readlane(q.s0, r));
       }
       x += tb - ta;
     }
@@ -1532,7 +1609,7 @@ __global__ __launch_bounds__(FJ_W * 64) void k_exact_few_join(ExactArgs a, int w
   int at = 0;  // rows given out to the waves so far
 #pragma unroll
   for (int e = 0; e < FJ_W; ++e) {
-    const int rows = meta[e].x, kvh = meta[e].y, w = w0 + e, count = meta[e].z - w + 1, s0 = meta[e].w;
+    const int rows = meta[e].x & 63, r0 = (int)((unsigned)meta[e].x >> 6) * EX_FEW, kvh = meta[e].y, w = w0 + e, count = meta[e].z - w + 1, s0 = meta[e].w;
     const bool many = count > FJ_MANY;
     for (int r = y; r < rows; r += ny) {  // uniform
       if (!many && (at++ & (FJ_W - 1)) != wave) continue;
@@ -1557,8 +1634,8 @@ __global__ __launch_bounds__(FJ_W * 64) void k_exact_few_join(ExactArgs a, int w
 #pragma unroll
         for (int k = 1; k < FJ_W; ++k) s.add(s_l[k][0], s_l[k][1], s_o[k][d4]);
       }
-      const int tok = r / a.grp;
-      if (g == 0) s.store<0>(a, (size_t)(s0 + tok) * a.Hq + kvh * a.grp + (r - tok * a.grp), d4);
+      const int tok = (r0 + r) / a.grp;
+      if (g == 0) s.store<0>(a, (size_t)(s0 + tok) * a.Hq + kvh * a.grp + (r0 + r - tok * a.grp), d4);
     }
   }
 }
@@ -1595,9 +1672,12 @@ hipError_t launch_exact(const ExactArgs& a, bool fp32, Keys keys, hipStream_t st
   }
   if (a.splits > 1) {
     const dim3 joins(a.Hkv * a.blocks * (a.rows / EJ_ROWS)), threads(EJ_ROWS * 32);
-    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), joins, threads, 0, st, a);
-    else if (a.rows == EX_ROWS) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), joins, threads, 0, st, a);
-    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2>), joins, threads, 0, st, a);
+    const bool four = keys == Keys::PAGES4;
+    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32, EX_FEW>), joins, threads, 0, st, a);
+    else if (a.rows == EX_ROWS && four) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS, 0>), joins, threads, 0, st, a);
+    else if (a.rows == EX_ROWS) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS, EX_FEW>), joins, threads, 0, st, a);
+    else if (four) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2, 0>), joins, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2, EX_FEW>), joins, threads, 0, st, a);
   }
   return hipGetLastError();
 }
