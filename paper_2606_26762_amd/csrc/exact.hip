@@ -1115,29 +1115,22 @@ __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
 // steps, which is made for thousands of them.  64 requests over 1.07 GB of pages: 198 us, 5.4
 // TB/s; one over 1500 tokens 9.6 us, the chain of its two or three tiles.
 constexpr int FW_W = 4;              // waves per workgroup
-constexpr int FW_KEYS4 = 64;         // keys to a tile of pages of 4 bits
-constexpr int FW_START4 = 1;         // tiles that an item's start and end count as, before its first
 constexpr int FW_VB = 32 * 64 + 64;  // bytes of one 32-dim block of a V tile (64 of padding: bank spread)
 
 // What k_exact_few takes of request i.
 struct Few {
   int s0, add, rows, kv, tiles;  // tiles: one even if its rows see nothing, 0 if it is not that kernel's
 };
-template <int FP4>
 __device__ __forceinline__ Few few_of(const ExactArgs& a, int i) {
   Few r;
   const int c0 = min(max(a.cu[i], 0), a.total), c1 = min(max(a.cu[i + 1], 0), a.total);
   r.s0 = c0;
   r.add = max(c1 - c0, 0);
-  // (total * Hq, and with it a request's rows, are below 2^31)
-  r.rows = FP4 ? min(r.add, a.max_add) * a.grp : (int)min((long long)min(r.add, a.max_add) * a.grp, (long long)EX_FEW + 1);
+  r.rows = (int)min((long long)min(r.add, a.max_add) * a.grp, (long long)EX_FEW + 1);
   r.kv = min(max(a.kv_len[i], 0), a.stride << a.shift);
-  r.tiles = r.rows < 1 || r.rows > (FP4 ? a.few_limit : EX_FEW) ? 0 : max(1, (r.kv + (FP4 ? FW_KEYS4 : 32) - 1) / (FP4 ? FW_KEYS4 : 32)) + FP4 * FW_START4;
+  r.tiles = r.rows < 1 || r.rows > EX_FEW ? 0 : max(1, (r.kv + 31) / 32);
   return r;
 }
-// groups of 32 rows
-template <int FP4>
-__device__ __forceinline__ int groups_of(int rows) { return FP4 ? (rows + EX_FEW - 1) / EX_FEW : 1; }
 __device__ __forceinline__ long long lane_ll(long long x, int l) {
   const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)x, l), hi = __builtin_amdgcn_readlane((int)(x >> 32), l);
   return (long long)((unsigned long long)hi << 32 | lo);
@@ -1152,12 +1145,8 @@ __device__ __forceinline__ long long wave_sum(long long x) {
   }
   return x;
 }
-// FP4: pages of 4 bits.  Lane (m, h) loads the blocks h and 2 + h of 32 dims of key m's row of K
-// and of V and turns them to bfloat16, K into the operand (the query's dims lie
-// accordingly), V into the wave's LDS; the loads run two tiles ahead.
-template <int FP4>
 __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2 * 4 * FW_VB];  // two V tiles of 32 keys: in use and the next; of one tile of 64
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2][4 * FW_VB];  // the V tile in use and the next
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int w = blockIdx.x * FW_W + wave;
@@ -1165,13 +1154,12 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   int32_t* meta = a.few_meta + w * 4;
   // total tiles and this wave's run: lane l sums the requests of the l-th of 64 blocks
   const int per64 = (a.n + 63) / 64;
-  long long mine = 0, items = 0;
+  long long mine = 0;
   Few q{};
   for (int j = 0; j < per64; ++j) {
     const int i = lane * per64 + j;
-    if (i < a.n) q = few_of<FP4>(a, i);
-    mine += i < a.n ? (long long)q.tiles * groups_of<FP4>(q.rows) : 0;
-    if (FP4) items += i < a.n && q.tiles ? groups_of<FP4>(q.rows) : 0;
+    if (i < a.n) q = few_of(a, i);
+    mine += i < a.n ? q.tiles : 0;
   }
   long long upto = wave_sum(mine);
   const long long N = lane_ll(upto, 63) * a.Hkv;
@@ -1180,11 +1168,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   // two waves to a compute unit, since more partials cost more than more loads in
   // flight give (30 000 tokens, 4 kv heads, 2048 waves 32 us, 470 24; 8 x 8000, 7 rows
   // 38 and 31, 32 rows 64 and 35; but 64 x 8000, 2048 waves 203, 512 231)
-  // Pages of 4 bits: 8 tiles of 64 keys instead, and not where items are of 8 or fewer on average,
-  // which leave few partials (see `alone` below)
-  long long share = min(FP4 ? EX_FEW_RUN4 : 16ll, (N + 511) / 512);
-  if (FP4 && N <= EX_FEW_RUN4 * lane_ll(wave_sum(items), 63) * a.Hkv) share = 1;
-  const long long per = max(max((N + waves - 1) / waves, share), FP4 ? 1ll : 2ll);
+  const long long per = max(max((N + waves - 1) / waves, min(16ll, (N + 511) / 512)), 2ll);
   const long long x1 = min(N, (w + 1) * per);
   long long x = w * per;
   if (lane == 0) meta[0] = 0;
@@ -1200,27 +1184,26 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   const uint8_t* vb = (const uint8_t*)a.v;
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const int grp16 = lane >> 4, s16 = lane & 15;
-  const uint8_t* vl0 = s_mem[wave] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
+  const uint8_t* vl0 = s_mem[wave][0] + (4 * half + (s16 >> 2)) * 64 + (grp16 & 1) * 32 + (s16 & 3) * 8;
 
-  // tiles [ta, tb) of request i's kv head kvh, rows r0 .. r0 + rows - 1; whole: that is all of them
-  auto item = [&](int i, int s0, int add, int r0, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
+  // tiles [ta, tb) of request i's kv head kvh; whole: that is all of them
+  auto item = [&](int i, int s0, int add, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
     const int off = kv - add;
     const bool rvalid = m < rows;
-    const int tok = rvalid ? (r0 + m) / a.grp : 0;
-    const int head = kvh * a.grp + (rvalid ? r0 + m - tok * a.grp : 0);
+    const int tok = rvalid ? m / a.grp : 0;
+    const int head = kvh * a.grp + (rvalid ? m - tok * a.grp : 0);
     const size_t orow = (size_t)(s0 + tok) * a.Hq + head;
     const int klim = rvalid ? off + tok : -1;
-    const int ntok = (r0 + rows - 1) / a.grp + 1;
-    const int wfull = off + r0 / a.grp + 1;             // keys that every row sees
+    const int ntok = (rows - 1) / a.grp + 1;
+    const int wfull = off + 1;                          // keys that every row sees
     const int kend = min(max(off + ntok, 0), kv);       // keys that some row sees
-    const int tend = min(tb, (kend + (FP4 ? FW_KEYS4 : 32) - 1) / (FP4 ? FW_KEYS4 : 32));
+    const int tend = min(tb, (kend + 31) / 32);
     const int32_t* row = a.table + (size_t)i * a.stride;
     bf16x8 bq[8];
     {
       const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(s0 + tok) * a.qs + head * (D * 2));
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk)
-        bq[kk] = __builtin_bit_cast(bf16x8, qr[FP4 ? 8 * (kk >> 2) + 4 * half + (kk & 3) : 2 * kk + half]);
+      for (int kk = 0; kk < 8; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[2 * kk + half]);
     }
     f32x16 oacc[4] = {zero, zero, zero, zero};
     float mref = EX_NONE, lrun = 0.f;
@@ -1245,176 +1228,10 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
         const unsigned r = __builtin_amdgcn_ds_bpermute(64 * g + (lane & ~3), rw);
         const uint8_t* p = vb + (size_t)r * (D * 2) + (lane & 3) * 16;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) lds_dma16(p + b * 64, s_mem[wave] + buf * (4 * FW_VB) + b * FW_VB + g * 1024);
+        for (int b = 0; b < 4; ++b) lds_dma16(p + b * 64, s_mem[wave][buf] + b * FW_VB + g * 1024);
       }
     };
-    auto part_of = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
-    // 4 bits: 32 keys u of a tile, this lane's blocks `half` and 2 + half of its key, and the key's scales
-    struct Codes {
-      uint4 k[2], v[2];
-      uint32_t ks, vs;
-      bool bad;
-    };
-    auto key4 = [&](int t, int u) { return min(t * FW_KEYS4 + 32 * u + m, kend - 1); };
-    auto id4 = [&](int t, int u) { return row[key4(t, u) >> a.shift]; };
-    auto row4 = [&](int t, int u, int id, Codes& c) {  // of the pages (below 2^32)
-      c.bad = (unsigned)id >= (unsigned)a.num_pages;
-      return (unsigned)((((unsigned)(c.bad ? 0 : id) * a.Hkv + kvh) << a.shift) + (key4(t, u) & ((1 << a.shift) - 1)));
-    };
-    auto load4k = [&](size_t r, Codes& c) {
-      const uint4* k4 = reinterpret_cast<const uint4*>(kb) + r * 4 + half;
-      c.ks = reinterpret_cast<const uint32_t*>(a.ksc)[r];
-      c.k[0] = k4[0];
-      c.k[1] = k4[2];
-    };
-    auto load4v = [&](size_t r, Codes& c) {
-      const uint4* v4 = reinterpret_cast<const uint4*>(vb) + r * 4 + half;
-      c.vs = reinterpret_cast<const uint32_t*>(a.vsc)[r];
-      c.v[0] = v4[0];
-      c.v[1] = v4[2];
-    };
-    auto scale_of = [&](uint32_t w, int i) { return __uint_as_float(((w >> (16 * i + 8 * half)) & 255) << 23); };
-    // V's place in the wave's LDS: key row m of 64 bytes in each 32-dim block, its four chunks of 16
-    // permuted, chunk j at j ^ (m / 4 % 4), so that 16 rows' writes fall on distinct banks
-    uint8_t* const vw = s_mem[wave] + half * FW_VB + m * 64;
-    const uint8_t* const vr = s_mem[wave] + (4 * half + (s16 >> 2)) * 64 + (s16 & 1) * 8;
-    const int vchunk = (grp16 & 1) * 2 + ((s16 & 3) >> 1);
-    const uint8_t *const vlo = vr + ((vchunk ^ half) * 16), *const vhi = vr + 512 + ((vchunk ^ half ^ 2) * 16);
-    if constexpr (FP4) {
-      if (ta < tend) {
-        Codes c[2];
-        int id[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) id[u] = id4(ta, u);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const unsigned r = row4(ta, u, id[u], c[u]);
-          load4k(r, c[u]);
-          load4v(r, c[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) id[u] = id4(min(ta + 1, tend - 1), u);
-        for (int t = ta; t < tend; ++t) {
-          unsigned badm[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) badm[u] = (unsigned)__ballot(c[u].bad);
-          const bool masked = (t + 1) * FW_KEYS4 > wfull || (badm[0] | badm[1]) != 0;  // uniform
-          // blocks of V that read as NaN: their codes go into the products as zeros, and NaN into the
-          // outputs of the rows that see them (a zero weight times NaN would be one)
-          auto has_nan = [](uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & w & 0x80808080u; };
-          const bool odd = __ballot((has_nan(c[0].vs) | has_nan(c[1].vs)) != 0) != 0;  // uniform
-          unsigned nans[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // keys of each block of 32 dims
-          if (odd) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-#pragma unroll
-              for (int b = 0; b < 4; ++b) nans[u][b] = (unsigned)__ballot(((c[u].vs >> (8 * b)) & 255) == 255) & ~badm[u];
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-                if (((c[u].vs >> (16 * i + 8 * half)) & 255) == 255) {
-                  c[u].vs &= ~(255u << (16 * i + 8 * half));
-                  c[u].v[i] = make_uint4(0, 0, 0, 0);
-                }
-            }
-          }
-          f32x16 s[2];
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-              s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                  __builtin_bit_cast(bf16x8, values4(part_of(c[u].k[kk >> 2], kk & 3), scale_of(c[u].ks, kk >> 2))), bq[kk],
-                  kk ? s[u] : zero, 0, 0, 0);
-          // the next tile's K goes out once this one's is used, its V likewise
-          const int tn = min(t + 1, tend - 1);  // past the last tile the loads repeat it
-          unsigned next[2];
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            next[u] = row4(tn, u, id[u], c[u]);
-            load4k(next[u], c[u]);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<uint4*>(vw + u * (4 * FW_VB) + 2 * (j >> 2) * FW_VB + (((j & 3) ^ ((m >> 2) & 3)) * 16)) =
-                  values4(part_of(c[u].v[j >> 2], j & 3), scale_of(c[u].vs, j >> 2));
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int u = 0; u < 2; ++u) load4v(next[u], c[u]);
-#pragma unroll
-          for (int u = 0; u < 2; ++u) id[u] = id4(min(t + 2, tend - 1), u);
-          __builtin_amdgcn_sched_barrier(0);
-          const int rel = klim - t * FW_KEYS4 - 4 * half;
-          if (masked) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const unsigned bm = badm[u] >> (4 * half);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const int key = 8 * (j >> 2) + (j & 3);
-                s[u][j] = 32 * u + key > rel || ((bm >> key) & 1) ? -INFINITY : s[u][j];
-              }
-            }
-          }
-          float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) top[u] = fmaxf(top[u], s[u][j]);
-          float tmax = fmaxf(top[0], top[1]);
-          tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
-          const bool grow = tmax > mref + 8.0f;
-          if (__ballot(grow)) {  // uniform
-            const float mnew = grow ? tmax : mref;
-            const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
-            lrun *= alpha;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
-            mref = mnew;
-          }
-          float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            v8i16 vo[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int at = u * (4 * FW_VB) + (i >> 1) * FW_VB + (i & 1) * 1024;
-              const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vlo + at));
-              const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vhi + at));
-              vo[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            }
-            bf16x8 pb[2];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float p = __builtin_amdgcn_exp2f(fmaf(s[u][j], EX_SCALE, -mref));
-              part[j & 3] += p;
-              pb[j >> 3][j & 7] = (__bf16)p;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              oacc[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vo[i]), pb[i & 1], oacc[i >> 1], 0, 0, 0);
-          }
-          lrun += (part[0] + part[1]) + (part[2] + part[3]);
-          if (odd) {
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              int hit = 0;
-#pragma unroll
-              for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                  const int key = 8 * (j >> 2) + (j & 3);
-                  hit |= 32 * u + key <= rel ? (int)(nans[u][b] >> (4 * half + key)) & 1 : 0;
-                }
-              oacc[b] += (xor32(hit) | hit) ? NAN : 0.f;
-            }
-          }
-        }
-      }
-    } else if (ta < tend) {
+    if (ta < tend) {
       u16x8 kr[8];
       bool bad;
       int rw = row_of(ta, id_of(ta), bad);
@@ -1548,9 +1365,95 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
   while (x < x1 && i0 < a.n) {
     if (per64 > 1) {  // else the lanes have them
       q = Few{};
-      if (i0 + lane < a.n) q = few_of<FP4>(a, i0 + lane);
+      if (i0 + lane < a.n) q = few_of(a, i0 + lane);
     }
-    const long long span = (long long)q.tiles * groups_of<FP4>(q.rows), incl = wave_sum(span), excl = incl - span;
+    const long long incl = wave_sum(q.tiles), excl = incl - q.tiles;
+    const long long all = before + lane_ll(incl, 63);
+    while (x < x1 && x < all * a.Hkv) {
+      // the request that x is in: the last one that begins at or before it
+      const int r = __builtin_amdgcn_readfirstlane(__popcll(__ballot((before + excl) * a.Hkv <= x)) - 1);
+      const int T = __builtin_amdgcn_readlane(q.tiles, r);
+      const long long first = (before + lane_ll(excl, r)) * a.Hkv;
+      const int kvh = __builtin_amdgcn_readfirstlane((int)((x - first) / T));
+      const int ta = __builtin_amdgcn_readfirstlane((int)(x - first - (long long)kvh * T));
+      const int tb = __builtin_amdgcn_readfirstlane((int)min((long long)T, ta + (x1 - x)));
+      item(i0 + r, __builtin_amdgcn_readlane(q.s0, r), __builtin_amdgcn_readlane(q.add, r),
+           __builtin_amdgcn_readlane(q.rows, r), __builtin_amdgcn_readlane(q.kv, r), kvh, ta, tb, ta == 0 && tb == T,
+           ta == 0);
+      if (ta == 0 && tb < T && lane == 0) {
+        // its rows, kv head, the wave that it ends in, its first row of q
+        *reinterpret_cast<int4*>(meta) = make_int4(__builtin_amdgcn_readlane(q.rows, r), kvh,
+                                                   (int)((first + (long long)(kvh + 1) * T - 1) / per),
+                                                   __builtin_amdgcn_readlane(q.s0, r));
+      }
+      x += tb - ta;
+    }
+    before = all;
+    i0 += 64;
+  }
+}
+
+constexpr int FW_KEYS4 = 64;  // keys to a tile of pages of 4 bits
+constexpr int FW_START4 = 1;  // tiles that an item's start and end count as, before its first
+
+// What the kernels over pages of 4 bits take of request i, which may have more rows.
+__device__ __forceinline__ Few few4_of(const ExactArgs& a, int i) {
+  Few r;
+  const int c0 = min(max(a.cu[i], 0), a.total), c1 = min(max(a.cu[i + 1], 0), a.total);
+  r.s0 = c0;
+  r.add = max(c1 - c0, 0);
+  r.rows = min(r.add, a.max_add) * a.grp;  // (total * Hq is below 2^31)
+  r.kv = min(max(a.kv_len[i], 0), a.stride << a.shift);
+  r.tiles = r.rows < 1 || r.rows > a.few_limit ? 0 : max(1, (r.kv + FW_KEYS4 - 1) / FW_KEYS4) + FW_START4;
+  return r;
+}
+__device__ __forceinline__ int groups_of(int rows) { return (rows + EX_FEW - 1) / EX_FEW; }  // of 32 rows
+
+// Wave w's run of the tiles: item(i, s0, add, r0, rows, kv, kvh, ta, tb, whole, slot) for tiles
+// [ta, tb) of request i's kv head kvh, rows r0 .. r0 + rows - 1; whole: those are all of the item's.
+// Items are (request, kv head, group of 32 rows), their tiles of 64 keys; runs, partials and notes as in
+// k_exact_few.
+template <typename ITEM>
+__device__ __forceinline__ void few4_runs(const ExactArgs& a, int w, ITEM item) {
+  const int lane = threadIdx.x & 63;
+  int32_t* meta = a.few_meta + w * 4;
+  // total tiles and this wave's run: lane l sums the requests of the l-th of 64 blocks
+  const int per64 = (a.n + 63) / 64;
+  long long mine = 0, items = 0;
+  Few q{};
+  for (int j = 0; j < per64; ++j) {
+    const int i = lane * per64 + j;
+    if (i < a.n) q = few4_of(a, i);
+    mine += i < a.n ? (long long)q.tiles * groups_of(q.rows) : 0;
+    items += i < a.n && q.tiles ? groups_of(q.rows) : 0;
+  }
+  long long upto = wave_sum(mine);
+  const long long N = lane_ll(upto, 63) * a.Hkv;
+  const long long waves = (long long)gridDim.x * FW_W;
+  // tiles of a run: as long as EX_FEW_RUN4 are not reached as many as leave two waves to a
+  // compute unit, since more partials cost more than more loads in flight give (up to 8 tiles: one
+  // token over 130 000, 8 kv heads, 39 us, 64 over 125 to 8000 34; up to 16: 37 and 41), but where items
+  // are of 8 or fewer on average, which leave few partials (see `alone` below)
+  long long share = min((long long)EX_FEW_RUN4, (N + 511) / 512);
+  if (N <= EX_FEW_RUN4 * lane_ll(wave_sum(items), 63) * a.Hkv) share = 1;
+  const long long per = max((N + waves - 1) / waves, share);
+  const long long x1 = min(N, (w + 1) * per);
+  long long x = w * per;
+  if (lane == 0) meta[0] = 0;
+  if (x >= N) return;  // uniform, and nothing below synchronises waves
+  int i0 = 0;            // first request of the 64 in the lanes
+  long long before = 0;  // tiles before it
+  if (per64 > 1) {
+    const int l = __builtin_amdgcn_readfirstlane(__popcll(__ballot((upto - mine) * a.Hkv <= x)) - 1);
+    i0 = l * per64;
+    before = lane_ll(upto - mine, l);
+  }
+  while (x < x1 && i0 < a.n) {
+    if (per64 > 1) {  // else the lanes have them
+      q = Few{};
+      if (i0 + lane < a.n) q = few4_of(a, i0 + lane);
+    }
+    const long long span = (long long)q.tiles * groups_of(q.rows), incl = wave_sum(span), excl = incl - span;
     const long long all = before + lane_ll(incl, 63);
     while (x < x1 && x < all * a.Hkv) {
       // the request that x is in: the last one that begins at or before it
@@ -1558,22 +1461,22 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
       const int T = __builtin_amdgcn_readlane(q.tiles, r);
       const long long first = (before + lane_ll(excl, r)) * a.Hkv;
       // its kv heads one after the other, the groups of rows of each, their tiles
-      const int rows = __builtin_amdgcn_readlane(q.rows, r), groups = groups_of<FP4>(rows);
+      const int rows = __builtin_amdgcn_readlane(q.rows, r), groups = groups_of(rows);
       const long long at = (x - first) / T;
-      const int kvh = __builtin_amdgcn_readfirstlane((int)(FP4 ? at / groups : at));
-      const int r0 = FP4 ? __builtin_amdgcn_readfirstlane((int)(at - (long long)kvh * groups)) * EX_FEW : 0;
-      const int mine = FP4 ? min(rows - r0, EX_FEW) : rows;
+      const int kvh = __builtin_amdgcn_readfirstlane((int)(at / groups));
+      const int r0 = __builtin_amdgcn_readfirstlane((int)(at - (long long)kvh * groups)) * EX_FEW;
+      const int mine = min(rows - r0, EX_FEW);
       const int ta = __builtin_amdgcn_readfirstlane((int)(x - first - at * T));
-      // FP4: an item of half a run or less, or of four tiles, is its first tile's wave's
+      // an item of half a run or less, or of four tiles, is its first tile's wave's
       // alone, so that many short items leave no partials
-      const bool alone = FP4 && (2 * T <= per || T <= 4 + FW_START4);  // uniform
+      const bool alone = 2 * T <= per || T <= 4 + FW_START4;  // uniform
       const int tb = __builtin_amdgcn_readfirstlane(alone ? T : (int)min((long long)T, ta + (x1 - x)));
       if (alone && ta > 0) {
         x += T - ta;
         continue;
       }
       item(i0 + r, __builtin_amdgcn_readlane(q.s0, r), __builtin_amdgcn_readlane(q.add, r), r0, mine,
-           __builtin_amdgcn_readlane(q.kv, r), kvh, max(ta - FP4 * FW_START4, 0), tb - FP4 * FW_START4, ta == 0 && tb == T, ta == 0);
+           __builtin_amdgcn_readlane(q.kv, r), kvh, max(ta - FW_START4, 0), tb - FW_START4, ta == 0 && tb == T, ta == 0);
       if (ta == 0 && tb < T && lane == 0) {
         // its rows and their group, kv head, the wave that it ends in, its first row of q
         *reinterpret_cast<int4*>(meta) = make_int4(mine | (int)((unsigned)(r0 / EX_FEW) << 6), kvh,
@@ -1584,6 +1487,443 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few(ExactArgs a) {
     before = all;
     i0 += 64;
   }
+}
+
+// Pages of 4 bits, groups of 32 rows.  Lane (m, h) loads the blocks h and 2 + h of 32 dims of key
+// m's row of K and of V and turns them to bfloat16, K into the operand (the query's dims lie
+// accordingly), V into the wave's LDS; a tile's loads go out once the one before is used.
+__global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2 * 4 * FW_VB];  // V of a tile, by its halves of 32 keys
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int w = blockIdx.x * FW_W + wave;
+  const int m = lane & 31, half = lane >> 5;
+  const uint8_t* kb = (const uint8_t*)a.k;
+  const uint8_t* vb = (const uint8_t*)a.v;
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int grp16 = lane >> 4, s16 = lane & 15;
+
+  // tiles [ta, tb) of request i's kv head kvh, rows r0 .. r0 + rows - 1; whole: that is all of them
+  auto item = [&](int i, int s0, int add, int r0, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
+    const int off = kv - add;
+    const bool rvalid = m < rows;
+    const int tok = rvalid ? (r0 + m) / a.grp : 0;
+    const int head = kvh * a.grp + (rvalid ? r0 + m - tok * a.grp : 0);
+    const size_t orow = (size_t)(s0 + tok) * a.Hq + head;
+    const int klim = rvalid ? off + tok : -1;
+    const int ntok = (r0 + rows - 1) / a.grp + 1;
+    const int wfull = off + r0 / a.grp + 1;             // keys that every row sees
+    const int kend = min(max(off + ntok, 0), kv);       // keys that some row sees
+    const int tend = min(tb, (kend + FW_KEYS4 - 1) / FW_KEYS4);
+    const int32_t* row = a.table + (size_t)i * a.stride;
+    bf16x8 bq[8];
+    {
+      const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(s0 + tok) * a.qs + head * (D * 2));
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+        bq[kk] = __builtin_bit_cast(bf16x8, qr[8 * (kk >> 2) + 4 * half + (kk & 3)]);
+    }
+    f32x16 oacc[4] = {zero, zero, zero, zero};
+    float mref = EX_NONE, lrun = 0.f;
+    auto part_of = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
+    // 4 bits: 32 keys u of a tile, this lane's blocks `half` and 2 + half of its key, and the key's scales
+    struct Codes {
+      uint4 k[2], v[2];
+      uint32_t ks, vs;
+      bool bad;
+    };
+    auto key4 = [&](int t, int u) { return min(t * FW_KEYS4 + 32 * u + m, kend - 1); };
+    auto id4 = [&](int t, int u) { return row[key4(t, u) >> a.shift]; };
+    auto row4 = [&](int t, int u, int id, Codes& c) {  // of the pages (below 2^32)
+      c.bad = (unsigned)id >= (unsigned)a.num_pages;
+      return (unsigned)((((unsigned)(c.bad ? 0 : id) * a.Hkv + kvh) << a.shift) + (key4(t, u) & ((1 << a.shift) - 1)));
+    };
+    auto load4k = [&](size_t r, Codes& c) {
+      const uint4* k4 = reinterpret_cast<const uint4*>(kb) + r * 4 + half;
+      c.ks = reinterpret_cast<const uint32_t*>(a.ksc)[r];
+      c.k[0] = k4[0];
+      c.k[1] = k4[2];
+    };
+    auto load4v = [&](size_t r, Codes& c) {
+      const uint4* v4 = reinterpret_cast<const uint4*>(vb) + r * 4 + half;
+      c.vs = reinterpret_cast<const uint32_t*>(a.vsc)[r];
+      c.v[0] = v4[0];
+      c.v[1] = v4[2];
+    };
+    auto scale_of = [&](uint32_t w, int i) { return __uint_as_float(((w >> (16 * i + 8 * half)) & 255) << 23); };
+    // V's place in the wave's LDS: key row m of 64 bytes in each 32-dim block, its four chunks of 16
+    // permuted, chunk j at j ^ (m / 4 % 4), so that 16 rows' writes fall on distinct banks
+    uint8_t* const vw = s_mem[wave] + half * FW_VB + m * 64;
+    const uint8_t* const vr = s_mem[wave] + (4 * half + (s16 >> 2)) * 64 + (s16 & 1) * 8;
+    const int vchunk = (grp16 & 1) * 2 + ((s16 & 3) >> 1);
+    const uint8_t *const vlo = vr + ((vchunk ^ half) * 16), *const vhi = vr + 512 + ((vchunk ^ half ^ 2) * 16);
+    if (ta < tend) {
+      Codes c[2];
+      int id[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) id[u] = id4(ta, u);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const unsigned r = row4(ta, u, id[u], c[u]);
+        load4k(r, c[u]);
+        load4v(r, c[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) id[u] = id4(min(ta + 1, tend - 1), u);
+      for (int t = ta; t < tend; ++t) {
+        unsigned badm[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) badm[u] = (unsigned)__ballot(c[u].bad);
+        const bool masked = (t + 1) * FW_KEYS4 > wfull || (badm[0] | badm[1]) != 0;  // uniform
+        // blocks of V that read as NaN: their codes go into the products as zeros, and NaN into the
+        // outputs of the rows that see them (a zero weight times NaN would be one)
+        auto has_nan = [](uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & w & 0x80808080u; };
+        const bool odd = __ballot((has_nan(c[0].vs) | has_nan(c[1].vs)) != 0) != 0;  // uniform
+        unsigned nans[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // keys of each block of 32 dims
+        if (odd) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) nans[u][b] = (unsigned)__ballot(((c[u].vs >> (8 * b)) & 255) == 255) & ~badm[u];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              if (((c[u].vs >> (16 * i + 8 * half)) & 255) == 255) {
+                c[u].vs &= ~(255u << (16 * i + 8 * half));
+                c[u].v[i] = make_uint4(0, 0, 0, 0);
+              }
+          }
+        }
+        f32x16 s[2];
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(bf16x8, values4(part_of(c[u].k[kk >> 2], kk & 3), scale_of(c[u].ks, kk >> 2))), bq[kk],
+                kk ? s[u] : zero, 0, 0, 0);
+        // the next tile's K goes out once this one's is used, its V likewise
+        const int tn = min(t + 1, tend - 1);  // past the last tile the loads repeat it
+        unsigned next[2];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          next[u] = row4(tn, u, id[u], c[u]);
+          load4k(next[u], c[u]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint4*>(vw + u * (4 * FW_VB) + 2 * (j >> 2) * FW_VB + (((j & 3) ^ ((m >> 2) & 3)) * 16)) =
+                values4(part_of(c[u].v[j >> 2], j & 3), scale_of(c[u].vs, j >> 2));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) load4v(next[u], c[u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) id[u] = id4(min(t + 2, tend - 1), u);
+        __builtin_amdgcn_sched_barrier(0);
+        const int rel = klim - t * FW_KEYS4 - 4 * half;
+        if (masked) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const unsigned bm = badm[u] >> (4 * half);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int key = 8 * (j >> 2) + (j & 3);
+              s[u][j] = 32 * u + key > rel || ((bm >> key) & 1) ? -INFINITY : s[u][j];
+            }
+          }
+        }
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) top[u] = fmaxf(top[u], s[u][j]);
+        float tmax = fmaxf(top[0], top[1]);
+        tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
+        const bool grow = tmax > mref + 8.0f;
+        if (__ballot(grow)) {  // uniform
+          const float mnew = grow ? tmax : mref;
+          const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
+          lrun *= alpha;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
+          mref = mnew;
+        }
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          v8i16 vo[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int at = u * (4 * FW_VB) + (i >> 1) * FW_VB + (i & 1) * 1024;
+            const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vlo + at));
+            const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vhi + at));
+            vo[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          }
+          bf16x8 pb[2];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[u][j], EX_SCALE, -mref));
+            part[j & 3] += p;
+            pb[j >> 3][j & 7] = (__bf16)p;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            oacc[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vo[i]), pb[i & 1], oacc[i >> 1], 0, 0, 0);
+        }
+        lrun += (part[0] + part[1]) + (part[2] + part[3]);
+        if (odd) {
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            int hit = 0;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const int key = 8 * (j >> 2) + (j & 3);
+                hit |= 32 * u + key <= rel ? (int)(nans[u][b] >> (4 * half + key)) & 1 : 0;
+              }
+            oacc[b] += (xor32(hit) | hit) ? NAN : 0.f;
+          }
+        }
+      }
+    }
+    lrun += xor32(lrun);
+    if (!rvalid) return;
+    if (whole) {
+      const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;
+      const float lse = write_row<0, 16>(
+          a, orow, lrun == 0.f ? -INFINITY : mref + log2f(lrun),
+          [&](int i) {
+            const int b = i >> 2, e = 4 * (i & 3);
+            return (f32x4){oacc[b][e], oacc[b][e + 1], oacc[b][e + 2], oacc[b][e + 3]} * inv;
+          },
+          [&](int i) { return (i >> 2) * 32 + (i & 3) * 8 + half * 4; });
+      if (half == 0 && a.lse) a.lse[orow] = lse;
+      return;
+    }
+    const size_t prow = ((size_t)w * 2 + slot) * a.few_rows + m;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(a.few_o + prow * D + b * 32 + e * 8 + half * 4) =
+            (f32x4){oacc[b][4 * e], oacc[b][4 * e + 1], oacc[b][4 * e + 2], oacc[b][4 * e + 3]};
+    if (half == 0) {
+      a.few_ml[prow * 2] = mref;
+      a.few_ml[prow * 2 + 1] = lrun;
+    }
+  };
+  few4_runs(a, w, item);
+}
+
+// The value of lane l ^ 16, as xor32.
+__device__ __forceinline__ uint32_t xor16_u(uint32_t v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return (__lane_id() & 16) ? r[0] : r[1];
+}
+__device__ __forceinline__ float xor16(float v) { return __uint_as_float(xor16_u(__float_as_uint(v))); }
+
+// Pages of 4 bits, at most 16 rows per kv head (a single token of a group of up to 16 heads):
+// products of 16 rows, half of whose registers and exponentials are not spent on rows that
+// are none, so that two tiles of codes are in flight.  Lane (m, g) loads block g of 32 dims of keys
+// m, 16 + m, 32 + m and 48 + m of a tile; S^T = K Q^T and O^T = V^T P on v_mfma_f32_16x16x32_bf16: a row's
+// scores of keys 16 u + 4 g .. + 3 are its lane g's, and those of two u are a P operand as they
+// are, V's transposed reads taking their keys in that order.
+constexpr int FQ_VB = FW_KEYS4 * 64 + 64;  // bytes of one 32-dim block of a V tile
+__global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][4 * FQ_VB];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int m = lane & 15, g = lane >> 4;
+  const uint8_t* const kb = (const uint8_t*)a.k;
+  const uint8_t* const vb = (const uint8_t*)a.v;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  // V's place in the wave's LDS: key row k of 64 bytes in each 32-dim block, chunk j of 16 at
+  // j ^ (k / 4 % 4), so that 16 rows' writes fall on distinct banks
+  uint8_t* const vw = s_mem[wave] + g * FQ_VB + m * 64;
+  const int wswz = (m >> 2) & 3;
+  // source lane m of 16 reads key 4 g + m / 4 of 16, dims 4 (m % 4) .. + 3 of 16
+  const uint8_t* const vr = s_mem[wave] + (4 * g + (m >> 2)) * 64 + (m & 1) * 8;
+  const uint8_t *const vr0 = vr + ((((m & 3) >> 1) ^ g) * 16), *const vr1 = vr + (((((m & 3) >> 1) | 2) ^ g) * 16);
+
+  auto item = [&](int i, int s0, int add, int, int rows, int kv, int kvh, int ta, int tb, bool whole, int slot) {
+    const int off = kv - add;
+    const bool rvalid = m < rows;
+    const int tok = rvalid ? m / a.grp : 0;
+    const int head = kvh * a.grp + (rvalid ? m - tok * a.grp : 0);
+    const size_t orow = (size_t)(s0 + tok) * a.Hq + head;
+    const int klim = rvalid ? off + tok : -1;
+    const int wfull = off + 1;                                     // keys that every row sees
+    const int kend = min(max(off + (rows - 1) / a.grp + 1, 0), kv);  // keys that some row sees
+    const int tend = min(tb, (kend + FW_KEYS4 - 1) / FW_KEYS4);
+    const int32_t* row = a.table + (size_t)i * a.stride;
+    bf16x8 bq[4];
+    {
+      const u16x8* qr = reinterpret_cast<const u16x8*>((const uint8_t*)a.q + (size_t)(s0 + tok) * a.qs + head * (D * 2));
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) bq[kk] = __builtin_bit_cast(bf16x8, qr[4 * g + kk]);
+    }
+    f32x4 oacc[8] = {zero, zero, zero, zero, zero, zero, zero, zero};
+    float mref = EX_NONE, lrun = 0.f;
+    struct Codes {
+      uint4 k[4], v[4];
+      uint32_t ks[4], vs[4];   // scales
+      unsigned long long bad;  // keys on pages that are none
+    };
+    auto key_of = [&](int t) { return min(t * FW_KEYS4 + lane, kend - 1); };  // keys past the last repeat it
+    auto id_of = [&](int t) { return row[key_of(t) >> a.shift]; };
+    auto load = [&](int t, int id, Codes& c) {
+      const bool bad = (unsigned)id >= (unsigned)a.num_pages;
+      c.bad = __ballot(bad);
+      // (below 2^32)
+      const unsigned mine = (((unsigned)(bad ? 0 : id) * a.Hkv + kvh) << a.shift) + (key_of(t) & ((1 << a.shift) - 1));
+      size_t r[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) r[u] = (size_t)(unsigned)__builtin_amdgcn_ds_bpermute(4 * (16 * u + m), (int)mine) * 4 + g;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        c.ks[u] = a.ksc[r[u]];
+        c.k[u] = reinterpret_cast<const uint4*>(kb)[r[u]];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        c.vs[u] = a.vsc[r[u]];
+        c.v[u] = reinterpret_cast<const uint4*>(vb)[r[u]];
+      }
+    };
+    auto part_of = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
+    // tile t from c, whose registers then take tile t + 2; id: its page
+    auto step = [&](int t, Codes& c, int& id) {
+      const unsigned long long bad = c.bad;
+      const bool masked = (t + 1) * FW_KEYS4 > wfull || bad != 0;  // uniform
+      f32x4 s[4];
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf16x8, values4(part_of(c.k[u], kk), __uint_as_float(c.ks[u] << 23))), bq[kk],
+              kk ? s[u] : zero, 0, 0, 0);
+      // blocks of V that read as NaN: their codes go into the products as zeros, and NaN into the
+      // outputs of the rows that see them (a zero weight times NaN would be one)
+      const bool odd = __ballot(max(max(c.vs[0], c.vs[1]), max(c.vs[2], c.vs[3])) == 255) != 0;  // uniform
+      unsigned long long nans[4] = {0, 0, 0, 0};  // bit 16 b + k: block b of key 16 u + k
+      if (odd) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          nans[u] = __ballot(c.vs[u] == 255) & ~(((bad >> (16 * u)) & 0xFFFF) * 0x0001000100010001ull);
+          if (c.vs[u] == 255) {
+            c.vs[u] = 0;
+            c.v[u] = make_uint4(0, 0, 0, 0);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<uint4*>(vw + u * 1024 + ((j ^ wswz) * 16)) = values4(part_of(c.v[u], j), __uint_as_float(c.vs[u] << 23));
+      if (t + 2 < tend) {  // uniform
+        load(t + 2, id, c);
+        id = id_of(min(t + 3, tend - 1));
+      }
+      const int rel = klim - t * FW_KEYS4 - 4 * g;
+      if (masked) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const unsigned bm = (unsigned)(bad >> (16 * u)) >> (4 * g);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[u][j] = 16 * u + j > rel || ((bm >> j) & 1) ? -INFINITY : s[u][j];
+        }
+      }
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tmax = fmaxf(tmax, s[u][j]);
+      tmax = fmaxf(tmax, xor16(tmax));
+      tmax = fmaxf(tmax, xor32(tmax)) * EX_SCALE;
+      const bool grow = tmax > mref + 8.0f;
+      if (__ballot(grow)) {  // uniform
+        const float mnew = grow ? tmax : mref;
+        const float alpha = __builtin_amdgcn_exp2f(mref - mnew);
+        lrun *= alpha;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) oacc[d] *= alpha;
+        mref = mnew;
+      }
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        v8i16 vo[8];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          const uint8_t* at = (d & 1 ? vr1 : vr0) + (d >> 1) * FQ_VB + 2 * p * 1024;
+          const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)at);
+          const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(at + 1024));
+          vo[d] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        bf16x8 pb;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * p + (j >> 2)][j & 3], EX_SCALE, -mref));
+          part[j & 3] += x;
+          pb[j] = (__bf16)x;
+        }
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+          oacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vo[d]), pb, oacc[d], 0, 0, 0);
+      }
+      lrun += (part[0] + part[1]) + (part[2] + part[3]);
+      if (odd) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          uint32_t hit = 0;
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              hit |= 16 * u + j <= rel ? (uint32_t)(nans[u] >> (16 * b + 4 * g + j)) & 1 : 0;
+          hit |= xor16_u(hit);
+          hit |= xor32_u(hit);
+          const float add_nan = hit ? NAN : 0.f;
+          oacc[2 * b] += add_nan;
+          oacc[2 * b + 1] += add_nan;
+        }
+      }
+    };
+    if (ta < tend) {
+      Codes c0, c1;
+      load(ta, id_of(ta), c0);
+      load(min(ta + 1, tend - 1), id_of(min(ta + 1, tend - 1)), c1);
+      int id = id_of(min(ta + 2, tend - 1));
+      for (int t = ta; t < tend; t += 2) {
+        step(t, c0, id);
+        if (t + 1 < tend) step(t + 1, c1, id);  // uniform
+      }
+    }
+    lrun += xor16(lrun);
+    lrun += xor32(lrun);
+    if (!rvalid) return;
+    if (whole) {
+      const float inv = lrun > 0.f || lrun != lrun ? 1.0f / lrun : 0.f;
+      const float lse = write_row<0, 8>(a, orow, lrun == 0.f ? -INFINITY : mref + log2f(lrun),
+                                        [&](int d) { return oacc[d] * inv; }, [&](int d) { return 16 * d + 4 * g; });
+      if (g == 0 && a.lse) a.lse[orow] = lse;
+      return;
+    }
+    const size_t prow = ((size_t)(blockIdx.x * FW_W + wave) * 2 + slot) * a.few_rows + m;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) *reinterpret_cast<f32x4*>(a.few_o + prow * D + 16 * d + 4 * g) = oacc[d];
+    if (g == 0) {
+      a.few_ml[prow * 2] = mref;
+      a.few_ml[prow * 2 + 1] = lrun;
+    }
+  };
+  few4_runs(a, blockIdx.x * FW_W + wave, item);
 }
 
 // Joins the partials of the items that begin in waves 8 b .. 8 b + 7 of
@@ -1645,8 +1985,9 @@ __global__ __launch_bounds__(FJ_W * 64) void k_exact_few_join(ExactArgs a, int w
 hipError_t launch_exact(const ExactArgs& a, bool fp32, Keys keys, hipStream_t st) {
   if (a.few) {
     const int wgs = (a.few + FW_W - 1) / FW_W;
-    if (keys == Keys::PAGES4) hipLaunchKernelGGL((k_exact_few<1>), dim3(wgs), dim3(FW_W * 64), 0, st, a);
-    else hipLaunchKernelGGL((k_exact_few<0>), dim3(wgs), dim3(FW_W * 64), 0, st, a);
+    if (keys != Keys::PAGES4) hipLaunchKernelGGL(k_exact_few, dim3(wgs), dim3(FW_W * 64), 0, st, a);
+    else if (a.few_rows <= 16) hipLaunchKernelGGL(k_exact_few4_16, dim3(wgs), dim3(FW_W * 64), 0, st, a);
+    else hipLaunchKernelGGL(k_exact_few4, dim3(wgs), dim3(FW_W * 64), 0, st, a);
     // a workgroup per row and 8 waves, up to 2048 of them, at least four to 8 waves
     const int parts = (wgs * FW_W + FJ_W - 1) / FJ_W;
     hipLaunchKernelGGL(k_exact_few_join, dim3(parts, std::min(a.few_rows, std::max(FJ_Y, 2048 / parts))), dim3(FJ_W * 64), 0,
