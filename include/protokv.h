@@ -645,7 +645,7 @@ typedef struct {
 } protokv_pages4;
 
 typedef struct {
-  int32_t num_tokens;     /* N, >= 0 (0: nothing is done); 2 N num_kv_heads < 2^29 */
+  int32_t num_tokens;     /* N, >= 0 (0: nothing is done); 2 N num_kv_heads < 2^27 - 8 */
   int32_t num_kv_heads, head_dim, kv_dtype;
   void* k;                /* device rows of num_kv_heads heads: read by store, written by read */
   void* v;

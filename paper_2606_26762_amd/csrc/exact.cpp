@@ -448,8 +448,8 @@ protokv_status page4_rows(const protokv_page4_rows_args* a, bool store, void* st
   s = check_page_sizes(a->pages.num_pages, a->pages.page_size, who);
   if (s != PROTOKV_OK) return s;
   const int64_t rows = 2 * (int64_t)a->num_tokens * h.kv;
-  if (rows >= (1ll << 29))  // eight threads to a row, fewer than 2^32 to a launch
-    return fail(PROTOKV_E_UNSUPPORTED, who, "2 * num_tokens * num_kv_heads must be below 2^29");
+  if (rows >= (1ll << 27) - 8)  // up to 32 threads to a row, fewer than 2^32 to a launch in whole workgroups
+    return fail(PROTOKV_E_UNSUPPORTED, who, "2 * num_tokens * num_kv_heads must be below 2^27 - 8");
   if (rows == 0) return PROTOKV_OK;  // (empty arrays may have no address)
   s = check_pages4(a->pages, h.kv, who);
   if (s == PROTOKV_OK) s = check_rows(a->k, a->k_stride, h.kv, h, who, "k");

@@ -8,117 +8,133 @@ namespace pkv {
 
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------------------
-// Rows into and out of 4 bits.  A row (token, head, k or v) to eight lanes, 16
-// dims each; a block of 32 dims is two of them.  v_cvt_scalef32_pk_fp4_f32 divides by
-// the power of two, rounds to the nearest code, ties to the even one, and ends at 6,
-// which is the format's own rule (all bfloat16 values and the codes' borders checked
-// against it); the way back is exact.  Bound by the rows' bytes.
+// Rows into and out of 4 bits.  A thread takes 16 bytes of a row (token, head, k or v),
+// so that a wave's accesses are whole rows: 4 dims of float32, eight threads to a block of
+// 32, or 8 of bfloat16, four.  v_cvt_scalef32_pk_fp4_f32 divides by the power of two,
+// rounds to the nearest code, ties to the even one, and ends at 6, which is the format's own rule
+// (all bfloat16 values and the codes' borders checked against it); the way back is
+// exact.  Bound by the rows' bytes.
 // ---------------------------------------------------------------------------
 
-// Rows of a call: row r is k's or v's (r / Hkv odd) head r % Hkv of token r / (2 Hkv).
+// Row r of a call is k's or v's head r % Hkv of token r / (2 Hkv), k's first.
 struct Row4 {
-  long long at;  // bytes from the rows' start
-  int slot;      // -1: none
-  int head;
+  int token, head;
   bool value;
 };
-__device__ __forceinline__ Row4 row4_of(const Page4Rows& a, long long r) {
-  const int t = (int)(r / (2 * a.Hkv)), j = (int)(r - (long long)t * (2 * a.Hkv));
-  Row4 x;
-  x.value = j >= a.Hkv;
-  x.head = x.value ? j - a.Hkv : j;
-  x.slot = a.slots[t];
-  if ((unsigned)x.slot >= (unsigned)a.nslots) x.slot = -1;
-  x.at = (long long)t * (x.value ? a.vs : a.ks);
-  return x;
+__device__ __forceinline__ Row4 row4_of(const Page4Rows& a, unsigned r) {  // below 2^27
+  const unsigned per = 2 * a.Hkv, t = r / per;
+  const int j = (int)(r - t * per);
+  return {(int)t, j >= a.Hkv ? j - a.Hkv : j, j >= a.Hkv};
+}
+__device__ __forceinline__ int slot4_of(const Page4Rows& a, const Row4& x) {
+  const int s = a.slots[x.token];
+  return (unsigned)s < (unsigned)a.nslots ? s : -1;
+}
+template <int FP32>
+__device__ __forceinline__ uint4* row4_at(const Page4Rows& a, const Row4& x) {
+  return reinterpret_cast<uint4*>((x.value ? a.v : a.k) + x.token * (x.value ? a.vs : a.ks) + (size_t)x.head * (D * (FP32 ? 4 : 2)));
 }
 // row of the pages that a slot's head is
-__device__ __forceinline__ long long place4(const Page4Rows& a, const Row4& x) {
-  return (((long long)(x.slot >> a.shift) * a.Hkv + x.head) << a.shift) + (x.slot & ((1 << a.shift) - 1));
+__device__ __forceinline__ long long place4(const Page4Rows& a, const Row4& x, int slot) {
+  return (((long long)(slot >> a.shift) * a.Hkv + x.head) << a.shift) + (slot & ((1 << a.shift) - 1));
 }
 
-template <int FP32>
+// P4_U: pieces of a thread, a workgroup's width apart, all in flight
+template <int FP32, int P4_U>
 __global__ __launch_bounds__(256) void k_page4_store(Page4Rows a) {
-  const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) >> 3;
-  const int c = threadIdx.x & 7;
-  if (r >= a.rows) return;  // all eight lanes of a row together
-  const Row4 x = row4_of(a, r);
-  if (x.slot < 0) return;
-  const uint8_t* src = (x.value ? a.v : a.k) + x.at + (size_t)x.head * (D * (FP32 ? 4 : 2));
-  float v[16];
-  if constexpr (FP32) {
-    const float4* p = reinterpret_cast<const float4*>(src) + 4 * c;
+  constexpr int W = FP32 ? 4 : 8;  // dims to a piece
+  uint4 in[P4_U];
+  Row4 x[P4_U];
+  int slot[P4_U];
+  const unsigned c = threadIdx.x % (D / W);
+#pragma unroll
+  for (int u = 0; u < P4_U; ++u) {
+    const unsigned r = (blockIdx.x * P4_U + u) * (256u / (D / W)) + threadIdx.x / (D / W);
+    slot[u] = -1;
+    if (r < a.rows) {  // the threads of a row together
+      x[u] = row4_of(a, r);
+      slot[u] = slot4_of(a, x[u]);
+      in[u] = row4_at<FP32>(a, x[u])[c];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < P4_U; ++u) {
+    if (slot[u] < 0) continue;
+    const uint32_t w[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
+    float v[W];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float4 w = p[i];
-      v[4 * i] = w.x;
-      v[4 * i + 1] = w.y;
-      v[4 * i + 2] = w.z;
-      v[4 * i + 3] = w.w;
+      if constexpr (FP32) {
+        v[i] = __uint_as_float(w[i]);
+      } else {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      }
     }
-  } else {
-    const uint4* p = reinterpret_cast<const uint4*>(src) + 2 * c;
-    const uint4 w[2] = {p[0], p[1]};
+    // the block's largest |x| by its bits, where infinities and NaN lie above every number
+    uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint4 q = w[i >> 2];
-      const uint32_t u = (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w;
-      v[2 * i] = __uint_as_float(u << 16);
-      v[2 * i + 1] = __uint_as_float(u & 0xFFFF0000u);
+    for (int i = 0; i < W; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));  // lane ^ 1
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));  // lane ^ 2
+    if (FP32) top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x141, 0xf, 0xf, false));  // the other four of eight
+    // least e with top <= 7 * 2^e: two below top's exponent, one more past 1.75
+    const bool odd = top >= 0x7F800000u;
+    const int s = odd ? 255 : min(max((int)((top + 0x1FFFFFu) >> 23) - 2, 2), 252);
+    const float scale = __uint_as_float((uint32_t)s << 23);
+    uint32_t codes = 0;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[0], v[1], scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[2], v[3], scale, 1);
+    if constexpr (!FP32) {
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[4], v[5], scale, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[6], v[7], scale, 3);
     }
+    if (odd) codes = 0;
+    const long long at = place4(a, x[u], slot[u]);
+    uint8_t* out = (x[u].value ? a.pv : a.pk) + at * (D / 2);
+    if constexpr (FP32) reinterpret_cast<uint16_t*>(out)[c] = (uint16_t)codes;
+    else reinterpret_cast<uint32_t*>(out)[c] = codes;
+    if (c % (32 / W) == 0) (x[u].value ? a.vsc : a.ksc)[at * (D / 32) + c / (32 / W)] = (uint8_t)s;
   }
-  // the largest |x| by its bits, where infinities and NaN lie above every number
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));  // the pair's other lane
-  // least e with top <= 7 * 2^e: two below top's exponent, one more past 1.75
-  const bool odd = top >= 0x7F800000u;
-  const int s = odd ? 255 : min(max((int)((top + 0x1FFFFFu) >> 23) - 2, 2), 252);
-  const float scale = __uint_as_float((uint32_t)s << 23);
-  uint32_t lo = 0, hi = 0;
-  lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, v[0], v[1], scale, 0);
-  lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, v[2], v[3], scale, 1);
-  lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, v[4], v[5], scale, 2);
-  lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, v[6], v[7], scale, 3);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(hi, v[8], v[9], scale, 0);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(hi, v[10], v[11], scale, 1);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(hi, v[12], v[13], scale, 2);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(hi, v[14], v[15], scale, 3);
-  const long long at = place4(a, x);
-  reinterpret_cast<uint2*>((x.value ? a.pv : a.pk) + at * (D / 2))[c] = odd ? make_uint2(0, 0) : make_uint2(lo, hi);
-  if (!(c & 1)) (x.value ? a.vsc : a.ksc)[at * (D / 32) + (c >> 1)] = (uint8_t)s;
 }
 
-template <int FP32>
+template <int FP32, int P4_U>
 __global__ __launch_bounds__(256) void k_page4_read(Page4Rows a) {
-  const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) >> 3;
-  const int c = threadIdx.x & 7;
-  if (r >= a.rows) return;
-  const Row4 x = row4_of(a, r);
-  uint2 w = make_uint2(0, 0);
-  float scale = 1.f;
-  if (x.slot >= 0) {
-    const long long at = place4(a, x);
-    w = reinterpret_cast<const uint2*>((x.value ? a.pv : a.pk) + at * (D / 2))[c];
-    scale = __uint_as_float((uint32_t)(x.value ? a.vsc : a.ksc)[at * (D / 32) + (c >> 1)] << 23);
+  constexpr int W = FP32 ? 4 : 8;
+  Row4 x[P4_U];
+  int slot[P4_U];
+  uint32_t codes[P4_U], s[P4_U];
+  const unsigned c = threadIdx.x % (D / W), r0 = blockIdx.x * P4_U * (256u / (D / W)) + threadIdx.x / (D / W);
+#pragma unroll
+  for (int u = 0; u < P4_U; ++u) {
+    x[u] = row4_of(a, min(r0 + u * (256u / (D / W)), (unsigned)a.rows - 1));  // past the last row it is read again
+    slot[u] = slot4_of(a, x[u]);
   }
-  uint8_t* dst = (x.value ? a.v : a.k) + x.at + (size_t)x.head * (D * (FP32 ? 4 : 2));
-  if constexpr (FP32) {
-    float4* p = reinterpret_cast<float4*>(dst) + 4 * c;
-    auto put = [&](int i, f32x2 l, f32x2 h) { p[i] = make_float4(l[0], l[1], h[0], h[1]); };
-    put(0, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 1));
-    put(1, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 3));
-    put(2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.y, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.y, scale, 1));
-    put(3, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.y, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.y, scale, 3));
-  } else {
-    uint4* p = reinterpret_cast<uint4*>(dst) + 2 * c;
-    p[0] = values4(w.x, scale);
-    p[1] = values4(w.y, scale);
+#pragma unroll
+  for (int u = 0; u < P4_U; ++u) {
+    codes[u] = s[u] = 0;
+    if (slot[u] < 0) continue;
+    const long long at = place4(a, x[u], slot[u]);
+    const uint8_t* in = (x[u].value ? a.pv : a.pk) + at * (D / 2);
+    codes[u] = FP32 ? reinterpret_cast<const uint16_t*>(in)[c] : reinterpret_cast<const uint32_t*>(in)[c];
+    s[u] = (x[u].value ? a.vsc : a.ksc)[at * (D / 32) + c / (32 / W)];
+  }
+#pragma unroll
+  for (int u = 0; u < P4_U; ++u) {
+    if (r0 + u * (256u / (D / W)) >= a.rows) break;
+    const float scale = __uint_as_float(s[u] << 23);
+    uint4 out;
+    if constexpr (FP32) {
+      const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], scale, 0);
+      const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], scale, 1);
+      out = make_uint4(__float_as_uint(lo[0]), __float_as_uint(lo[1]), __float_as_uint(hi[0]), __float_as_uint(hi[1]));
+    } else {
+      out = values4(codes[u], scale);
+    }
+    row4_at<FP32>(a, x[u])[c] = out;
   }
 }
 
@@ -430,12 +446,22 @@ __global__ __launch_bounds__(1024) void k_release_collect(protokv_page_release_a
 
 }  // namespace
 
+template <int FP32, int U>
+static void page4_rows(const Page4Rows& a, bool store, hipStream_t st) {
+  constexpr unsigned per = 256 / (FP32 ? 32 : 16) * U;  // rows of a workgroup
+  const dim3 wgs((unsigned)((a.rows + per - 1) / per)), threads(256);
+  if (store) hipLaunchKernelGGL((k_page4_store<FP32, U>), wgs, threads, 0, st, a);
+  else hipLaunchKernelGGL((k_page4_read<FP32, U>), wgs, threads, 0, st, a);
+}
+
 hipError_t launch_page4_rows(const Page4Rows& a, bool fp32, bool store, hipStream_t st) {
-  const dim3 wgs((unsigned)((a.rows * 8 + 255) / 256)), threads(256);
-  if (store && fp32) hipLaunchKernelGGL((k_page4_store<1>), wgs, threads, 0, st, a);
-  else if (store) hipLaunchKernelGGL((k_page4_store<0>), wgs, threads, 0, st, a);
-  else if (fp32) hipLaunchKernelGGL((k_page4_read<1>), wgs, threads, 0, st, a);
-  else hipLaunchKernelGGL((k_page4_read<0>), wgs, threads, 0, st, a);
+  // four pieces to a thread where one would take more than 8192 workgroups (store and read, 8 heads:
+  // 64 tokens of 4 heads 2.9 + 3.0 us with one, 4.0 + 3.6 with four; 18 432 tokens 51 and 44, float32 93 and 84)
+  const bool many = a.rows * (fp32 ? 32 : 16) > 8192 * 256;
+  if (fp32 && many) page4_rows<1, 4>(a, store, st);
+  else if (fp32) page4_rows<1, 1>(a, store, st);
+  else if (many) page4_rows<0, 4>(a, store, st);
+  else page4_rows<0, 1>(a, store, st);
   return hipGetLastError();
 }
 

@@ -113,12 +113,27 @@ __device__ __forceinline__ void rotate_rows(const RotateArgs& a, const NormArgs&
         const double x = lo.get(i), y = hi.get(i);
         ss = fma(x, x, fma(y, y, ss));
       }
-      const float inv = (float)(1.0 / sqrt(sum8(ss) * (1.0 / D) + nm.eps));
+      double inv = 1.0 / sqrt(sum8(ss) * (1.0 / D) + nm.eps);
       float x[8], y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = lo.get(i) * inv;
-        y[i] = hi.get(i) * inv;
+        x[i] = lo.get(i);
+        y[i] = hi.get(i);
+      }
+      if (inv < 0x1p-100 || inv > 0x1p100) {  // near float32's ends a power of two comes first (products in float64: 5% longer)
+        const float by = inv < 1.0 ? 0x1p-64f : 0x1p100f;
+        inv *= inv < 1.0 ? 0x1p64 : 0x1p-100;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] *= by;
+          y[i] *= by;
+        }
+      }
+      const float f = (float)inv;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] *= f;
+        y[i] *= f;
       }
       if (w) {
 #pragma unroll
