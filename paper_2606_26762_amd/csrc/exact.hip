@@ -1413,7 +1413,7 @@ __device__ __forceinline__ int groups_of(int rows) { return (rows + EX_FEW - 1) 
 // [ta, tb) of request i's kv head kvh, rows r0 .. r0 + rows - 1; whole: those are all of the item's.
 // Items are (request, kv head, group of 32 rows), their tiles of 64 keys; runs, partials and notes as in
 // k_exact_few.
-template <typename ITEM>
+template <int ALONE, typename ITEM>
 __device__ __forceinline__ void few4_runs(const ExactArgs& a, int w, ITEM item) {
   const int lane = threadIdx.x & 63;
   int32_t* meta = a.few_meta + w * 4;
@@ -1435,7 +1435,12 @@ __device__ __forceinline__ void few4_runs(const ExactArgs& a, int w, ITEM item) 
   // token over 130 000, 8 kv heads, 39 us, 64 over 125 to 8000 34; up to 16: 37 and 41), but where items
   // are of 8 or fewer on average, which leave few partials (see `alone` below)
   long long share = min((long long)EX_FEW_RUN4, (N + 511) / 512);
-  if (N <= EX_FEW_RUN4 * lane_ll(wave_sum(items), 63) * a.Hkv) share = 1;
+  const long long all_items = lane_ll(wave_sum(items), 63) * a.Hkv;
+  if (N <= EX_FEW_RUN4 * all_items) share = 1;
+  // an item of half a run or less, or of so many tiles, is its first tile's wave's alone, so that
+  // many short items leave no partials; of more tiles where there are items for half the waves (64 x 16
+  // tokens over 1000, 28 / 4 heads, 1024 items of 16 tiles, shared 63 us, alone 53)
+  const int single = (all_items >= 1024 ? ALONE : 4) + FW_START4;
   const long long per = max((N + waves - 1) / waves, share);
   const long long x1 = min(N, (w + 1) * per);
   long long x = w * per;
@@ -1467,9 +1472,7 @@ __device__ __forceinline__ void few4_runs(const ExactArgs& a, int w, ITEM item) 
       const int r0 = __builtin_amdgcn_readfirstlane((int)(at - (long long)kvh * groups)) * EX_FEW;
       const int mine = min(rows - r0, EX_FEW);
       const int ta = __builtin_amdgcn_readfirstlane((int)(x - first - at * T));
-      // an item of half a run or less, or of four tiles, is its first tile's wave's
-      // alone, so that many short items leave no partials
-      const bool alone = 2 * T <= per || T <= 4 + FW_START4;  // uniform
+      const bool alone = 2 * T <= per || T <= single;  // uniform
       const int tb = __builtin_amdgcn_readfirstlane(alone ? T : (int)min((long long)T, ta + (x1 - x)));
       if (alone && ta > 0) {
         x += T - ta;
@@ -1490,8 +1493,13 @@ __device__ __forceinline__ void few4_runs(const ExactArgs& a, int w, ITEM item) 
 }
 
 // Pages of 4 bits, groups of 32 rows.  Lane (m, h) loads the blocks h and 2 + h of 32 dims of key
-// m's row of K and of V and turns them to bfloat16, K into the operand (the query's dims lie
-// accordingly), V into the wave's LDS; a tile's loads go out once the one before is used.
+// m's row of K and of V and turns them to bfloat16, exactly (v_cvt_scalef32_pk_bf16_fp4), K into the
+// operand (the query's dims lie accordingly), V into the wave's LDS; a tile's loads go out
+// once the one before is used.  The weights are rounded to bfloat16 for the second product, as in the
+// other kernels here.  Tiles of 64 keys: two chains of products side by side, and the maximum, its
+// exchange and its test once (tiles of 32, 8 x 40 tokens over 16 000, 32 / 8 heads: 140 us, of 64 125).  Bound by
+// the VALU and the matrix cores in turn, with two waves to a SIMD: 400 instructions and 32 products to a tile,
+// 64 x 16 tokens over 8000, 28 / 4 heads, 218 us, 0.54 PFLOP/s of what is seen.
 __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2 * 4 * FW_VB];  // V of a tile, by its halves of 32 keys
   const int lane = threadIdx.x & 63;
@@ -1626,13 +1634,15 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
         const int rel = klim - t * FW_KEYS4 - 4 * half;
         if (masked) {
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const unsigned bm = badm[u] >> (4 * half);
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const int key = 8 * (j >> 2) + (j & 3);
-              s[u][j] = 32 * u + key > rel || ((bm >> key) & 1) ? -INFINITY : s[u][j];
-            }
+            for (int j = 0; j < 16; ++j) s[u][j] = 32 * u + 8 * (j >> 2) + (j & 3) > rel ? -INFINITY : s[u][j];
+          if (badm[0] | badm[1]) {  // uniform
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                s[u][j] = (badm[u] >> (4 * half + 8 * (j >> 2) + (j & 3))) & 1 ? -INFINITY : s[u][j];
           }
         }
         float top[2] = {-INFINITY, -INFINITY};
@@ -1716,7 +1726,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
       a.few_ml[prow * 2 + 1] = lrun;
     }
   };
-  few4_runs(a, w, item);
+  few4_runs<16>(a, w, item);
 }
 
 // The value of lane l ^ 16, as xor32.
@@ -1731,7 +1741,9 @@ __device__ __forceinline__ float xor16(float v) { return __uint_as_float(xor16_u
 // are none, so that two tiles of codes are in flight.  Lane (m, g) loads block g of 32 dims of keys
 // m, 16 + m, 32 + m and 48 + m of a tile; S^T = K Q^T and O^T = V^T P on v_mfma_f32_16x16x32_bf16: a row's
 // scores of keys 16 u + 4 g .. + 3 are its lane g's, and those of two u are a P operand as they
-// are, V's transposed reads taking their keys in that order.
+// are, V's transposed reads taking their keys in that order.  Bound by the cache's bytes: 64 tokens over
+// 32 768, 28 / 4 heads, 1.14 GB, 219 us with the join, 5.2 TB/s (by 32 rows 229); over contexts of 500 to 32 768,
+// 0.35 GB, 75 us and the join's 9; one token over 1500 9 us, a chain of one or two tiles.
 constexpr int FQ_VB = FW_KEYS4 * 64 + 64;  // bytes of one 32-dim block of a V tile
 __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][4 * FQ_VB];
@@ -1923,7 +1935,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
       a.few_ml[prow * 2 + 1] = lrun;
     }
   };
-  few4_runs(a, blockIdx.x * FW_W + wave, item);
+  few4_runs<4>(a, blockIdx.x * FW_W + wave, item);
 }
 
 // Joins the partials of the items that begin in waves 8 b .. 8 b + 7 of

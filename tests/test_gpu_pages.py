@@ -402,6 +402,44 @@ def test_page4_attend_of_many_requests():
     _paged4(reqs, 2, 1, 8, "bf16", 21)
 
 
+def test_page4_attend_of_many_single_tokens():
+    """Hundreds of requests of one token or none: short items, and long ones that several waves share."""
+    log("case: page4 attend of many single tokens")
+    rng = np.random.default_rng(22)
+    reqs = [(int(rng.integers(0, 700)), int(rng.random() < 0.9)) for _ in range(300)]
+    reqs[5], reqs[200], reqs[299] = (9000, 1), (6000, 1), (3000, 1)
+    _paged4(reqs, 5, 1, 16, "bf16", 22, prior=True)
+
+
+@pytest.mark.parametrize("hq,hk,P,prior", [(14, 2, 16, True), (28, 4, 16, False)])
+def test_page4_attend_of_some_rows_to_many_requests(hq, hk, P, prior):
+    """So many requests of some rows that they go in groups of 32, whole items and shared ones."""
+    log(f"case: page4 attend of some rows heads {hq}/{hk} prior {prior}")
+    _paged4([(97 * i % 1500, i % 17) for i in range(64)], hq, hk, P, "bf16", 23, prior=prior)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hq,most", [(2, 4), (2, 1), (40, 4)])
+def test_page4_attend_rows_beyond_max_add_are_left(hq, most, dtype):
+    import torch
+    log(f"case: page4 max_add {most} {dtype}")
+    pk, g = PK(), _g(16)
+    dt = _dt(dtype)
+    pages = pages4(4, 1, 16)
+    held(g, pages, torch.arange(4, device="cuda"), 64, 1, 16, dtype)
+    q = _randn(g, 12, hq, D, dtype=dt)
+    args = (pages, _i32([[0, 1], [2, 3]]), _i32([0, 8, 12]), _i32([20, 30]))
+    full, _ = pk.page4_attend(q, *args, 8)
+    o = torch.full_like(full, 7.5)
+    pk.page4_attend(q, *args, most, out=o)
+    torch.cuda.synchronize()
+    keep = torch.zeros(12, dtype=torch.bool, device="cuda")
+    keep[:most] = keep[8:8 + most] = True
+    assert bool((o[~keep] == 7.5).all())
+    got, want = o[keep].double(), full[keep].double()
+    assert bool(((got - want).abs() <= 2 * HB * (want.abs() + 0.05)).all())
+
+
 @pytest.mark.parametrize("P", [1, 2])
 def test_page4_attend_ids_staged_in_runs(P):
     log(f"case: page4 {P} tokens to a page")
