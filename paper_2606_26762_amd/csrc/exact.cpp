@@ -208,7 +208,7 @@ size_t lay_out(ExactArgs& a, uint8_t* base) {
     off += (bytes + 255) & ~(size_t)255;
     return p;
   };
-  if (a.few) {
+  if (a.few && !a.few_alone) {
     const size_t rows = (size_t)a.few * 2 * a.few_rows;
     a.few_o = (float*)take(rows * D * 4);
     a.few_ml = (float*)take(rows * 2 * 4);
@@ -286,6 +286,7 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
       a.splits = 1;
     }
     if (all || with_few) few_waves(tiles);
+    a.few_alone = span <= 64 * EX_FEW_ALONE4;
   } else if (with_few) {
     few_waves(((int64_t)a.Hkv * a.n * ((span + 31) / 32) + 1) / 2);
   }

@@ -22,6 +22,7 @@ constexpr int EX_MIN_TILES = 4;  // a context of fewer than twice as many tiles 
 constexpr int EX_FEW = 32;        // rows per kv head of a request that the few-rows kernel takes
 constexpr int EX_FEW_WAVES = 2048;  // waves of the few-rows kernel, at most (two to a SIMD)
 constexpr int EX_FEW_RUN4 = 8;    // its tiles of 64 keys of 4 bits to a wave that are not spread over more waves than 512
+constexpr int EX_FEW_ALONE4 = 4;  // items of so few such tiles are one wave's, and leave no partials
 constexpr int MAX_REQUESTS = 8192;
 constexpr int MAX_AXES = 8;
 
@@ -64,6 +65,7 @@ struct ExactArgs {
   int32_t* few_meta;
   int few, few_rows;  // its waves (0: not launched, the row blocks take every request), its rows at most
   int few_limit;      // pages of 4 bits: rows per kv head of a request that it takes, in groups of 32
+  bool few_alone;     // pages of 4 bits: no item has more than EX_FEW_ALONE4 tiles, so that there is nothing to join
   int rows;    // query rows of a row block
   int blocks;  // row-block indices per kv head (0: no row blocks)
   int splits;  // most context splits of a row block

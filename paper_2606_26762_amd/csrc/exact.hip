@@ -1440,11 +1440,11 @@ __device__ __forceinline__ void few4_runs(const ExactArgs& a, int w, ITEM item) 
   // an item of half a run or less, or of so many tiles, is its first tile's wave's alone, so that
   // many short items leave no partials; of more tiles where there are items for half the waves (64 x 16
   // tokens over 1000, 28 / 4 heads, 1024 items of 16 tiles, shared 63 us, alone 53)
-  const int single = (all_items >= 1024 ? ALONE : 4) + FW_START4;
+  const int single = (all_items >= 1024 ? ALONE : EX_FEW_ALONE4) + FW_START4;
   const long long per = max((N + waves - 1) / waves, share);
   const long long x1 = min(N, (w + 1) * per);
   long long x = w * per;
-  if (lane == 0) meta[0] = 0;
+  if (lane == 0 && !a.few_alone) meta[0] = 0;
   if (x >= N) return;  // uniform, and nothing below synchronises waves
   int i0 = 0;            // first request of the 64 in the lanes
   long long before = 0;  // tiles before it
@@ -1935,7 +1935,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
       a.few_ml[prow * 2 + 1] = lrun;
     }
   };
-  few4_runs<4>(a, blockIdx.x * FW_W + wave, item);
+  few4_runs<EX_FEW_ALONE4>(a, blockIdx.x * FW_W + wave, item);
 }
 
 // Joins the partials of the items that begin in waves 8 b .. 8 b + 7 of
@@ -2000,7 +2000,10 @@ hipError_t launch_exact(const ExactArgs& a, bool fp32, Keys keys, hipStream_t st
     if (keys != Keys::PAGES4) hipLaunchKernelGGL(k_exact_few, dim3(wgs), dim3(FW_W * 64), 0, st, a);
     else if (a.few_rows <= 16) hipLaunchKernelGGL(k_exact_few4_16, dim3(wgs), dim3(FW_W * 64), 0, st, a);
     else hipLaunchKernelGGL(k_exact_few4, dim3(wgs), dim3(FW_W * 64), 0, st, a);
+  }
+  if (a.few && !a.few_alone) {
     // a workgroup per row and 8 waves, up to 2048 of them, at least four to 8 waves
+    const int wgs = (a.few + FW_W - 1) / FW_W;
     const int parts = (wgs * FW_W + FJ_W - 1) / FJ_W;
     hipLaunchKernelGGL(k_exact_few_join, dim3(parts, std::min(a.few_rows, std::max(FJ_Y, 2048 / parts))), dim3(FJ_W * 64), 0,
                        st, a, wgs * FW_W);

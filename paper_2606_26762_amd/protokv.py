@@ -817,14 +817,14 @@ def _pages4(pages, dev, kv_heads) -> Pages4:
     scales (k_scale, v_scale) [num_pages][kv heads][page size][4]."""
     import torch
     k, v, ks, vs = pages
-    shape = k.shape
-    if len(shape) != 4 or shape[1] != kv_heads or shape[3] != 64:
-        raise ValueError(f"pages: expected k and v [num_pages, {kv_heads}, page_size, 64]")
-    n, _, size, _ = shape
-    u8 = torch.uint8
-    return Pages4(_flat(k, "pages", u8, dev, *shape), _flat(v, "pages", u8, dev, *shape),
-                  _flat(ks, "pages' scales", u8, dev, n, kv_heads, size, 4),
-                  _flat(vs, "pages' scales", u8, dev, n, kv_heads, size, 4), n, size)
+    shape, u8 = k.shape, torch.uint8
+    if len(shape) != 4 or shape[1] != kv_heads or shape[3] != 64 or v.shape != shape or ks.shape != (*shape[:3], 4) or (
+            vs.shape != ks.shape):
+        raise ValueError(f"pages: expected k and v [num_pages, {kv_heads}, page_size, 64] and scales [.., 4]")
+    for t in pages:
+        if t.dtype != u8 or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError(f"pages: expected contiguous uint8 tensors on the current device, got {t.dtype} on {t.device}")
+    return Pages4(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), shape[0], shape[2])
 
 
 def page4_store(k, v, pages, slots, *, stream=None):

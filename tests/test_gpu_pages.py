@@ -402,6 +402,14 @@ def test_page4_attend_of_many_requests():
     _paged4(reqs, 2, 1, 8, "bf16", 21)
 
 
+@pytest.mark.parametrize("reqs", [[(255, 1), (0, 1), (200, 0)], [(256, 1), (3, 1)], [(250, 6)] * 3, [(100, 156), (17, 1)], [(255, 1)] * 100])
+def test_page4_attend_of_short_tables(reqs):
+    """Contexts that one wave goes through, so that nothing is left to join, and the first that it does not."""
+    log(f"case: page4 short tables {reqs[:3]}")
+    _paged4(reqs, 7, 1, 16, "bf16", 24, prior=True)
+    _paged4(reqs, 6, 2, 8, "bf16", 24)
+
+
 def test_page4_attend_of_many_single_tokens():
     """Hundreds of requests of one token or none: short items, and long ones that several waves share."""
     log("case: page4 attend of many single tokens")

@@ -90,6 +90,9 @@ def test_page4_attend_workspace_goes_by_sizes_alone():
     assert L.protokv_page4_attend_workspace(ctypes.byref(attend(cu=None, q=None, o=None, workspace=None, pages__k=None)),
                                             ctypes.byref(m)) == 0
     assert 0 < n.value == m.value < 1 << 28
+    for kw, some in ((dict(max_add=1, table_stride=16), False), (dict(max_add=1, table_stride=17), True)):
+        assert L.protokv_page4_attend_workspace(ctypes.byref(attend(**kw)), ctypes.byref(n)) == 0
+        assert (n.value > 0) == some   # up to 256 tokens a wave needs no other
     assert L.protokv_page4_attend_workspace(ctypes.byref(attend(head_dim=64)), ctypes.byref(n)) == 2
     assert L.protokv_page4_attend_workspace(None, ctypes.byref(n)) == 1
     assert L.protokv_page4_attend_workspace(ctypes.byref(attend()), None) == 1
