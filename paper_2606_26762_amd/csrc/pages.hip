@@ -9,6 +9,7 @@ namespace pkv {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------
 // Rows into and out of 4 bits.  A thread takes 16 bytes of a row (token, head, k or v),
@@ -273,11 +274,19 @@ __global__ __launch_bounds__(256) void k_page_fork_rows(protokv_page_fork_args a
 // ---------------------------------------------------------------------------
 template <typename T>
 __device__ __forceinline__ void copy_rows_of(const uint8_t* from, uint8_t* to, int heads, size_t head_bytes, unsigned per) {
-  const unsigned all = heads * per;  // units of T: below 2^31, as a page's bytes are
-  for (unsigned u = blockIdx.y * 256 + threadIdx.x; u < all; u += gridDim.y * 256) {
-    const unsigned h = u / per;
-    const size_t at = h * head_bytes + (size_t)(u - h * per) * sizeof(T);
-    *reinterpret_cast<T*>(to + at) = *reinterpret_cast<const T*>(from + at);
+  const unsigned all = heads * per, step = gridDim.y * 256;  // units of T: below 2^31, as a page's bytes are
+  for (unsigned u0 = blockIdx.y * 256 + threadIdx.x; u0 < all; u0 += 4 * step) {
+    T x[4];  // four units in flight
+    size_t at[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const unsigned u = min(u0 + k * step, all - 1), h = u / per;  // past the last unit it is read again
+      at[k] = h * head_bytes + (size_t)(u - h * per) * sizeof(T);
+      x[k] = *reinterpret_cast<const T*>(from + at[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (u0 + k * step < all) *reinterpret_cast<T*>(to + at[k]) = x[k];
   }
 }
 __global__ __launch_bounds__(256) void k_page_copy(PageCopy a) {
@@ -291,7 +300,7 @@ __global__ __launch_bounds__(256) void k_page_copy(PageCopy a) {
   uint8_t* base = a.base[e] + (size_t)(layer - a.first[e]) * a.layer_stride[e];
   const unsigned bytes = (unsigned)(rows * rb);
   if (bytes == 0) return;
-  if (rb % 16 == 0) copy_rows_of<uint4>(base + src * page, base + dst * page, a.Hkv, head, bytes / 16);
+  if (rb % 16 == 0) copy_rows_of<u32x4>(base + src * page, base + dst * page, a.Hkv, head, bytes / 16);
   else copy_rows_of<uint32_t>(base + src * page, base + dst * page, a.Hkv, head, bytes / 4);
 }
 
