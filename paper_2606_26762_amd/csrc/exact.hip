@@ -229,6 +229,22 @@ __device__ __forceinline__ void add_odd(f32x16& o, const f32x16& hits) {
   for (int i = 0; i < 16; ++i) o[i] += hits[i] > 0.f ? (SIGN > 0 ? INFINITY : -INFINITY) : 0.f;
 }
 
+// Pages of 4 bits, few rows: what is not finite (6 * 2^126, 4 * 2^126 and more, NaN) is in blocks with a scale byte from
+// here on.  A tile that has some is put into LDS without it; behind the tile's products it is read from
+// the pages once more, a 1 where a value was +inf or NaN, then where it was -inf or NaN, and two more products
+// with a 1 for every key that a row sees tell which outputs they belong to.  So a hidden key, one
+// of a page that is none (whose place page 0 takes) and the last key's repeats add nothing.  (The compiler is
+// told that such tiles are rare: 64 x 16 tokens over 8000, 28 / 4 heads, 216 us without, 205 with.)
+constexpr uint32_t ODD_SCALE = 253;
+__device__ __forceinline__ uint4 odd_values(uint4 w, uint32_t flip) {  // flip 0: of +inf and NaN; 0x80008000: of -inf and NaN
+  const u32x4 x = {w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip};
+  return __builtin_bit_cast(uint4, odd_operand<1>(__builtin_bit_cast(v8i16, x)));
+}
+__device__ __forceinline__ void drop_odd(uint8_t* p) {  // 16 bytes in LDS
+  const u32x4 x = *reinterpret_cast<u32x4*>(p);
+  *reinterpret_cast<u32x4*>(p) = __builtin_bit_cast(u32x4, odd_operand<0>(__builtin_bit_cast(v8i16, x)));
+}
+
 // Barrier for LDS traffic only: outstanding global loads are not waited for.
 __device__ __forceinline__ void ex_barrier() {
   __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
@@ -1562,9 +1578,16 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
     // V's place in the wave's LDS: key row m of 64 bytes in each 32-dim block, its four chunks of 16
     // permuted, chunk j at j ^ (m / 4 % 4), so that 16 rows' writes fall on distinct banks
     uint8_t* const vw = s_mem[wave] + half * FW_VB + m * 64;
+    auto place = [&](int u, int j) { return vw + u * (4 * FW_VB) + 2 * (j >> 2) * FW_VB + (((j & 3) ^ ((m >> 2) & 3)) * 16); };
     const uint8_t* const vr = s_mem[wave] + (4 * half + (s16 >> 2)) * 64 + (s16 & 1) * 8;
     const int vchunk = (grp16 & 1) * 2 + ((s16 & 3) >> 1);
     const uint8_t *const vlo = vr + ((vchunk ^ half) * 16), *const vhi = vr + 512 + ((vchunk ^ half ^ 2) * 16);
+    auto read_v = [&](int u, int i) {  // operand of 32-dim block i / 2, 16-key step i % 2
+      const int at = u * (4 * FW_VB) + (i >> 1) * FW_VB + (i & 1) * 1024;
+      const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vlo + at));
+      const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vhi + at));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
     if (ta < tend) {
       Codes c[2];
       int id[2];
@@ -1583,24 +1606,8 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) badm[u] = (unsigned)__ballot(c[u].bad);
         const bool masked = (t + 1) * FW_KEYS4 > wfull || (badm[0] | badm[1]) != 0;  // uniform
-        // blocks of V that read as NaN: their codes go into the products as zeros, and NaN into the
-        // outputs of the rows that see them (a zero weight times NaN would be one)
-        auto has_nan = [](uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & w & 0x80808080u; };
-        const bool odd = __ballot((has_nan(c[0].vs) | has_nan(c[1].vs)) != 0) != 0;  // uniform
-        unsigned nans[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // keys of each block of 32 dims
-        if (odd) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-#pragma unroll
-            for (int b = 0; b < 4; ++b) nans[u][b] = (unsigned)__ballot(((c[u].vs >> (8 * b)) & 255) == 255) & ~badm[u];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              if (((c[u].vs >> (16 * i + 8 * half)) & 255) == 255) {
-                c[u].vs &= ~(255u << (16 * i + 8 * half));
-                c[u].v[i] = make_uint4(0, 0, 0, 0);
-              }
-          }
-        }
+        auto has_odd = [](uint32_t w) { return ((w & 0x7F7F7F7Fu) + (256 - ODD_SCALE) * 0x01010101u) & w & 0x80808080u; };
+        const bool odd = __ballot((has_odd(c[0].vs) | has_odd(c[1].vs)) != 0) != 0;  // uniform
         f32x16 s[2];
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
@@ -1623,8 +1630,11 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<uint4*>(vw + u * (4 * FW_VB) + 2 * (j >> 2) * FW_VB + (((j & 3) ^ ((m >> 2) & 3)) * 16)) =
-                values4(part_of(c[u].v[j >> 2], j & 3), scale_of(c[u].vs, j >> 2));
+            *reinterpret_cast<uint4*>(place(u, j)) = values4(part_of(c[u].v[j >> 2], j & 3), scale_of(c[u].vs, j >> 2));
+        if (__builtin_expect(odd, 0)) {
+#pragma unroll 1
+          for (int j = 0; j < 16; ++j) drop_odd(place(j >> 3, j & 7));
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < 2; ++u) load4v(next[u], c[u]);
@@ -1666,12 +1676,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
         for (int u = 0; u < 2; ++u) {
           v8i16 vo[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int at = u * (4 * FW_VB) + (i >> 1) * FW_VB + (i & 1) * 1024;
-            const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vlo + at));
-            const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vhi + at));
-            vo[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-          }
+          for (int i = 0; i < 8; ++i) vo[i] = read_v(u, i);
           bf16x8 pb[2];
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
@@ -1684,18 +1689,38 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
             oacc[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vo[i]), pb[i & 1], oacc[i >> 1], 0, 0, 0);
         }
         lrun += (part[0] + part[1]) + (part[2] + part[3]);
-        if (odd) {
+        if (__builtin_expect(odd, 0)) {
+#pragma unroll 1
+          for (int sign = 0; sign < 2; ++sign) {
+#pragma unroll 1
+            for (int u = 0; u < 2; ++u) {
+              Codes x;
+              load4v(row4(t, u, id4(t, u), x), x);
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            int hit = 0;
+              for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<uint4*>(place(u, j)) =
+                    odd_values(values4(part_of(x.v[j >> 2], j & 3), scale_of(x.vs, j >> 2)), sign ? 0x80008000u : 0);
+            }
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int b = 0; b < 4; ++b) {
+              f32x16 hits = zero;
 #pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const int key = 8 * (j >> 2) + (j & 3);
-                hit |= 32 * u + key <= rel ? (int)(nans[u][b] >> (4 * half + key)) & 1 : 0;
-              }
-            oacc[b] += (xor32(hit) | hit) ? NAN : 0.f;
+              for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                  bf16x8 see;
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) {
+                    const int key = 16 * st + 8 * (j >> 2) + (j & 3);
+                    see[j] = 32 * u + key > rel || ((badm[u] >> (4 * half + key)) & 1) ? (__bf16)0.f : (__bf16)1.f;
+                  }
+                  hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, read_v(u, 2 * b + st)), see, hits, 0, 0, 0);
+                }
+#pragma unroll
+              for (int e = 0; e < 16; ++e) oacc[b][e] += hits[e] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+              asm volatile("" : "+v"(oacc[b]));  // added here, and not kept for later
+              __builtin_amdgcn_sched_barrier(0);
+            }
           }
         }
       }
@@ -1787,14 +1812,18 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
     };
     auto key_of = [&](int t) { return min(t * FW_KEYS4 + lane, kend - 1); };  // keys past the last repeat it
     auto id_of = [&](int t) { return row[key_of(t) >> a.shift]; };
+    auto none = [&](int id) { return (unsigned)id >= (unsigned)a.num_pages; };
+    // the lane's key's row of the pages (below 2^32), and the block of it that this lane has of key 16 u + m
+    auto place = [&](int t, int id) {
+      return (int)((((unsigned)(none(id) ? 0 : id) * a.Hkv + kvh) << a.shift) + (key_of(t) & ((1 << a.shift) - 1)));
+    };
+    auto row_of = [&](int mine, int u) { return (size_t)(unsigned)__builtin_amdgcn_ds_bpermute(4 * (16 * u + m), mine) * 4 + g; };
     auto load = [&](int t, int id, Codes& c) {
-      const bool bad = (unsigned)id >= (unsigned)a.num_pages;
-      c.bad = __ballot(bad);
-      // (below 2^32)
-      const unsigned mine = (((unsigned)(bad ? 0 : id) * a.Hkv + kvh) << a.shift) + (key_of(t) & ((1 << a.shift) - 1));
+      c.bad = __ballot(none(id));
+      const int mine = place(t, id);
       size_t r[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) r[u] = (size_t)(unsigned)__builtin_amdgcn_ds_bpermute(4 * (16 * u + m), (int)mine) * 4 + g;
+      for (int u = 0; u < 4; ++u) r[u] = row_of(mine, u);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         c.ks[u] = a.ksc[r[u]];
@@ -1807,6 +1836,12 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
       }
     };
     auto part_of = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
+    auto read_v = [&](int p, int d) {  // operand of 16 dims d, keys 32 p .. + 31
+      const uint8_t* at = (d & 1 ? vr1 : vr0) + (d >> 1) * FQ_VB + 2 * p * 1024;
+      const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)at);
+      const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(at + 1024));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
     // tile t from c, whose registers then take tile t + 2; id: its page
     auto step = [&](int t, Codes& c, int& id) {
       const unsigned long long bad = c.bad;
@@ -1819,25 +1854,16 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
           s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
               __builtin_bit_cast(bf16x8, values4(part_of(c.k[u], kk), __uint_as_float(c.ks[u] << 23))), bq[kk],
               kk ? s[u] : zero, 0, 0, 0);
-      // blocks of V that read as NaN: their codes go into the products as zeros, and NaN into the
-      // outputs of the rows that see them (a zero weight times NaN would be one)
-      const bool odd = __ballot(max(max(c.vs[0], c.vs[1]), max(c.vs[2], c.vs[3])) == 255) != 0;  // uniform
-      unsigned long long nans[4] = {0, 0, 0, 0};  // bit 16 b + k: block b of key 16 u + k
-      if (odd) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          nans[u] = __ballot(c.vs[u] == 255) & ~(((bad >> (16 * u)) & 0xFFFF) * 0x0001000100010001ull);
-          if (c.vs[u] == 255) {
-            c.vs[u] = 0;
-            c.v[u] = make_uint4(0, 0, 0, 0);
-          }
-        }
-      }
+      const bool odd = __ballot(max(max(c.vs[0], c.vs[1]), max(c.vs[2], c.vs[3])) >= ODD_SCALE) != 0;  // uniform
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           *reinterpret_cast<uint4*>(vw + u * 1024 + ((j ^ wswz) * 16)) = values4(part_of(c.v[u], j), __uint_as_float(c.vs[u] << 23));
+      if (__builtin_expect(odd, 0)) {
+#pragma unroll 1
+        for (int j = 0; j < 16; ++j) drop_odd(vw + (j >> 2) * 1024 + (((j & 3) ^ wswz) * 16));
+      }
       if (t + 2 < tend) {  // uniform
         load(t + 2, id, c);
         id = id_of(min(t + 3, tend - 1));
@@ -1872,12 +1898,7 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
       for (int p = 0; p < 2; ++p) {
         v8i16 vo[8];
 #pragma unroll
-        for (int d = 0; d < 8; ++d) {
-          const uint8_t* at = (d & 1 ? vr1 : vr0) + (d >> 1) * FQ_VB + 2 * p * 1024;
-          const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)at);
-          const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(at + 1024));
-          vo[d] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
+        for (int d = 0; d < 8; ++d) vo[d] = read_v(p, d);
         bf16x8 pb;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -1890,20 +1911,36 @@ __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
           oacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vo[d]), pb, oacc[d], 0, 0, 0);
       }
       lrun += (part[0] + part[1]) + (part[2] + part[3]);
-      if (odd) {
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          uint32_t hit = 0;
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
+      if (__builtin_expect(odd, 0)) {
+#pragma unroll 1
+        for (int sign = 0; sign < 2; ++sign) {
+          const int z = anew(), mine = place(t + z, id_of(t + z));
+#pragma unroll 1
+          for (int u = 0; u < 4; ++u) {
+            const size_t r = row_of(mine, u);
+            const uint4 w = reinterpret_cast<const uint4*>(vb)[r];
+            const float scale = __uint_as_float((uint32_t)a.vsc[r] << 23);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              hit |= 16 * u + j <= rel ? (uint32_t)(nans[u] >> (16 * b + 4 * g + j)) & 1 : 0;
-          hit |= xor16_u(hit);
-          hit |= xor32_u(hit);
-          const float add_nan = hit ? NAN : 0.f;
-          oacc[2 * b] += add_nan;
-          oacc[2 * b + 1] += add_nan;
+              *reinterpret_cast<uint4*>(vw + z + u * 1024 + ((j ^ wswz) * 16)) = odd_values(values4(part_of(w, j), scale), sign ? 0x80008000u : 0);
+          }
+#pragma unroll 1
+          for (int p = 0; p < 2; ++p) {
+            bf16x8 see;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int key = 32 * p + 16 * (j >> 2) + (j & 3);
+              see[j] = key > rel + z || ((bad >> (4 * g + key)) & 1) ? (__bf16)0.f : (__bf16)1.f;
+            }
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+              const f32x4 hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, read_v(p, d)), see, zero, 0, 0, 0);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) oacc[d][e] += hits[e] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+              asm volatile("" : "+v"(oacc[d]));  // added here: hits kept for later take registers of the loads in flight
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
         }
       }
     };
