@@ -741,7 +741,7 @@ typedef struct {
 } protokv_page_array;
 
 typedef struct {
-  int32_t num_copies;     /* n, >= 0 */
+  int32_t num_copies;     /* n, >= 0; above 8192 (a fork's most) n times the layers of all arrays < 2^24 */
   int32_t num_kv_heads, num_pages, page_size;
   int32_t num_arrays;     /* 1..128, with at most 65535 layers in all */
   const protokv_page_array* arrays;  /* host */

@@ -641,18 +641,26 @@ protokv_status protokv_page_copy(const protokv_page_copy_args* a, void* stream) 
   if (a->num_copies == 0) return PROTOKV_OK;
   if (!a->src || !a->dst || off4(a->src) || off4(a->dst) || off4(a->rows))
     return fail(PROTOKV_E_INVALID, who, "src and dst must be non-NULL, and they and rows aligned to 4 bytes");
+  // a launch has fewer than 2^32 threads: fewer workgroups to a page where there are many pages, and
+  // parts of the copies in launches of their own where that is not enough
+  const int64_t most_wgs = (1ll << 32) / 256 - 1;
+  if (layers * a->num_copies > most_wgs && a->num_copies > MAX_REQUESTS)
+    return fail(PROTOKV_E_UNSUPPORTED, who, "more than 8192 copies, and num_copies times the layers not below 2^24");
+  const int64_t each = std::min<int64_t>(a->num_copies, most_wgs / layers);  // (at least 256)
   // four units to a thread, up to 64 workgroups to a page
-  const int64_t parts = std::min<int64_t>((most + 1023) / 1024, 64);
-  if (parts * layers * a->num_copies >= (1ll << 32) / 256)
-    return fail(PROTOKV_E_UNSUPPORTED, who, "too many copies and layers for one launch");
+  const int64_t parts = std::min({(most + 1023) / 1024, (int64_t)64, most_wgs / (layers * each)});
   c.num_arrays = a->num_arrays;
   c.num_pages = a->num_pages;
   c.Hkv = a->num_kv_heads;
   c.shift = log2i(a->page_size);
-  c.src = a->src;
-  c.dst = a->dst;
-  c.rows = a->rows;
-  return device(launch_page_copy(c, a->num_copies, (int)layers, (unsigned)parts, (hipStream_t)stream), who);
+  for (int64_t i = 0; i < a->num_copies; i += each) {
+    c.src = a->src + i;
+    c.dst = a->dst + i;
+    c.rows = a->rows ? a->rows + i : nullptr;
+    s = device(launch_page_copy(c, (int)std::min(each, a->num_copies - i), (int)layers, (unsigned)parts, (hipStream_t)stream), who);
+    if (s != PROTOKV_OK) return s;
+  }
+  return PROTOKV_OK;
 })
 
 protokv_status protokv_page_release(const protokv_page_release_args* a, void* stream) PKV_GUARD("page_release", {
