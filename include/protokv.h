@@ -734,10 +734,11 @@ typedef struct {
 protokv_status protokv_page_fork(const protokv_page_fork_args* a, void* stream);
 
 typedef struct {
-  void* base;             /* device, aligned to 16 bytes: [layers][num_pages][num_kv_heads][page_size] rows */
+  void* base;             /* device, [layers][num_pages][num_kv_heads][page_size] rows; aligned to 16 bytes, to 4
+                           * if row_bytes is no multiple of 16 and layers follow one another without a gap */
   int32_t row_bytes;      /* a multiple of 4, up to 4096 */
   int32_t layers;         /* >= 1 */
-  int64_t layer_stride;   /* bytes between layers, a multiple of 16 (one layer: any) */
+  int64_t layer_stride;   /* bytes between layers: a layer's, or more and a multiple of 16 (one layer: any) */
 } protokv_page_array;
 
 typedef struct {

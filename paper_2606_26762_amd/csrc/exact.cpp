@@ -622,14 +622,18 @@ protokv_status protokv_page_copy(const protokv_page_copy_args* a, void* stream) 
   int64_t layers = 0, most = 0;
   for (int i = 0; i < a->num_arrays; ++i) {
     const protokv_page_array& x = a->arrays[i];
-    if (a->num_copies && (!x.base || off16(x.base))) return fail(PROTOKV_E_INVALID, who, "arrays: base must be non-NULL and aligned to 16 bytes");
     if (x.row_bytes < 4 || x.row_bytes > 4096 || x.row_bytes % 4)
       return fail(PROTOKV_E_INVALID, who, "arrays: row_bytes must be a multiple of 4 in [4, 4096]");
     if (x.layers < 1) return fail(PROTOKV_E_INVALID, who, "arrays: layers must be >= 1");
     const int64_t page = (int64_t)x.row_bytes * a->num_kv_heads * a->page_size;
     if (page >= (1ll << 31)) return fail(PROTOKV_E_UNSUPPORTED, who, "a page of 2^31 bytes or more");
-    if (x.layers > 1 && (x.layer_stride < page * a->num_pages || x.layer_stride % 16))
-      return fail(PROTOKV_E_INVALID, who, "arrays: layer_stride must hold the pages and be a multiple of 16");
+    // rows of 16 bytes each are copied by 16, others by 4, whose layers, one behind the other, need no more alignment
+    const bool gap = x.layers > 1 && x.layer_stride != page * a->num_pages, by4 = x.row_bytes % 16 && !gap;
+    if (a->num_copies && (!x.base || (by4 ? off4(x.base) : off16(x.base))))
+      return fail(PROTOKV_E_INVALID, who, "arrays: base must be non-NULL and aligned to 16 bytes (to 4 for rows that are no "
+                  "multiple of 16, if layers follow one another)");
+    if (gap && (x.layer_stride < page * a->num_pages || x.layer_stride % 16))
+      return fail(PROTOKV_E_INVALID, who, "arrays: layer_stride must be a layer's bytes, or more and a multiple of 16");
     c.base[i] = (uint8_t*)x.base;
     c.layer_stride[i] = x.layers > 1 ? x.layer_stride : 0;
     c.row_bytes[i] = x.row_bytes;

@@ -49,3 +49,22 @@ def test_page_copy_of_more_than_a_fork_s_most():
     pk.page_copy([x], src[:n], dst[:n])
     torch.cuda.synchronize()
     assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("layers,pages,hk,P,row", [(3, 7, 1, 1, 4), (5, 9, 1, 2, 4), (2, 5, 3, 1, 12), (4, 3, 1, 1, 20)])
+def test_page_copy_of_rows_that_are_no_multiple_of_16(layers, pages, hk, P, row):
+    """Scales of pages of one or two tokens: layers that do not begin at multiples of 16 bytes, in one array, each
+    by itself, and beside an array of 64-byte rows."""
+    import torch
+    log(f"case: page_copy of {layers} layers of {pages} pages of {hk} x {P} rows of {row}")
+    pk, g = PK(), _g(72)
+    src, dst, rows = [0, 2, -1], [1, pages - 1, 0], [P, P, P]
+    x = torch.randint(0, 256, (layers, pages, hk, P, row), generator=g, device="cuda", dtype=torch.uint8)
+    y = torch.randint(0, 256, (layers, pages, hk, P, 64), generator=g, device="cuda", dtype=torch.uint8)
+    want = [_copied(t, src, dst, rows) for t in (x, y)]
+    a, b = x.clone(), x.clone()
+    pk.page_copy([a, y], _i32(src), _i32(dst))
+    for layer in b:
+        pk.page_copy([layer], _i32(src), _i32(dst), _i32(rows))
+    torch.cuda.synchronize()
+    assert torch.equal(a, want[0]) and torch.equal(b, want[0]) and torch.equal(y, want[1])
