@@ -123,6 +123,8 @@ __device__ __forceinline__ void rotate_rows(const RotateArgs& a, const NormArgs&
       if (inv < 0x1p-100 || inv > 0x1p100) {  // near float32's ends a power of two comes first (products in float64: 5% longer)
         const float by = inv < 1.0 ? 0x1p-64f : 0x1p100f;
         inv *= inv < 1.0 ? 0x1p64 : 0x1p-100;
+        // beyond 2^53 now only of a head of zeros, which stays zeros for any eps above 0
+        if (inv < 0x1p1000) inv = fmin(inv, 0x1p100);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           x[i] *= by;
