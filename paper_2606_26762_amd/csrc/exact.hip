@@ -46,15 +46,14 @@ struct Item {
 };
 
 // Row block blk of sequence i, whose rows are c0 .. c1 - 1; false if there is none.
-// FEW: a request of at most so many rows is not the row blocks' (0: few_limit).
-template <int R, int FEW = EX_FEW>
+template <int R>
 __device__ __forceinline__ bool set_item(const ExactArgs& a, int i, int c0, int c1, int blk, Item& it) {
   it.seq = i;
   it.s0 = c0;
   it.add = c1 - c0;
   if (it.add <= 0 || blk < 0) return false;
   it.rows = min(it.add, a.max_add) * a.grp;
-  if (blk >= (it.rows + R - 1) / R || (a.few && it.rows <= (FEW ? FEW : a.few_limit))) return false;
+  if (blk >= (it.rows + R - 1) / R || (a.few && it.rows <= EX_FEW)) return false;
   it.row0 = blk * R;
   int kv = it.add;
   it.off = 0;
@@ -71,7 +70,7 @@ __device__ __forceinline__ bool set_item(const ExactArgs& a, int i, int c0, int 
 // f(i) = floor(cu[i] grp / R) + i, non-decreasing, so it is found by comparing 64
 // entries at a time; indices behind a sequence's rows are left empty.  Every
 // lane of the wave takes part; false (uniform) if the block is empty.
-template <int R, int FEW = EX_FEW>
+template <int R>
 __device__ __forceinline__ bool find_item(const ExactArgs& a, int b, Item& it) {
   const int lane = threadIdx.x & 63;
   auto entry = [&](int i) { return min(max(a.cu[i], 0), a.total); };
@@ -91,7 +90,7 @@ __device__ __forceinline__ bool find_item(const ExactArgs& a, int b, Item& it) {
     lo += l * step;
     hi = min(hi, lo + step);
   }
-  return set_item<R, FEW>(a, lo, c0, c1, b - first(c0, lo), it);
+  return set_item<R>(a, lo, c0, c1, b - first(c0, lo), it);
 }
 
 // The sum of x over the wave.
@@ -288,7 +287,7 @@ __global__ __launch_bounds__(512, 1) void k_exact_bf16(ExactArgs a) {
   Item it;
   constexpr int ROWS = EX_ROWS / KH;
   if (!PAGED && a.n <= 64 ? !find_dearest<ROWS>(a, a.blocks - 1 - blk, it)
-                          : !find_item<ROWS, PAGED == 2 ? 0 : EX_FEW>(a, blk, it))
+                          : !find_item<ROWS>(a, blk, it))
     return;  // uniform in the workgroup
   int per;
   const int tiles = (it.kend + EX_KEYS - 1) / EX_KEYS;
@@ -1099,12 +1098,12 @@ struct Sum {
 // block), 32 threads per row.  A latency chain: block, references, partials (3 x 20
 // rows over 2500 tokens in float32 5.3 us).
 constexpr int EJ_ROWS = 16;
-template <int FP32, int R, int FEW>
+template <int FP32, int R>
 __global__ __launch_bounds__(EJ_ROWS * 32) void k_exact_join(ExactArgs a) {
   const int part = blockIdx.x % (R / EJ_ROWS), rest = blockIdx.x / (R / EJ_ROWS);
   const int kvh = rest % a.Hkv, blk = rest / a.Hkv;
   Item it;
-  if (!find_item<R, FEW>(a, blk, it)) return;
+  if (!find_item<R>(a, blk, it)) return;
   int per;
   const int tiles = (it.kend + (FP32 ? EX_KEYS32 : EX_KEYS) - 1) / (FP32 ? EX_KEYS32 : EX_KEYS);
   const int nsp = ex_splits(a.splits, tiles, per);
@@ -2065,12 +2064,9 @@ hipError_t launch_exact(const ExactArgs& a, bool fp32, Keys keys, hipStream_t st
   }
   if (a.splits > 1) {
     const dim3 joins(a.Hkv * a.blocks * (a.rows / EJ_ROWS)), threads(EJ_ROWS * 32);
-    const bool four = keys == Keys::PAGES4;
-    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32, EX_FEW>), joins, threads, 0, st, a);
-    else if (a.rows == EX_ROWS && four) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS, 0>), joins, threads, 0, st, a);
-    else if (a.rows == EX_ROWS) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS, EX_FEW>), joins, threads, 0, st, a);
-    else if (four) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2, 0>), joins, threads, 0, st, a);
-    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2, EX_FEW>), joins, threads, 0, st, a);
+    if (fp32) hipLaunchKernelGGL((k_exact_join<1, EX_ROWS_F32>), joins, threads, 0, st, a);
+    else if (a.rows == EX_ROWS) hipLaunchKernelGGL((k_exact_join<0, EX_ROWS>), joins, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_exact_join<0, EX_ROWS / 2>), joins, threads, 0, st, a);
   }
   return hipGetLastError();
 }
