@@ -563,8 +563,15 @@ typedef struct {
  * such as a layer of protokv_attend's) o and lse are those over both:
  * lse = log(e^own + e^prior), o weighted by e^(own - lse) and e^(prior - lse);
  * a prior_lse of -inf leaves prior_o unread.  o and lse may be the prior's
- * own arrays (o prior_o and lse prior_lse).  Fewer than 2^23 row blocks: rows * Hq
- * / 128 and sequences * Hkv together. */
+ * own arrays (o prior_o and lse prior_lse).
+ * Scores, sums, lse and o are formed in float32.  With kv_dtype bfloat16 the
+ * softmax weights are rounded to bfloat16 for their product with V (the sum is of
+ * the unrounded ones): with A the weights' mean of |v|, o is off by up to 2^-8
+ * (A + |o|) from that and by 2^-8 |o| from its own rounding.  Before the division
+ * by their sum weights reach 2^8 there (1 in float32), so that finite values
+ * beyond 2^119 / keys (2^127 / keys) may overflow to infinity.  All of this holds
+ * for the calls over pages too.
+ * Fewer than 2^23 row blocks: rows * Hq / 128 and sequences * Hkv together. */
 protokv_status protokv_prompt_attend(const protokv_prompt_args* a, void* stream);
 
 typedef struct {
@@ -682,7 +689,9 @@ typedef struct {
 } protokv_page4_attend_args;
 
 /* protokv_page_attend over a cache in 4 bits: every rule of that call, with the
- * values that the cache holds, which enter the products exactly. */
+ * values that the cache holds, which enter the products exactly (the weights of
+ * bfloat16 calls are rounded as there).  Values that are not finite (s = 253 and
+ * more) reach the rows that see them and no others. */
 protokv_status protokv_page4_attend(const protokv_page4_attend_args* a, void* stream);
 
 /* Bytes of workspace for these sizes, as protokv_page_attend_workspace.  Host only. */

@@ -274,7 +274,7 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
     // idle and a long context among short ones holds one for its whole length.  A wave's tile of 64
     // keys counts 16 of plan_blocks' tenths where the waves fill the GPU, else 10, launches and join
     // 60, and a fifth on top, which the blocks' count is closer by.  28 / 4 heads: 64 x 16 tokens
-    // over 8000 327 us by blocks, 218; 8 x 40 over 250 to 16 000, 32 / 8 heads, 109 and 58; but 8 x 512
+    // over 8000 327 us a call by blocks, 205 to 220 so; 8 x 40 over 250 to 16 000, 32 / 8 heads, 109 and 58; but 8 x 512
     // over 16 000 895 and 1300, one chunk of 64 over 30 000 49 and 61.  Over 96 shapes of 1 to 64 requests
     // this choice took 2.5 % longer than the better of the two on average, 38 % at most.
     const int64_t groups = many ? rows / EX_FEW + a.n : a.n, tiles = a.Hkv * groups * ((span + 63) / 64);

@@ -1513,8 +1513,9 @@ __device__ __forceinline__ void few4_runs(const ExactArgs& a, int w, ITEM item) 
 // once the one before is used.  The weights are rounded to bfloat16 for the second product, as in the
 // other kernels here.  Tiles of 64 keys: two chains of products side by side, and the maximum, its
 // exchange and its test once (tiles of 32, 8 x 40 tokens over 16 000, 32 / 8 heads: 140 us, of 64 125).  Bound by
-// the VALU and the matrix cores in turn, with two waves to a SIMD: 400 instructions and 32 products to a tile,
-// 64 x 16 tokens over 8000, 28 / 4 heads, 218 us, 0.54 PFLOP/s of what is seen.
+// the VALU and the matrix cores in turn, with two waves to a SIMD: 400 instructions and 32 products to a tile, of
+// which 128 convert codes that the request's other groups of rows convert again (64 x 16 tokens over 8000, 28 / 4 heads,
+// four groups: 205 - 220 us a call, the join's 27 among them, 0.53 - 0.57 PFLOP/s of what is seen, for 94 us of bytes or products).
 __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4(ExactArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][2 * 4 * FW_VB];  // V of a tile, by its halves of 32 keys
   const int lane = threadIdx.x & 63;
@@ -1767,7 +1768,10 @@ __device__ __forceinline__ float xor16(float v) { return __uint_as_float(xor16_u
 // scores of keys 16 u + 4 g .. + 3 are its lane g's, and those of two u are a P operand as they
 // are, V's transposed reads taking their keys in that order.  Bound by the cache's bytes: 64 tokens over
 // 32 768, 28 / 4 heads, 1.14 GB, 219 us with the join, 5.2 TB/s (by 32 rows 229); over contexts of 500 to 32 768,
-// 0.35 GB, 75 us and the join's 9; one token over 1500 9 us, a chain of one or two tiles.
+// 0.35 GB, 73 us and the join's 9; one token over 1500 9 us, a chain of one or two tiles.  The weights are rounded to
+// bfloat16 here too, though the matrix cores would have time for more: with a second product of what the rounding leaves
+// over, outputs are within 1.65e-3 of float64's (relative, in the mean square; their own rounding) in place of 2.30e-3,
+// but the registers that it takes are those of the loads in flight (ragged contexts 80 -> 91 us, 64 x 32 768 219 -> 235).
 constexpr int FQ_VB = FW_KEYS4 * 64 + 64;  // bytes of one 32-dim block of a V tile
 __global__ __launch_bounds__(FW_W * 64, 2) void k_exact_few4_16(ExactArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t s_mem[FW_W][4 * FQ_VB];

@@ -145,7 +145,13 @@ __global__ __launch_bounds__(256) void k_page4_read(Page4Rows a) {
 // else a second launch does that, with workgroups to each fork.  Latency chains both.
 // ---------------------------------------------------------------------------
 constexpr int FK_NT = 1024;
-constexpr int PG_FEW = 16384;  // table entries, and pages, that one workgroup goes through by itself
+// Table entries, and pages, that one workgroup goes through by itself.  Both sides, microseconds of kernels at 1024, 4096,
+// 8192, 16 384 and 32 768 entries: forks of 64 requests, four each, 4.8, 7.9, 13.4, 26.6, 52.6 by one workgroup and 5.9,
+// 6.6, 6.6, 6.7, 7.8 by two launches; a third of 256 requests released 4.6, 6.9, 12.3, 22.1, 43.3 and 7.4, 8.5, 8.8, 8.9,
+// 9.4 by three; of 8 requests, which three waves go through there, 4.6, 7.1, 12.9, 23.6, 47.3 and 7.5, 11.5, 15.7, 25.2,
+// 42.6.  The sides meet near 3500 entries for forks and between 5000 and 20 000 for releases: forks above that, and
+// releases of many requests, would be faster with a lower limit.
+constexpr int PG_FEW = 16384;
 constexpr int PG_REQ = 2048;   // and requests
 
 // Inclusive running sum over the workgroup's threads; total: of all.  s: FK_NT / 64
@@ -464,8 +470,12 @@ static void page4_rows(const Page4Rows& a, bool store, hipStream_t st) {
 }
 
 hipError_t launch_page4_rows(const Page4Rows& a, bool fp32, bool store, hipStream_t st) {
-  // four pieces to a thread where one would take more than 8192 workgroups (store and read, 8 heads:
-  // 64 tokens of 4 heads 2.9 + 3.0 us with one, 4.0 + 3.6 with four; 18 432 tokens 51 and 44, float32 93 and 84)
+  // four pieces to a thread where one would take more than 8192 workgroups.  A store and the read of the same rows behind it,
+  // 8 heads, one, two and four pieces: 18 432 tokens 50.2, 45.3 and 44.6 us, float32 91.0, 84.6 and 84.2, 8000 of float32
+  // (16 000 workgroups) 33.6, 31.2 and 31.0; fewer are as long as the host's part of the two calls.  The kernels of
+  // small calls: 64 tokens of 4 heads 2.4 + 2.3 with one, 3.5 + 2.7 with four, 2048 of 8 (2048 workgroups) 5.2 + 4.8 and
+  // 6.6 + 5.3, 4608 8.8 + 9.2 and 9.7 + 8.5, 8000 13.3 + 14.3 and 14.7 + 12.9 (their rows not in a cache; the store
+  // alone has nothing from more pieces there, the read has from about 4000 workgroups on)
   const bool many = a.rows * (fp32 ? 32 : 16) > 8192 * 256;
   if (fp32 && many) page4_rows<1, 4>(a, store, st);
   else if (fp32) page4_rows<1, 1>(a, store, st);

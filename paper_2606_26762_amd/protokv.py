@@ -734,7 +734,9 @@ def page_plan(ctx, add, table, free_pages, count, page_size: int, max_tokens: in
     """protokv_page_plan: one step's slots, positions and lengths from the requests'
     held (ctx) and new (add, < 0: over) tokens, int32 [n]; table int32 [n][width] and
     the stack free_pages [num_pages] are updated in place, count [1] is not
-    (count_out or a new tensor holds the pages left).  The results are parts of one
+    (count_out or a new tensor holds the pages left).  add < 0 gives back a request's
+    pages whoever else holds them: once some may be shared (``page_fork``), requests are
+    ended by ``page_release``, and their add is 0 here.  The results are parts of one
     new tensor."""
     import torch
     dev, i32, n = _device(ctx, stream), torch.int32, ctx.shape[0]
@@ -862,8 +864,8 @@ def page4_read(pages, slots, dtype, *, k_out=None, v_out=None, stream=None):
 
 
 def page4_attend(q, pages, table, cu, kv_len, max_add: int, *, out=None, lse=None, prior=None, workspace=None, stream=None):
-    """protokv_page4_attend: ``page_attend`` over pages of 4 bits (as in ``page4_store``).
-    -> (o, lse); lse=False: none."""
+    """protokv_page4_attend: ``page_attend`` over pages of 4 bits (as in ``page4_store``), the softmax weights
+    of bfloat16 calls rounded to bfloat16 as there.  -> (o, lse); lse=False: none."""
     import torch
     dev, dtype, i32, f32 = _device(q, stream), q.dtype, torch.int32, torch.float32
     qp, qs = _rows(q, "q", dtype, dev)
