@@ -273,10 +273,10 @@ protokv_status page_attend_shape(const protokv_page_attend_args* p, ExactArgs& a
     // whatever the lengths, where a row block of few rows leaves most of its compute unit
     // idle and a long context among short ones holds one for its whole length.  A wave's tile of 64
     // keys counts 16 of plan_blocks' tenths where the waves fill the GPU, else 10, launches and join
-    // 60, and a fifth on top, which the blocks' count is closer by.  28 / 4 heads: 64 x 16 tokens
-    // over 8000 327 us a call by blocks, 205 to 220 so; 8 x 40 over 250 to 16 000, 32 / 8 heads, 109 and 58; but 8 x 512
-    // over 16 000 895 and 1300, one chunk of 64 over 30 000 49 and 61.  Over 96 shapes of 1 to 64 requests
-    // this choice took 2.5 % longer than the better of the two on average, 38 % at most.
+    // 60, and a fifth on top, which the blocks' count is closer by.  Calls by row blocks and by groups, 28 / 4 heads: 64 x 16
+    // tokens over 8000 328 and 207 us; 8 x 40 over 250 to 16 000, 32 / 8 heads, 105 and 55; but 8 x 512 over 16 000 890
+    // and 1268, one chunk of 64 over 30 000 49 and 61.  Over 100 shapes of 1 to 64 requests this choice took
+    // 1.8 % longer than the better of the two on average, 29 % at most.
     const int64_t groups = many ? rows / EX_FEW + a.n : a.n, tiles = a.Hkv * groups * ((span + 63) / 64);
     const int64_t run = std::max<int64_t>({(tiles + EX_FEW_WAVES - 1) / EX_FEW_WAVES, std::min<int64_t>(EX_FEW_RUN4, (tiles + 511) / 512), 1});
     const bool all = many && (run * (tiles > 1024 * run ? 16 : 10) + 60) * 6 / 5 <= cost;
